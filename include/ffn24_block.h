@@ -1,0 +1,44 @@
+/* ffn24_block -- the operators around the feed-forward block: layer norm, the gated feed-forward block, int8 products.
+ *
+ * C ABI of libffn24.so, the second half.  ffn24.h has the conventions that hold here too: device pointers owned by the caller, row-major,
+ * contiguous and 16-byte aligned; `stream` a hipStream_t (NULL = the default stream); calls only enqueue kernels, they neither synchronise nor
+ * allocate device memory (the *_ctx_create calls allocate); return values FFN24_OK or a negative FFN24_ERR_* code; bad arguments are rejected
+ * before anything is launched; outputs are overwritten.  No call keeps a tensor's address: a backward is handed what it needs again.  An output must not
+ * overlap an input or another output unless the call says so.  T == 0 is a no-op everywhere (gradients of weights are then zero).
+ *
+ * Together they are the pre-norm gated feed-forward sublayer, the baseline that the paper's Table 1 compares 2:4 activation sparsity with
+ * (SwiGLU): layer_norm_fwd, gated_fwd, gated_bwd, layer_norm_bwd in training, layer_norm_fwd and gated_i8_fwd in int8 serving.
+ */
+#ifndef FFN24_BLOCK_H
+#define FFN24_BLOCK_H
+
+#include "ffn24.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* Element type of a norm's tokens. */
+typedef enum { FFN24_NORM_BF16 = 0, FFN24_NORM_F32 = 1 } ffn24_norm_dtype;
+
+/* Layer norm of T tokens of D values, 1 <= D <= 16384, with an optional residual in front:
+ *   S = X + R, rounded to the element type (R == NULL: S is X itself, and the S argument must be NULL);
+ *   mean[t] = sum_d S / D;  rstd[t] = 1 / sqrt(sum_d (S - mean)^2 / D + eps);  Y = (S - mean) rstd weight + bias.
+ * weight, bias fp32 [D], bias may be NULL (no bias); mean, rstd fp32 [T], both may be NULL (a forward without a backward).  Statistics in fp32, the
+ * variance from the centred values.  eps > 0.  S may be X or R (in place); Y may be S's or X's buffer if the caller needs neither. */
+FFN24_API int layer_norm_fwd(const void* X, const void* R, const float* weight, const float* bias, int64_t T, int64_t D, float eps,
+                             ffn24_norm_dtype dtype, void* S, void* Y, float* mean, float* rstd, void* stream);
+
+/* Its backward.  With xh = (S - mean) rstd and p = dY weight:
+ *   dX = rstd (p - sum_d p / D - xh sum_d (p xh) / D) + dS;   dweight[d] = sum_t dY xh;   dbias[d] = sum_t dY.
+ * S is what the forward normalised.  dS, the gradient that reaches S along the residual stream, may be NULL (0); dX is the gradient of X and of R.  dX
+ * may be dS's buffer.  dbias may be NULL.  scratch: layer_norm_bwd_scratch(T, D) bytes of device memory, used until the call's last kernel has run.  The sums over tokens
+ * are added in an order that depends on T and D alone: results repeat bit for bit. */
+FFN24_API int64_t layer_norm_bwd_scratch(int64_t T, int64_t D);   /* bytes, or -1 for sizes out of range */
+FFN24_API int layer_norm_bwd(const void* dY, const void* S, const float* weight, const float* mean, const float* rstd, const void* dS, int64_t T,
+                             int64_t D, ffn24_norm_dtype dtype, void* dX, float* dweight, float* dbias, void* scratch, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* FFN24_BLOCK_H */
