@@ -38,6 +38,28 @@ FFN24_API int64_t layer_norm_bwd_scratch(int64_t T, int64_t D);   /* bytes, or -
 FFN24_API int layer_norm_bwd(const void* dY, const void* S, const float* weight, const float* mean, const float* rstd, const void* dS, int64_t T,
                              int64_t D, ffn24_norm_dtype dtype, void* dX, float* dweight, float* dbias, void* scratch, void* stream);
 
+/* Gated feed-forward block, bf16 with fp32 accumulation: with Wgu [D][2 F] = [Wg | Wu] (a row of it: F gate columns, then F up columns) and Wd [F][D],
+ *   [G | U] = X Wgu;   H = bf16(a(G) U);   Y = H Wd.
+ * Gate activations: a(x) = x / (1 + exp(-x)) (SwiGLU), and GELU in its tanh form, a(x) = x / (1 + exp(-2 sqrt(2/pi) (x + 0.044715 x^3))) (GEGLU). */
+typedef enum { FFN24_GATE_SILU = 0, FFN24_GATE_GELU_TANH = 1 } ffn24_gate;
+typedef struct gated_ctx gated_ctx; /* opaque; owns only its device workspace */
+
+/* A context for up to T tokens (1 <= T <= 2^20; every call says how many it has, any number up to T), D and F multiples of 64, at most 2^18.
+ * flags: 0 or FFN24_TRAINING (gated_bwd).  Workspace, allocated on the current device: 2 T F bytes; 10 T F with FFN24_TRAINING.  A context belongs to that
+ * device and to one thread at a time; calls on different streams are the caller's to order.  *out is untouched on error. */
+FFN24_API int gated_ctx_create(gated_ctx** out, int64_t T, int64_t D, int64_t F, ffn24_gate gate, int flags);
+/* The caller must have synchronised every stream that used the context.  NULL is allowed. */
+FFN24_API int gated_ctx_destroy(gated_ctx* ctx);
+
+/* X [T][D] -> Y [T][D], 0 <= T <= the context's.  The weights are read where they lie.  A training context keeps G, U and H in bf16 for gated_bwd. */
+FFN24_API int gated_fwd(gated_ctx* ctx, const void* X, int64_t T, const void* Wgu, const void* Wd, void* Y, void* stream);
+
+/* Backward of the context's last gated_fwd (FFN24_ERR_STATE without one, or without FFN24_TRAINING): dY [T][D] with that call's T, and its X, Wgu, Wd again:
+ *   dH = dY Wd^T;  dG = bf16(dH U a'(G));  dU = bf16(dH a(G));
+ *   dX = dG Wg^T + dU Wu^T;  dWgu = X^T [dG | dU];  dWd = H^T dY        (bf16 [T][D], [D][2 F], [F][D])
+ * It may be called more than once for a forward. */
+FFN24_API int gated_bwd(gated_ctx* ctx, const void* dY, const void* X, const void* Wgu, const void* Wd, void* dX, void* dWgu, void* dWd, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -12,7 +12,7 @@ import torch
 from . import ffn24
 from .ffn24 import Ffn24Error, _BF16, _F32, _check, _expect, _ptr, _stream  # noqa: F401
 
-EXPORTS = ("layer_norm_fwd", "layer_norm_bwd_scratch", "layer_norm_bwd")
+EXPORTS = ("layer_norm_fwd", "layer_norm_bwd_scratch", "layer_norm_bwd", "gated_ctx_create", "gated_ctx_destroy", "gated_fwd", "gated_bwd")
 
 _lib = None
 
@@ -26,6 +26,10 @@ def lib() -> ctypes.CDLL:
         L.layer_norm_fwd.argtypes = [vp, vp, vp, vp, i64, i64, f32, ci, vp, vp, vp, vp, vp]
         L.layer_norm_bwd_scratch.argtypes = [i64, i64]
         L.layer_norm_bwd.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, ci, vp, vp, vp, vp, vp]
+        L.gated_ctx_create.argtypes = [ctypes.POINTER(vp), i64, i64, i64, ci, ci]
+        L.gated_ctx_destroy.argtypes = [vp]
+        L.gated_fwd.argtypes = [vp, vp, i64, vp, vp, vp, vp]
+        L.gated_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp]
         for name in EXPORTS:
             getattr(L, name).restype = ci
         L.layer_norm_bwd_scratch.restype = i64
@@ -71,3 +75,71 @@ def layer_norm_bwd(dY, S, weight, mean, rstd, dS=None):
     _check(lib().layer_norm_bwd(_ptr(dY), _ptr(S), _ptr(weight), _ptr(mean), _ptr(rstd), _ptr(dS), T, D, _NORM_TYPES[S.dtype], _ptr(dX), _ptr(dw), _ptr(db),
                                 _ptr(scratch), _stream()), "layer_norm_bwd")
     return dX, dw, db
+
+
+# ---------------------------------------------------------------------------------------------- gated feed-forward block
+GATES = {"silu": 0, "gelu": 1}
+
+
+def _gate(act: str) -> int:
+    if act not in GATES:
+        raise ValueError(f"act: {act!r}, expected one of {tuple(GATES)}")
+    return GATES[act]
+
+
+class _Handle:
+    """Owns a context of the library; the subclass names its destructor."""
+    _h = None
+    _destroy = ""
+
+    def close(self):
+        if self._h:
+            torch.cuda.synchronize()
+            _check(getattr(lib(), self._destroy)(self._h), self._destroy)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class GatedContext(_Handle):
+    """The gated feed-forward block (see gated_ctx in the header) for up to T tokens: Y = (a(X Wg) * (X Wu)) Wd with Wgu = [Wg | Wu] [D, 2 F], Wd [F, D],
+    all bf16; act "silu" or "gelu" (its tanh form)."""
+    _destroy = "gated_ctx_destroy"
+
+    def __init__(self, T: int, D: int, F: int, act: str = "silu", training: bool = False):
+        self.T, self.D, self.F, self.training = T, D, F, training
+        h = ctypes.c_void_p()
+        _check(lib().gated_ctx_create(ctypes.byref(h), T, D, F, _gate(act), ffn24.FFN24_TRAINING if training else 0), "gated_ctx_create")
+        self._h = h
+
+    def _expect_weights(self, Wgu, Wd):
+        _expect(Wgu, (self.D, 2 * self.F), _BF16, "Wgu")
+        _expect(Wd, (self.F, self.D), _BF16, "Wd")
+
+    def fwd(self, X, Wgu, Wd, Y=None):
+        """X [t, D] with any t up to T -> Y [t, D]."""
+        t = X.shape[0]
+        _expect(X, (t, self.D), _BF16, "X")
+        self._expect_weights(Wgu, Wd)
+        Y = torch.empty_like(X) if Y is None else Y
+        _expect(Y, (t, self.D), _BF16, "Y")
+        _check(lib().gated_fwd(self._h, _ptr(X), t, _ptr(Wgu), _ptr(Wd), _ptr(Y), _stream()), "gated_fwd")
+        self._t = t
+        return Y
+
+    def bwd(self, dY, X, Wgu, Wd, out=None):
+        """Gradients of the last fwd, which had this X and these weights: (dX, dWgu, dWd)."""
+        t = getattr(self, "_t", X.shape[0])
+        _expect(dY, (t, self.D), _BF16, "dY")
+        _expect(X, (t, self.D), _BF16, "X")
+        self._expect_weights(Wgu, Wd)
+        dX, dWgu, dWd = (torch.empty_like(X), torch.empty_like(Wgu), torch.empty_like(Wd)) if out is None else out
+        _expect(dX, (t, self.D), _BF16, "dX")
+        _expect(dWgu, (self.D, 2 * self.F), _BF16, "dWgu")
+        _expect(dWd, (self.F, self.D), _BF16, "dWd")
+        _check(lib().gated_bwd(self._h, _ptr(dY), _ptr(X), _ptr(Wgu), _ptr(Wd), _ptr(dX), _ptr(dWgu), _ptr(dWd), _stream()), "gated_bwd")
+        return dX, dWgu, dWd

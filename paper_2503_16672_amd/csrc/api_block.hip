@@ -8,10 +8,35 @@ using namespace ffn24;
 
 namespace {
 constexpr int64_t MAX_TOKENS = 1 << 24;   // (row counts and grids stay within 32 bits)
+constexpr int64_t MAX_CTX_TOKENS = 1 << 20, MAX_WIDTH = 1 << 18;
 
 template <class... P> bool misaligned(const P*... p) { return ((reinterpret_cast<uintptr_t>(p) | ...) & 15u) != 0; }
 int done(int rc) { return rc ? FFN24_ERR_HIP : FFN24_OK; }
+
+struct GateCoefficients { float c1, c3; };
+constexpr float GELU_C1 = 1.5957691216057308f;   // 2 sqrt(2 / pi)
+GateCoefficients coefficients(ffn24_gate g) { return g == FFN24_GATE_SILU ? GateCoefficients{1.f, 0.f} : GateCoefficients{GELU_C1, GELU_C1 * 0.044715f}; }
+
+// the checks that the contexts share
+int check_sizes(int64_t T, int64_t D, int64_t F, ffn24_gate gate) {
+  if (gate != FFN24_GATE_SILU && gate != FFN24_GATE_GELU_TANH) return FFN24_ERR_DTYPE;
+  if (T < 1 || T > MAX_CTX_TOKENS || D < 64 || D > MAX_WIDTH || D % 64 || F < 64 || F > MAX_WIDTH || F % 64) return FFN24_ERR_SHAPE;
+  return FFN24_OK;
+}
+int check_device(int device) {
+  int dev = -1;
+  if (hipGetDevice(&dev) != hipSuccess) return FFN24_ERR_HIP;
+  return dev == device ? FFN24_OK : FFN24_ERR_STATE;
+}
 }  // namespace
+
+struct gated_ctx {
+  int64_t T, D, F;
+  GateCoefficients gate;
+  int training, device;
+  int64_t fwd_T;               // tokens of the last forward, -1: none yet
+  void *H, *GU, *dGU;          // [T][F], and in training [T][2 F] twice
+};
 
 extern "C" {
 
@@ -38,6 +63,65 @@ int layer_norm_bwd(const void* dY, const void* S, const float* weight, const flo
   if (misaligned(dY, S, weight, mean, rstd, dS, dX, dweight, dbias, scratch)) return FFN24_ERR_ALIGN;
   return done(launch_norm_bwd(dY, S, weight, mean, rstd, dS, (int)T, (int)D, dtype == FFN24_NORM_F32, dX, dweight, dbias, static_cast<float*>(scratch),
                               static_cast<hipStream_t>(stream)));
+}
+
+int gated_ctx_create(gated_ctx** out, int64_t T, int64_t D, int64_t F, ffn24_gate gate, int flags) {
+  if (!out) return FFN24_ERR_NULL;
+  if (int rc = check_sizes(T, D, F, gate)) return rc;
+  if (flags & ~FFN24_TRAINING) return FFN24_ERR_STATE;
+  gated_ctx* c = new (std::nothrow) gated_ctx();
+  if (!c) return FFN24_ERR_HIP;
+  c->T = T; c->D = D; c->F = F; c->gate = coefficients(gate);
+  c->training = flags & FFN24_TRAINING; c->fwd_T = -1;
+  const size_t tf = (size_t)T * (size_t)F;
+  bool ok = hipGetDevice(&c->device) == hipSuccess && hipMalloc(&c->H, 2 * tf) == hipSuccess;
+  if (ok && c->training) ok = hipMalloc(&c->GU, 4 * tf) == hipSuccess && hipMalloc(&c->dGU, 4 * tf) == hipSuccess;
+  if (!ok) {
+    (void)hipGetLastError();
+    gated_ctx_destroy(c);
+    return FFN24_ERR_HIP;
+  }
+  *out = c;
+  return FFN24_OK;
+}
+
+int gated_ctx_destroy(gated_ctx* c) {
+  if (!c) return FFN24_OK;
+  int bad = 0;
+  for (void* p : {c->H, c->GU, c->dGU}) if (p && hipFree(p) != hipSuccess) bad = 1;
+  delete c;
+  return bad ? FFN24_ERR_HIP : FFN24_OK;
+}
+
+int gated_fwd(gated_ctx* c, const void* X, int64_t T, const void* Wgu, const void* Wd, void* Y, void* stream) {
+  if (!c) return FFN24_ERR_NULL;
+  if (T < 0 || T > c->T) return FFN24_ERR_SHAPE;
+  if (T > 0 && (!X || !Wgu || !Wd || !Y)) return FFN24_ERR_NULL;
+  if (misaligned(X, Wgu, Wd, Y)) return FFN24_ERR_ALIGN;
+  if (int rc = check_device(c->device)) return rc;
+  c->fwd_T = -1;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const int t = (int)T, D = (int)c->D, F = (int)c->F;
+  if (T > 0) {
+    if (launch_gated_up(X, Wgu, t, D, F, c->gate.c1, c->gate.c3, c->H, c->GU, s)) return FFN24_ERR_HIP;
+    if (launch_gated_down(c->H, Wd, t, D, F, Y, s)) return FFN24_ERR_HIP;
+  }
+  c->fwd_T = T;
+  return FFN24_OK;
+}
+
+int gated_bwd(gated_ctx* c, const void* dY, const void* X, const void* Wgu, const void* Wd, void* dX, void* dWgu, void* dWd, void* stream) {
+  if (!c) return FFN24_ERR_NULL;
+  if (!c->training || c->fwd_T < 0) return FFN24_ERR_STATE;
+  if (!dWgu || !dWd || (c->fwd_T > 0 && (!dY || !X || !Wgu || !Wd || !dX))) return FFN24_ERR_NULL;
+  if (misaligned(dY, X, Wgu, Wd, dX, dWgu, dWd)) return FFN24_ERR_ALIGN;
+  if (int rc = check_device(c->device)) return rc;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const int t = (int)c->fwd_T, D = (int)c->D, F = (int)c->F;
+  if (t == 0) return done(launch_zero(dWgu, (size_t)4 * D * F, s) || launch_zero(dWd, (size_t)2 * D * F, s));
+  if (launch_gated_dgate(dY, Wd, c->GU, t, D, F, c->gate.c1, c->gate.c3, c->dGU, s)) return FFN24_ERR_HIP;
+  if (launch_gated_dx(c->dGU, Wgu, t, D, F, dX, s)) return FFN24_ERR_HIP;
+  return done(launch_gated_wgrad(X, dY, c->H, c->dGU, t, D, F, dWgu, dWd, s));
 }
 
 }  // extern "C"

@@ -1,0 +1,242 @@
+// Epilogues of the gated block's and the int8 products' GEMMs, whose results may end anywhere inside a tile: what lies beyond M or N is not stored.
+// The lane's part of the accumulators as in epilogues.hpp.  M (along the rows) is a multiple of 8.
+#pragma once
+#include "epilogues.hpp"
+
+namespace ffn24 {
+
+// Two-factor scaling of an int8 product: the 32-bit sums times the token's and the output channel's scale.  A is the weight, its rows the channels; `sw` is as
+// long as the weight's panel form (whole blocks of 256 rows).
+struct I8Scales { const float* sx; const float* sw; };
+
+// the accumulators as results: their float values, or the integers in them scaled
+template <bool I8, int MI, int NI, class Acc>
+__device__ __forceinline__ void scale_i8(const I8Scales& sc, Acc& acc, int m_lane, int n_lane, int N) {
+  if constexpr (!I8) return;
+  LaneVec<MI> w;
+  w.load(sc.sw, m_lane, 1.f);
+#pragma unroll
+  for (int ni = 0; ni < NI; ni++) {
+    const float sx = sc.sx[min(n_lane + ni, N - 1)];
+#pragma unroll
+    for (int mi = 0; mi < MI; mi++)
+#pragma unroll
+      for (int v = 0; v < 16; v++) acc[mi][ni][v] = (float)__builtin_bit_cast(int, (float)acc[mi][ni][v]) * (sx * w.at(16 * mi + v));
+  }
+}
+
+// out[n][m], m contiguous, through LDS (ColMajorStage)
+template <bool I8>
+struct EdgeColMajor {
+  static constexpr bool STAGED = true;
+  struct Args { __bf16* C; int M, N; I8Scales sc; };
+  template <int MI, int NI, class Acc>
+  static __device__ __forceinline__ void run(const Args& e, Acc& acc, int m_lane, int n_lane, char* wbuf) {
+    using S = ColMajorStage<MI, NI>;
+    using LT = LaneTile<MI, NI>;
+    scale_i8<I8, MI, NI>(e.sc, acc, m_lane, n_lane, e.N);
+#pragma unroll
+    for (int ni = 0; ni < NI; ni++)
+#pragma unroll
+      for (int mi = 0; mi < MI; mi++)
+#pragma unroll
+        for (int q = 0; q < 2; q++) {
+          u32x4 o;
+#pragma unroll
+          for (int d = 0; d < 4; d++) o[d] = pack_bf16x2(acc[mi][ni][8 * q + 2 * d], acc[mi][ni][8 * q + 2 * d + 1]);
+          S::put(wbuf, ni, 2 * mi + q, o);
+        }
+    const int n0 = n_lane - NI * LT::rho(), m0 = m_lane - 16 * MI * LT::h();
+    const int lane = lane_id(), c = lane & (S::PIECES - 1), sub = lane / S::PIECES;
+    constexpr int PER = 64 / S::PIECES;
+    __bf16* out = e.C + (size_t)n0 * e.M + m0 + 8 * c;
+    const int rows = m0 + 8 * c < e.M ? e.N - n0 : 0;
+#pragma unroll
+    for (int j = 0; j < LT::COLS / PER; j++) {
+      const int r = PER * j + sub;
+      if (r < rows) *reinterpret_cast<u32x4*>(out + (size_t)r * e.M) = *reinterpret_cast<const u32x4*>(wbuf + S::at(r, c));
+    }
+  }
+};
+
+// out[m][n], n contiguous, N a multiple of 8
+struct EdgeRowMajor {
+  struct Args { __bf16* C; int M, N; };
+  template <int MI, int NI, class Acc>
+  static __device__ __forceinline__ void run(const Args& e, Acc& acc, int m_lane, int n_lane) {
+    if (n_lane >= e.N) return;
+#pragma unroll
+    for (int mi = 0; mi < MI; mi++)
+#pragma unroll
+      for (int v = 0; v < 16; v++) {
+        float o[NI];
+#pragma unroll
+        for (int ni = 0; ni < NI; ni++) o[ni] = acc[mi][ni][v];
+        const int m = m_lane + 16 * mi + v;
+        if (m < e.M) st_cols<NI>(e.C + (size_t)m * e.N + n_lane, o);
+      }
+  }
+};
+
+// The gate's activation a(x) = x s, s = sigmoid(c1 x + c3 x^3): SiLU with (1, 0), GELU in its tanh form with (2 sqrt(2 / pi), 0.044715 times that).
+// sigmoid(p) = 1 / (1 + 2^(-p log2 e)); 2^x is infinite for p < -88 and s then 0.  In the slope s + x s (1 - s) (c1 + 3 c3 x^2) x is held to +-1e4,
+// where s (1 - s) is 0 long since and the factor stays finite.
+struct Gate { float c1, c3; };
+__device__ __forceinline__ float sigmoid(float p) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * p)); }
+__device__ __forceinline__ float gate_act(const Gate& g, float x) { return x * sigmoid(x * (g.c1 + g.c3 * (x * x))); }
+__device__ __forceinline__ void gate_act_slope(const Gate& g, float x, float& a, float& slope) {
+  const float y = fminf(fmaxf(x, -1e4f), 1e4f), y2 = y * y, s = sigmoid(y * (g.c1 + g.c3 * y2));
+  a = x * s;
+  slope = s + y * (s - s * s) * (g.c1 + 3.f * g.c3 * y2);
+  if (x != x) slope = x;                                      // (the clamp takes NaN for a number)
+}
+
+// Gate and up projections: rows m are features, 8 gate features and the 8 up features of the same numbers in turn, columns n are tokens.
+// H[t][f] = bf16(a(G) U).  GU [T][2 F], if given, receives G and U in bf16 for the backward (training).  ROWMAX: raises rowmax[t] to the
+// bits of max_f |a(G) U| before it is rounded (as unsigned integers they order like the magnitudes, NaN above all).
+template <bool I8, bool ROWMAX>
+struct EpiGateUp {
+  static constexpr bool STAGED = true;
+  struct Args { __bf16* H; __bf16* GU; int F, T; Gate gate; I8Scales sc; uint32_t* rowmax; };
+  template <int MI, int NI, class Acc>
+  static __device__ __forceinline__ void run(const Args& e, Acc& acc, int m_lane, int n_lane, char* wbuf) {
+    using S = ColMajorStage<MI, NI>;
+    using LT = LaneTile<MI, NI>;
+    constexpr int HALF = S::PIECES / 2;                       // pieces of 8 features that the wave has of a token
+    scale_i8<I8, MI, NI>(e.sc, acc, m_lane, n_lane, e.T);
+    const int h = LT::h(), rho = LT::rho();
+    const int t0 = n_lane - NI * rho, f0 = (m_lane - 16 * MI * h) / 2;   // the wave's
+    const int lane = lane_id();
+    if (e.GU) {
+#pragma unroll
+      for (int ni = 0; ni < NI; ni++)
+#pragma unroll
+        for (int mi = 0; mi < MI; mi++)
+#pragma unroll
+          for (int q = 0; q < 2; q++) {
+            u32x4 o;
+#pragma unroll
+            for (int d = 0; d < 4; d++) o[d] = pack_bf16x2(acc[mi][ni][8 * q + 2 * d], acc[mi][ni][8 * q + 2 * d + 1]);
+            *reinterpret_cast<u32x4*>(wbuf + S::at(NI * rho + ni, HALF * q + MI * h + mi)) = o;
+          }
+      const int c = lane & (S::PIECES - 1), sub = lane / S::PIECES, f = f0 + 8 * (c & (HALF - 1));
+      constexpr int PER = 64 / S::PIECES;
+      __bf16* out = e.GU + (size_t)t0 * (2 * (size_t)e.F) + (c >= HALF ? e.F : 0) + f;
+      const int rows = f < e.F ? e.T - t0 : 0;
+#pragma unroll
+      for (int j = 0; j < LT::COLS / PER; j++) {
+        const int r = PER * j + sub;
+        if (r < rows) *reinterpret_cast<u32x4*>(out + (size_t)r * (2 * (size_t)e.F)) = *reinterpret_cast<const u32x4*>(wbuf + S::at(r, c));
+      }
+    }
+    auto at = [](int r, int c) { return (r * HALF + (c ^ ((r / NI) & (HALF - 1)))) << 4; };
+#pragma unroll
+    for (int ni = 0; ni < NI; ni++) {
+      uint32_t top = 0u;
+#pragma unroll
+      for (int mi = 0; mi < MI; mi++) {
+        u32x4 o;
+#pragma unroll
+        for (int d = 0; d < 4; d++) {
+          const float x = gate_act(e.gate, acc[mi][ni][2 * d]) * acc[mi][ni][8 + 2 * d], y = gate_act(e.gate, acc[mi][ni][2 * d + 1]) * acc[mi][ni][9 + 2 * d];
+          if constexpr (ROWMAX) top = max(top, max(__builtin_bit_cast(uint32_t, x) & 0x7FFFFFFFu, __builtin_bit_cast(uint32_t, y) & 0x7FFFFFFFu));
+          o[d] = pack_bf16x2(x, y);
+        }
+        *reinterpret_cast<u32x4*>(wbuf + at(NI * rho + ni, MI * h + mi)) = o;
+      }
+      if constexpr (ROWMAX) {                                 // (features beyond F are zero: the weight's rows there are)
+#pragma unroll
+        for (int s = LT::LANES; s < 64; s <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, s, 64));
+        if (h == 0 && n_lane + ni < e.T) atomicMax(e.rowmax + n_lane + ni, top);
+      }
+    }
+    const int c = lane & (HALF - 1), sub = lane / HALF, f = f0 + 8 * c;
+    constexpr int PER = 64 / HALF;
+    __bf16* out = e.H + (size_t)t0 * e.F + f;
+    const int rows = f < e.F ? e.T - t0 : 0;
+#pragma unroll
+    for (int j = 0; j < LT::COLS / PER; j++) {
+      const int r = PER * j + sub;
+      if (r < rows) *reinterpret_cast<u32x4*>(out + (size_t)r * e.F) = *reinterpret_cast<const u32x4*>(wbuf + at(r, c));
+    }
+  }
+};
+
+// dH and the gate's derivative: rows m are features, columns n tokens, the accumulators dH.  G and U of the forward come by DMA, CH of the lane's tokens at
+// a time, into a wave-private image (row: a token's G features, then its U features, 16-byte pieces at their place XOR the lane column), are replaced
+// there by dG = dH U a'(G) and dU = dH a(G), and leave as whole runs of dGU [T][2 F].
+struct EpiDGate {
+  static constexpr bool STAGED = true;
+  template <int NI> static constexpr int IMAGES = NI == 1 ? 2 : 1;   // (one column a lane: G and U of all of them at once)
+  struct Args { const __bf16* GU; __bf16* dGU; int F, T; Gate gate; };
+  template <int MI, int NI, class Acc>
+  static __device__ __forceinline__ void run(const Args& e, Acc& acc, int m_lane, int n_lane, char* wbuf) {
+    using LT = LaneTile<MI, NI>;
+    constexpr int CH = NI == 8 ? 2 : 1, BUFS = NI == 8 ? 2 : 1, CHUNKS = NI / CH;
+    constexpr int P = LT::ROWS / 8, ROW = 2 * P, ROWS = LT::LANES * CH, BYTES = ROWS * ROW * 16, MOVES = ROWS * ROW / 64;
+    const int lane = lane_id(), h = LT::h(), rho = LT::rho();
+    const int t0 = n_lane - NI * rho, f0 = m_lane - 16 * MI * h;
+    // what place 64 j + lane of the image of tokens ni0 .. holds: token, offset inside its 2 F values, inside the tensor or not
+    auto place = [&](int j, int ni0, int& t, int& f, bool& up) {
+      const int at = 64 * j + lane, r = at / ROW, k = (at % ROW) ^ ((r / CH) & (ROW - 1));
+      t = t0 + NI * (r / CH) + ni0 + r % CH;
+      up = k >= P;
+      f = f0 + 8 * (k & (P - 1));
+    };
+    auto fetch = [&](char* buf, int ni0) {
+#pragma unroll
+      for (int j = 0; j < MOVES; j++) {
+        int t, f;
+        bool up;
+        place(j, ni0, t, f, up);
+        const __bf16* p = e.GU + (size_t)min(t, e.T - 1) * (2 * (size_t)e.F) + (up ? e.F : 0) + min(f, e.F - 8);
+        __builtin_amdgcn_global_load_lds((glb_char*)p, (lds_char*)(buf + j * 1024), 16, 0, 0);
+      }
+    };
+    fetch(wbuf, 0);
+#pragma unroll
+    for (int k = 0; k < CHUNKS; k++) {
+      char* buf = wbuf + (k % BUFS) * BYTES;
+      wait_vmcnt<0>();
+      asm volatile("" ::: "memory");                          // (the compiler does not see the DMA write what is read here)
+      if (BUFS > 1 && k + 1 < CHUNKS) fetch(wbuf + ((k + 1) % BUFS) * BYTES, CH * (k + 1));
+#pragma unroll
+      for (int i = 0; i < CH; i++)
+#pragma unroll
+        for (int mi = 0; mi < MI; mi++)
+#pragma unroll
+          for (int q = 0; q < 2; q++) {
+            const int r = CH * rho + i, c = 2 * MI * h + 2 * mi + q, key = rho & (ROW - 1);
+            u32x4* pg = reinterpret_cast<u32x4*>(buf + ((r * ROW + (c ^ key)) << 4));
+            u32x4* pu = reinterpret_cast<u32x4*>(buf + ((r * ROW + ((P + c) ^ key)) << 4));
+            const u32x4 g = *pg, u = *pu;
+            u32x4 dg, du;
+#pragma unroll
+            for (int d = 0; d < 4; d++) {
+              const float h0 = acc[mi][CH * k + i][8 * q + 2 * d], h1 = acc[mi][CH * k + i][8 * q + 2 * d + 1];
+              float a0, a1, s0, s1;
+              gate_act_slope(e.gate, bf16_lo_to_f32(g[d]), a0, s0);
+              gate_act_slope(e.gate, bf16_hi_to_f32(g[d]), a1, s1);
+              dg[d] = pack_bf16x2(h0 * bf16_lo_to_f32(u[d]) * s0, h1 * bf16_hi_to_f32(u[d]) * s1);
+              du[d] = pack_bf16x2(h0 * a0, h1 * a1);
+            }
+            *pg = dg;
+            *pu = du;
+          }
+#pragma unroll
+      for (int j = 0; j < MOVES; j++) {
+        int t, f;
+        bool up;
+        place(j, CH * k, t, f, up);
+        const u32x4 v = *reinterpret_cast<const u32x4*>(buf + j * 1024 + 16 * lane);
+        if (t < e.T && f < e.F) *reinterpret_cast<u32x4*>(e.dGU + (size_t)t * (2 * (size_t)e.F) + (up ? e.F : 0) + f) = v;
+      }
+      if (BUFS == 1 && k + 1 < CHUNKS) {
+        wait_lgkmcnt0();                                      // the image has been read
+        fetch(wbuf, CH * (k + 1));
+      }
+    }
+  }
+};
+
+}  // namespace ffn24

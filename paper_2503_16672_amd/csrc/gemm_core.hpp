@@ -75,6 +75,10 @@ struct GemmArgs {
   const int* b_rowmap;   // optional: row n of B is taken from memory row b_rowmap[n] (token permutation, gathered by the DMA)
   int b_panel;           // B is in the B panel form (below) instead of row-major; not together with b_rowmap
   unsigned long long* clk;   // optional (profiling): workgroup i < CLK_SLOTS stores its own {shader-clock ticks, 100 MHz ticks} at 2 i
+  // TR_EDGE only: what is really there of the operands; M, N and K above are then rounded up to whole tiles and stages
+  int a_rows, b_rows;    // rows of A, of B (K-contiguous), or k's (k-major)
+  int a_pitch, b_pitch;  // bytes from one of them to the next
+  uint32_t gate;         // TR_GATE: bytes from a gate column of A to the up column of the same feature
 };
 
 // Measurement variants of the GEMM core (bit mask; 0 = the product).  They exist so that what bounds the main loop can be
@@ -194,6 +198,17 @@ __device__ __forceinline__ int swz8_big(int i) { return (i & 2) | (((i >> 3) & 1
 // 16-byte reads then (221 against 256 B/clk in a loop of nothing else; 32 without the swizzle).  Inside the 256 x 256 loops, beside the DMA's writes, the counters
 // see conflicts in 0-1 % of the LDS-active cycles with B k-major, but in a third of them with A k-major (panels: none), T = F = 16384, D 4096.
 constexpr int TR_A = 1, TR_B = 2;
+// Operands of any extent (dense; row-major or k-major, A also in panel form, whose blocks are whole): rows, columns and k's beyond a tensor's end come as
+// zeros.  The buffer descriptor of a stage starts where the stage does and ends with the tensor, so the hardware's bounds check makes them and no offset passes 32
+// bits, however large the tensor: scalar arithmetic, once a stage.  What a k-major row has beyond the tile's columns, and a row-major row beyond K
+// (never read: K is a multiple of the stage there), lands in results that are not stored.
+constexpr int TR_EDGE = 4;
+// 8-bit integers and 32-bit integer sums (in the accumulators' float registers, bit for bit): v_mfma_i32_16x16x64_i8 and 32x32x32_i8 take 16 bytes of k a lane where
+// the bf16 ops take 8 values, so with K counted in pairs of bytes everything else is the bf16 loop.
+constexpr int TR_I8 = 8;
+// A k-major with its two halves [gate | up] side by side: tile rows 16 j .. + 7 are gate features 8 j .. + 7, rows 16 j + 8 .. + 15 the up features of the
+// same numbers, so a lane holds both of a feature.  A piece of 16 bytes is 8 neighbouring features of either half.
+constexpr int TR_GATE = 16;
 template <int MI, int NI> __device__ __forceinline__ int tr_swz_a(int k) {
   if constexpr (MI * NI == 16) return (k & 3) | ((k >> 3) & 1) << 2;
   else if constexpr (MI == 4) return (k & 3) << 1;
@@ -258,8 +273,49 @@ struct Dma {
   uint32_t va[NA], vm[2], vb[NVB];   // per-lane byte offsets from the uniform bases
   uint32_t a_stage, m_stage, b_stage;          // bytes from one stage to the next in the A values / metadata / B stream
   int wave;
+  static constexpr bool EDGE = (TR & TR_EDGE) != 0, GATE = (TR & TR_GATE) != 0;
+  static_assert(!GATE || (EDGE && TRA), "a k-major A of two halves");
+  const char *ea, *eb;           // EDGE: where the block starts in A, in B
+  int64_t na, nb;                // ... and what there is from there on
+
+  // EDGE: the descriptor of stage kt of an operand
+  static __device__ __forceinline__ __amdgpu_buffer_rsrc_t part(const char* p, int64_t bytes, int kt, uint32_t stage) {
+    const int64_t at = (int64_t)kt * stage, left = bytes - at;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p + at), 0, (int)(left < 0 ? 0 : left < 0x7FFFFFFF ? left : 0x7FFFFFFF), 0x00020000);
+  }
+  __device__ __forceinline__ void init_edge(const GemmArgs& g, int m0, int n0, int tid) {
+    const int lane = tid & 63;
+    wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const bool panel = g.a_panel != 0;
+    const int ma = MI == 4 ? 0 : m0 & 255, mb = m0 - ma;
+    const uint32_t a_pitch = panel ? 64u : (uint32_t)g.a_pitch, b_pitch = (uint32_t)g.b_pitch;
+    // the first byte of the block, and one behind the tensor's last
+    const int64_t a0 = TRA ? (int64_t)m0 * (GATE ? 1 : G::ESIZE) : panel ? (int64_t)mb * g.K * G::ESIZE + ma * 64 : (int64_t)m0 * a_pitch;
+    const int64_t b0 = TRB ? (int64_t)n0 * G::ESIZE : (int64_t)n0 * b_pitch;
+    ea = static_cast<const char*>(g.A) + a0;
+    eb = static_cast<const char*>(g.B) + b0;
+    na = !TRA && panel ? (int64_t)0x7FFFFFFF << 16 : (int64_t)g.a_rows * g.a_pitch - a0;
+    nb = (int64_t)g.b_rows * g.b_pitch - b0;
+    a_stage = TRA ? (uint32_t)G::BK * a_pitch : panel ? 256u * (uint32_t)G::A_ROW : (uint32_t)G::A_ROW;
+    b_stage = TRB ? (uint32_t)G::BK * b_pitch : (uint32_t)G::B_ROW;
+#pragma unroll
+    for (int j = 0; j < NA; j++) {
+      if constexpr (TRA) { va[j] = k_major<MI, GATE>(NA * wave + j, lane, a_pitch, [](int k) { return tr_swz_a<MI, NI>(k); }, g.gate); continue; }
+      const int p = G::WIDE ? 8 * (NA * wave + j) + (lane >> 3) : 16 * (NA * wave + j) + (lane >> 2);
+      const int c = G::BIG ? (lane & 3) ^ swz4_big<SPARSE>((p >> 3) & 12) : G::WIDE ? (lane & 7) ^ swz8(p) : (lane & 3) ^ swz4(p);
+      va[j] = (uint32_t)(G::BIG ? p : unperm_m<MI>(p)) * a_pitch + (G::WIDE && panel ? (uint32_t)(c >> 2) * (256u * 64u) + (c & 3) * 16 : (uint32_t)c * 16);
+    }
+#pragma unroll
+    for (int j = 0; j < NVB; j++) {
+      if constexpr (TRB) { vb[j] = k_major<NI>(NVB * wave + j, lane, b_pitch, [](int k) { return tr_swz_b<MI, NI>(k); }); continue; }
+      const int p = G::B_ROW == 128 ? 8 * (NVB * wave + j) + (lane >> 3) : 16 * (NVB * wave + j) + (lane >> 2);
+      const int c = G::B_ROW == 128 ? (lane & 7) ^ (G::BIG ? swz8_big(big_n_col<SPARSE>(p)) : swz8(p)) : (lane & 3) ^ (G::BIG ? swz4_big<false>(big_n_col<SPARSE>(p)) : swz4(p));
+      vb[j] = (uint32_t)(G::BIG ? big_unperm_n<SPARSE>(p) : unperm_n<NI>(p)) * b_pitch + c * 16;
+    }
+  }
 
   __device__ __forceinline__ void init(const GemmArgs& g, int m0, int n0, int tid) {
+    if constexpr (EDGE) { init_edge(g, m0, n0, tid); return; }
     int lane = tid & 63;
     wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t b_row = (uint32_t)g.K * G::ESIZE;                 // bytes per B row in memory
@@ -314,10 +370,11 @@ struct Dma {
 
   // What a lane of instruction j fetches of a k-major operand: 8 / W rows of 128 W bytes of LDS an instruction, the 16-byte pieces of row k at
   // places XORed with the swizzle of k.
-  template <int W, class Swz>
-  static __device__ __forceinline__ uint32_t k_major(int j, int lane, uint32_t krow, Swz swz) {
-    const int k = (8 / W) * j + lane / (8 * W);
-    return (uint32_t)k * krow + (uint32_t)(((lane & (8 * W - 1)) ^ swz(k)) * 16);
+  template <int W, bool HALVES = false, class Swz>
+  static __device__ __forceinline__ uint32_t k_major(int j, int lane, uint32_t krow, Swz swz, uint32_t gate = 0) {
+    const int k = (8 / W) * j + lane / (8 * W), piece = (lane & (8 * W - 1)) ^ swz(k);
+    if constexpr (HALVES) return (uint32_t)k * krow + (uint32_t)(piece >> 1) * 16 + (piece & 1 ? gate : 0u);
+    return (uint32_t)k * krow + (uint32_t)(piece * 16);
   }
 
   // DMA instruction J of stage kt into the stage buffer at `buf` (uniform LDS pointer)
@@ -328,6 +385,11 @@ struct Dma {
     // Buffer loads: descriptor + lane's 32-bit offset + the stage's scalar offset.  A fetch is the setting of M0 and the load, where the form with a
     // 64-bit address took three instructions more (a scalar base, a copy of the offset that the selector would accept); beside a
     // 16 x 16 op (16 cycles) there is room for three in all.
+    if constexpr (EDGE) {
+      if constexpr (J < NA) load<16>(part(ea, na, kt, a_stage), buf + (NA * wave + J) * 1024, va[J], 0);
+      else load<16>(part(eb, nb, kt, b_stage), buf + G::B_OFF + (NVB * wave + J - NA) * 1024, vb[J - NA], 0);
+      return;
+    }
     if constexpr (J < NA) {
       load<16>(a, buf + (NA * wave + J) * 1024, va[J], (uint32_t)kt * a_stage);
     } else if constexpr (J < NA + G::NM) {
@@ -393,15 +455,21 @@ __device__ __forceinline__ void load_frag_dense1(const char* buf, const LaneCtx&
   if constexpr (I < MI) f.a[I] = *reinterpret_cast<const bf16x8*>(buf + L.a_row64 + I * (32 * 64) + c);
   else f.b[I - MI] = *reinterpret_cast<const bf16x8*>(buf + G::B_OFF + L.b_row64 + (I - MI) * (32 * 64) + c);
 }
-template <int M, int MI, int NI>
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x16 __attribute__((ext_vector_type(16)));
+template <int M, int TR = 0, int MI, int NI>
 __device__ __forceinline__ void mfma_dense1(const FragD<MI, NI>& f, f32x16 (&acc)[MI][NI]) {
   constexpr int mi = M / NI, ni = M % NI;
+  if constexpr ((TR & TR_I8) != 0) {
+    acc[mi][ni] = __builtin_bit_cast(f32x16, __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, f.a[mi]), __builtin_bit_cast(i32x4, f.b[ni]),
+                                                                                  __builtin_bit_cast(i32x16, acc[mi][ni]), 0, 0, 0));
+    return;
+  }
   acc[mi][ni] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.a[mi], f.b[ni], acc[mi][ni], 0, 0, 0);
 }
 // fp8 e4m3, v_mfma_f32_32x32x64_f8f6f4: 32 operand bytes per lane, paired byte by byte between A and B (measured:
 // any assignment of the 64 k to (lane half, byte) works if both operands use the same one).  The two 16-byte
 // fragments of a stage (S = 0 and S = 1 above) are exactly one such operand, so a 64-byte-row stage is one K step.
-typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 __device__ __forceinline__ i32x8 cat16(const bf16x8& lo, const bf16x8& hi) {
   i32x4 l = __builtin_bit_cast(i32x4, lo), h = __builtin_bit_cast(i32x4, hi);
@@ -484,7 +552,7 @@ struct StageRegs {                           // dense: chunk pairs q of 32 bytes
   template <int M> __device__ __forceinline__ void op(f32x16 (&acc)[MI][NI]) const {
     constexpr int s = M / (MI * NI), m = M % (MI * NI);
     if constexpr (F8) mfma_dense_f8<m>(f[2 * s], f[2 * s + 1], acc);
-    else mfma_dense1<m>(f[s], acc);
+    else mfma_dense1<m, TR>(f[s], acc);
   }
 };
 template <bool F8, int MI, int NI, int TR>
@@ -552,6 +620,10 @@ __device__ __forceinline__ void tile_coords(int ntm, int ntn, int pid, int& tm, 
 template <class E, class = void> struct epi_is_staged : std::false_type {};
 template <class E> struct epi_is_staged<E, std::void_t<decltype(E::STAGED)>> : std::true_type {};
 
+// ... or that many times this much: `template <int NI> static constexpr int IMAGES`
+template <class E, int NI, class = void> struct epi_wave_images { static constexpr int value = 1; };
+template <class E, int NI> struct epi_wave_images<E, NI, std::void_t<decltype(E::template IMAGES<NI>)>> { static constexpr int value = E::template IMAGES<NI>; };
+
 // Epilogue concept:  struct E { struct Args {...}; template <int MI, int NI, class Acc> static __device__ void run(const Args&, Acc& acc, m_lane, n_lane); }
 //   m_lane = global row of acc[0][*][0] for this lane (its 16 MI rows are m_lane + 16*mi + v),
 //   n_lane = global column of acc[*][0][*] (its NI columns are n_lane + ni).
@@ -561,7 +633,7 @@ template <class G, class Epi, int MI, int NI, class Acc>
 __device__ __forceinline__ void run_epilogue(const typename Epi::Args& ea, Acc& acc, int m_lane, int n_lane, char* smem, int wave) {
   if constexpr (epi_is_staged<Epi>::value) {
     // the epilogue stages its stores through the operand ring: every wave must have read its last fragments first
-    constexpr int WAVE_BYTES = (G::BN / 2) * G::BM;   // the wave's part of the result in bf16
+    constexpr int WAVE_BYTES = (G::BN / 2) * G::BM * epi_wave_images<Epi, NI>::value;   // the wave's part of the result in bf16
     static_assert(G::LDS_TOTAL >= GEMM_THREADS / 64 * WAVE_BYTES, "a staging area per wave");
     __builtin_amdgcn_s_barrier();
     Epi::template run<MI, NI>(ea, acc, m_lane, n_lane, smem + wave * WAVE_BYTES);
@@ -799,7 +871,7 @@ __device__ __forceinline__ void gemm_tile_small(const GemmArgs& g, const typenam
       constexpr int MODE = decltype(mode)::value;
       FFN24_FENCE();
       static_for<NMF>([&](auto M) {
-        mfma_dense1<M>(f0, acc);
+        mfma_dense1<M, TR>(f0, acc);
         ride<NF, FRAG_SLOTS, M>([&](auto I) { load_frag_dense1<G, 1, I, TR>(cur, L, f1); });
         FFN24_FENCE();
       });
@@ -810,7 +882,7 @@ __device__ __forceinline__ void gemm_tile_small(const GemmArgs& g, const typenam
       }
       FFN24_FENCE();
       static_for<NMF>([&](auto M) {
-        mfma_dense1<M>(f1, acc);
+        mfma_dense1<M, TR>(f1, acc);
         if constexpr (MODE == 0) ride<NDMA, NMF, M>([&](auto J) { dma.template issue<J>(kt + NB, cur); });
         if constexpr (MODE != 2) ride<NF, FRAG_SLOTS, M>([&](auto I) { load_frag_dense1<G, 0, I, TR>(nxt, L, f0); });
         FFN24_FENCE();
@@ -870,13 +942,15 @@ struct BigLane { int a, b, m; };   // byte offsets of the lane's first fragment 
 // does wait for; no vector instruction writes one within two instructions of its op, tests/test_kernel_hazards.py), and the end of the
 // main loop waits for the last ops.  Default modifiers of the f8f6f4 op: both operands e4m3, unscaled.
 __device__ __forceinline__ void op16_bf16(const bf16x8& a, const bf16x8& b, f32x4& c) { asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b)); }
+__device__ __forceinline__ void op16_i8(const bf16x8& a, const bf16x8& b, f32x4& c) { asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b)); }
 __device__ __forceinline__ void op16_f8(const i32x8& a, const i32x8& b, f32x4& c) { asm volatile("v_mfma_f32_16x16x128_f8f6f4 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b)); }
 __device__ __forceinline__ void op16_sp_bf16(const bf16x8& a, const i32x8& b, uint32_t idx, f32x4& c) { asm volatile("v_smfmac_f32_16x16x64_bf16 %0, %1, %2, %3" : "+a"(c) : "v"(a), "v"(b), "v"(idx)); }
 __device__ __forceinline__ void op16_sp_f8(const bf16x8& a, const i32x8& b, uint32_t idx, f32x4& c) { asm volatile("v_smfmac_f32_16x16x128_fp8_fp8 %0, %1, %2, %3" : "+a"(c) : "v"(a), "v"(b), "v"(idx)); }
-template <bool SPARSE, bool F8, int H, int M>
+template <bool SPARSE, bool F8, int H, int M, int TR = 0>
 __device__ __forceinline__ void big_op(const BigFrags<SPARSE, F8>& f, f32x4 (&acc)[8][8]) {
   constexpr int mi = M / 4, n = M % 4, ni = 4 * H + n;
-  if constexpr (!SPARSE && !F8) op16_bf16(f.a[mi][0], f.b[H][n][0], acc[mi][ni]);
+  if constexpr ((TR & TR_I8) != 0) op16_i8(f.a[mi][0], f.b[H][n][0], acc[mi][ni]);
+  else if constexpr (!SPARSE && !F8) op16_bf16(f.a[mi][0], f.b[H][n][0], acc[mi][ni]);
   else if constexpr (!SPARSE) op16_f8(cat16(f.a[mi][0], f.a[mi][1]), cat16(f.b[H][n][0], f.b[H][n][1]), acc[mi][ni]);
   else if constexpr (!F8) op16_sp_bf16(f.a[mi][0], cat16(f.b[H][n][0], f.b[H][n][1]), f.idx[mi], acc[mi][ni]);
   else op16_sp_f8(f.a[mi][0], cat16(f.b[H][n][0], f.b[H][n][1]), f.idx[mi], acc[mi][ni]);
@@ -1022,7 +1096,7 @@ __device__ __forceinline__ void gemm_tile_big(const GemmArgs& g, const typename 
     char *cur = ring(slot), *cur2 = ring(slot + 1), *nxt = ring(slot + STEP), *nxt2 = ring(slot + STEP + 1), *prv = ring(slot + NB - 1);
     FFN24_FENCE();
     static_for<32>([&](auto M) {
-      if constexpr (MATH) big_op<SPARSE, F8, 0, M>(f, acc);
+      if constexpr (MATH) big_op<SPARSE, F8, 0, M, TR>(f, acc);
       constexpr int J = paced<PACE, NDMA - PART>(M);
       if constexpr (REST && J >= 0) dma.template issue<PART + (J >= 0 ? J : 0)>(kt - 1 + NB, prv);
       constexpr int I = big_read_slot(M);
@@ -1036,7 +1110,7 @@ __device__ __forceinline__ void gemm_tile_big(const GemmArgs& g, const typename 
     }
     FFN24_FENCE();
     static_for<32>([&](auto M) {
-      if constexpr (MATH) big_op<SPARSE, F8, 1, M>(f, acc);
+      if constexpr (MATH) big_op<SPARSE, F8, 1, M, TR>(f, acc);
       constexpr int J = paced<PACE, H1>(M);
       if constexpr (ISSUE && J >= 0) dma.template issue<(J >= 0 ? J : 0)>(kt + NB, cur);
       if constexpr (FRAG && LEFT >= 0) {
@@ -1117,6 +1191,8 @@ __device__ __forceinline__ void gemm_tile_big(const GemmArgs& g, const typename 
 template <bool SPARSE, class Epi, bool F8 = false, int PROBE = 0, int MI = 4, int NI = 4, int TR = 0>
 __device__ __forceinline__ void gemm_tile(const GemmArgs& g, const typename Epi::Args& ea, char* smem, int pid, int pid_end = 0, int pid_step = 0) {
   static_assert(TR == 0 || (!F8 && !(SPARSE && (TR & TR_A))), "k-major operands: bf16, and a 2:4 operand has its own form");
+  static_assert(!(TR & ~(TR_A | TR_B)) || !SPARSE, "operands of any extent and 8-bit integers: dense");
+  static_assert(!(TR & TR_I8) || !(TR & (TR_A | TR_B)), "8-bit integers: K-contiguous");
   if constexpr (MI * NI == 16) gemm_tile_big<SPARSE, Epi, F8, PROBE, TR>(g, ea, smem, pid, pid_end, pid_step);
   else gemm_tile_small<SPARSE, Epi, F8, MI, NI, TR>(g, ea, smem, pid);
 }

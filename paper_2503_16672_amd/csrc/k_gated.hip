@@ -1,0 +1,91 @@
+// The gated feed-forward block in bf16, many tokens: five GEMMs on the core, forward two, backward three launches.  X, H, dY, dGU are [T][...] row-major; the
+// weights Wgu [D][2 F] (gate | up) and Wd [F][D] are read where they lie.
+//
+//   [G|U] = X Wgu, H = a(G) U      A = Wgu, k-major, gate and up features interleaved by 8 (TR_GATE); B = X
+//   Y = H Wd                       A = Wd, k-major; B = H
+//   dH = dY Wd^T -> dG, dU         A = Wd; B = dY
+//   dX = [dG|dU] Wgu^T             A = Wgu; B = dGU (K = 2 F)
+//   dWd = H^T dY, dWgu = X^T dGU   both operands k-major (K = T), one launch
+#include "launch_block.hpp"
+#include "launch_edge.hpp"
+
+namespace ffn24 {
+namespace {
+
+GemmArgs args(const void* A, int a_rows, int a_cols, const void* B, int b_rows, int b_cols, int M, int N, int K) {
+  GemmArgs g{};
+  g.A = A; g.B = B;
+  g.M = M; g.N = N; g.K = K;
+  g.a_rows = a_rows; g.a_pitch = 2 * a_cols;
+  g.b_rows = b_rows; g.b_pitch = 2 * b_cols;
+  return g;
+}
+
+// dWd and dWgu: workgroups [0, n_first) take the tiles of the first
+template <int MI, int NI>
+__global__ void __launch_bounds__(GEMM_THREADS, (Geo<false, false, MI, NI>::PER_CU)) gated_wgrad_kernel(GemmArgs ga, EdgeRowMajor::Args ea, int n_first, GemmArgs gb,
+                                                                                                        EdgeRowMajor::Args eb) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const bool second = (int)blockIdx.x >= n_first;
+  const GemmArgs g = second ? gb : ga;
+  const EdgeRowMajor::Args e = second ? eb : ea;
+  gemm_tile<false, EdgeRowMajor, false, 0, MI, NI, TR_A | TR_B | TR_EDGE>(g, e, smem, second ? (int)blockIdx.x - n_first : (int)blockIdx.x);
+}
+template <int MI, int NI>
+int launch_wgrad_tile(GemmArgs ga, const EdgeRowMajor::Args& ea, GemmArgs gb, const EdgeRowMajor::Args& eb, hipStream_t s) {
+  using G = Geo<false, false, MI, NI>;
+  auto kern = gated_wgrad_kernel<MI, NI>;
+  static std::atomic<bool> configured[MAX_DEVICES] = {};
+  if (int rc = ensure_dynamic_lds(reinterpret_cast<const void*>(kern), G::LDS_TOTAL, configured)) return rc;
+  ga.M = up_to(ga.M, G::BM); ga.N = up_to(ga.N, G::BN);
+  gb.M = up_to(gb.M, G::BM); gb.N = up_to(gb.N, G::BN);
+  const int na = (ga.M / G::BM) * (ga.N / G::BN), nb = (gb.M / G::BM) * (gb.N / G::BN);
+  hipLaunchKernelGGL(kern, dim3((unsigned)(na + nb)), dim3(GEMM_THREADS), G::LDS_TOTAL, s, ga, ea, na, gb, eb);
+  return (int)hipGetLastError();
+}
+
+__global__ void __launch_bounds__(256) zero_kernel(u32x4* p, size_t n) {
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) p[i] = u32x4{0u, 0u, 0u, 0u};
+}
+}  // namespace
+
+int launch_zero(void* p, size_t bytes, hipStream_t s) {
+  hipLaunchKernelGGL(zero_kernel, dim3(1024), dim3(256), 0, s, static_cast<u32x4*>(p), bytes / 16);
+  return (int)hipGetLastError();
+}
+
+int launch_gated_up(const void* X, const void* Wgu, int T, int D, int F, float c1, float c3, void* H, void* GU, hipStream_t s) {
+  GemmArgs g = args(Wgu, D, 2 * F, X, T, D, 2 * F, T, D);
+  g.gate = 2u * (uint32_t)F;
+  using Epi = EpiGateUp<false, false>;
+  return launch_edge<Epi, TR_A | TR_GATE>(g, Epi::Args{static_cast<__bf16*>(H), static_cast<__bf16*>(GU), F, T, Gate{c1, c3}, I8Scales{}, nullptr}, s);
+}
+
+int launch_gated_down(const void* H, const void* Wd, int T, int D, int F, void* Y, hipStream_t s) {
+  using Epi = EdgeColMajor<false>;
+  return launch_edge<Epi, TR_A>(args(Wd, F, D, H, T, F, D, T, F), Epi::Args{static_cast<__bf16*>(Y), D, T, I8Scales{}}, s);
+}
+
+int launch_gated_dgate(const void* dY, const void* Wd, const void* GU, int T, int D, int F, float c1, float c3, void* dGU, hipStream_t s) {
+  return launch_edge<EpiDGate, 0>(args(Wd, F, D, dY, T, D, F, T, D), EpiDGate::Args{static_cast<const __bf16*>(GU), static_cast<__bf16*>(dGU), F, T, Gate{c1, c3}}, s);
+}
+
+int launch_gated_dx(const void* dGU, const void* Wgu, int T, int D, int F, void* dX, hipStream_t s) {
+  using Epi = EdgeColMajor<false>;
+  return launch_edge<Epi, 0>(args(Wgu, D, 2 * F, dGU, T, 2 * F, D, T, 2 * F), Epi::Args{static_cast<__bf16*>(dX), D, T, I8Scales{}}, s);
+}
+
+int launch_gated_wgrad(const void* X, const void* dY, const void* H, const void* dGU, int T, int D, int F, void* dWgu, void* dWd, hipStream_t s) {
+  const int K = up_to(T, 64);
+  const GemmArgs ga = args(X, T, D, dGU, T, 2 * F, D, 2 * F, K), gb = args(H, T, F, dY, T, D, F, D, K);
+  const EdgeRowMajor::Args ea{static_cast<__bf16*>(dWgu), D, 2 * F}, eb{static_cast<__bf16*>(dWd), F, D};
+  switch (pick_edge_tile(D, 2 * F, K, F, D)) {
+    case 0: return launch_wgrad_tile<4, 4>(ga, ea, gb, eb, s);
+    case 1: return launch_wgrad_tile<4, 2>(ga, ea, gb, eb, s);
+    case 2: return launch_wgrad_tile<2, 2>(ga, ea, gb, eb, s);
+    case 3: return launch_wgrad_tile<2, 1>(ga, ea, gb, eb, s);
+    default: return launch_wgrad_tile<1, 1>(ga, ea, gb, eb, s);
+  }
+}
+
+}  // namespace ffn24

@@ -60,6 +60,19 @@ inline int pick_tile(bool sparse, bool f8, EpiCost epi, int M, int N, int K, int
   return best;
 }
 
+// The same for results that may end inside a tile (dense; 8-bit integers: K in pairs of bytes), and for two of one K that share a launch (M2 x N2; 0: one).
+inline long long edge_tiles(const TileCost& t, int M, int N) { return (long long)((M + 64 * t.mi - 1) / (64 * t.mi)) * ((N + 64 * t.ni - 1) / (64 * t.ni)); }
+inline int pick_edge_tile(int M, int N, int K, int M2 = 0, int N2 = 0) {
+  int best = 0;
+  long long best_time = 0;
+  for (int i = 0; i < NUM_TILES; i++) {
+    const TileCost& t = TILES_DENSE[i];
+    const long long time = (edge_tiles(t, M, N) + edge_tiles(t, M2, N2) + CHIP_CUS - 1) / CHIP_CUS * tile_time(t, K, false);
+    if (i == 0 || time * 100 < best_time * 97) { best = i; best_time = time; }
+  }
+  return best;
+}
+
 // Two launches of n 256 x 256 tiles each (a weight gradient; with the split the dense and the sparse tiles of one) that could be one go out
 // one after the other where sharing saves no round of the chip and the reduction is long: the other's operands then no longer share the
 // L2 with the first's for as long as the launches overlap, and the gap between them is short beside them.  Measured, together -> apart:
