@@ -60,6 +60,33 @@ FFN24_API int gated_fwd(gated_ctx* ctx, const void* X, int64_t T, const void* Wg
  * It may be called more than once for a forward. */
 FFN24_API int gated_bwd(gated_ctx* ctx, const void* dY, const void* X, const void* Wgu, const void* Wd, void* dX, void* dWgu, void* dWd, void* stream);
 
+/* Products of 8-bit integers with a scale for each token and each output channel (serving).  A row x (a token; a channel's weights) becomes
+ *   scale = max |x| * (1 / 127), factor and product rounded to fp32 (1 if all zero);  code = rint(x / scale), in -127 .. 127 (an IEEE division);
+ * and the product of X [T][K] and W [K][N] is Y[t][n] = bf16(sx[t] sw[n] sum_k X8[t][k] W8[k][n]), the sum in 32-bit integers, exact.  A token with an infinite or NaN
+ * value gets such a scale and NaN or infinite results; the others do not see it.  K a multiple of 16, at most 2^17; N a multiple of 8, at most 2^20; T at most 2^20.
+ *
+ * i8_weight quantises W (bf16 [K][N]) and lays it out as the products read it: i8_weight_bytes(K, N) bytes at `out`, to be used with the same K and N.  halves != 0:
+ * W is [Wg | Wu] of a gated block (N a multiple of 16), laid out for gated_i8 (not for matmul_i8). */
+FFN24_API int64_t i8_weight_bytes(int64_t K, int64_t N);   /* or -1 for sizes out of range */
+FFN24_API int i8_weight(const void* W, int64_t K, int64_t N, int halves, void* out, void* stream);
+/* X (bf16 [T][K]) -> codes [T][K], scales fp32 [T] */
+FFN24_API int quantise_i8(const void* X, int64_t T, int64_t K, void* codes, float* scales, void* stream);
+/* Y [T][N] (bf16) from codes and scales of quantise_i8 and weights of i8_weight */
+FFN24_API int matmul_i8(const void* codes, const float* scales, int64_t T, const void* weight, int64_t K, int64_t N, void* Y, void* stream);
+/* The two in one call: Y from bf16 X.  scratch: linear_i8_scratch(T, K) bytes, used until the call's last kernel has run. */
+FFN24_API int64_t linear_i8_scratch(int64_t T, int64_t K);   /* or -1 */
+FFN24_API int linear_i8(const void* X, int64_t T, const void* weight, int64_t K, int64_t N, void* Y, void* scratch, void* stream);
+
+/* The gated block on int8 weights: G, U in fp32 from such products of X and [Wg | Wu];  h = a(G) U;  sh[t] = max_f |h[t][f]| * (1 / 127) (1 if zero);
+ * H8 = rint(bf16(h) / sh), held to -127 .. 127;  Y = bf16(sh[t] sw[d] sum_f H8 Wd8).  T, D, F, gate as for gated_ctx_create, F at most 2^17.
+ * Workspace: T (D + 3 F + 12) bytes and the weights (3 D F and a little).  gated_i8_set_weights quantises Wgu [D][2 F] and Wd [F][D] (bf16) into the context, which
+ * does not need them afterwards; gated_i8_fwd before it returns FFN24_ERR_STATE. */
+typedef struct gated_i8_ctx gated_i8_ctx;
+FFN24_API int gated_i8_ctx_create(gated_i8_ctx** out, int64_t T, int64_t D, int64_t F, ffn24_gate gate);
+FFN24_API int gated_i8_ctx_destroy(gated_i8_ctx* ctx);
+FFN24_API int gated_i8_set_weights(gated_i8_ctx* ctx, const void* Wgu, const void* Wd, void* stream);
+FFN24_API int gated_i8_fwd(gated_i8_ctx* ctx, const void* X, int64_t T, void* Y, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

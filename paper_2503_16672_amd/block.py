@@ -12,7 +12,9 @@ import torch
 from . import ffn24
 from .ffn24 import Ffn24Error, _BF16, _F32, _check, _expect, _ptr, _stream  # noqa: F401
 
-EXPORTS = ("layer_norm_fwd", "layer_norm_bwd_scratch", "layer_norm_bwd", "gated_ctx_create", "gated_ctx_destroy", "gated_fwd", "gated_bwd")
+EXPORTS = ("layer_norm_fwd", "layer_norm_bwd_scratch", "layer_norm_bwd", "gated_ctx_create", "gated_ctx_destroy", "gated_fwd", "gated_bwd",
+           "i8_weight_bytes", "i8_weight", "quantise_i8", "matmul_i8", "linear_i8_scratch", "linear_i8", "gated_i8_ctx_create", "gated_i8_ctx_destroy",
+           "gated_i8_set_weights", "gated_i8_fwd")
 
 _lib = None
 
@@ -30,9 +32,19 @@ def lib() -> ctypes.CDLL:
         L.gated_ctx_destroy.argtypes = [vp]
         L.gated_fwd.argtypes = [vp, vp, i64, vp, vp, vp, vp]
         L.gated_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.i8_weight_bytes.argtypes = [i64, i64]
+        L.i8_weight.argtypes = [vp, i64, i64, ci, vp, vp]
+        L.quantise_i8.argtypes = [vp, i64, i64, vp, vp, vp]
+        L.matmul_i8.argtypes = [vp, vp, i64, vp, i64, i64, vp, vp]
+        L.linear_i8_scratch.argtypes = [i64, i64]
+        L.linear_i8.argtypes = [vp, i64, vp, i64, i64, vp, vp, vp]
+        L.gated_i8_ctx_create.argtypes = [ctypes.POINTER(vp), i64, i64, i64, ci]
+        L.gated_i8_ctx_destroy.argtypes = [vp]
+        L.gated_i8_set_weights.argtypes = [vp, vp, vp, vp]
+        L.gated_i8_fwd.argtypes = [vp, vp, i64, vp, vp]
         for name in EXPORTS:
             getattr(L, name).restype = ci
-        L.layer_norm_bwd_scratch.restype = i64
+        L.layer_norm_bwd_scratch.restype = L.i8_weight_bytes.restype = L.linear_i8_scratch.restype = i64
         _lib = L
     return _lib
 
@@ -143,3 +155,88 @@ class GatedContext(_Handle):
         _expect(dWd, (self.F, self.D), _BF16, "dWd")
         _check(lib().gated_bwd(self._h, _ptr(dY), _ptr(X), _ptr(Wgu), _ptr(Wd), _ptr(dX), _ptr(dWgu), _ptr(dWd), _stream()), "gated_bwd")
         return dX, dWgu, dWd
+
+
+# ---------------------------------------------------------------------------------------------- 8-bit integer products
+_I8 = (torch.int8,)
+
+
+def _size(nbytes: int, what: str) -> int:
+    if nbytes < 0:
+        raise Ffn24Error(-2, what)
+    return nbytes
+
+
+class I8Weight:
+    """W [K, N] (bf16) quantised per output channel and laid out for linear_i8 and matmul_i8 (see i8_weight in the header); W is not needed afterwards."""
+
+    def __init__(self, W):
+        self.K, self.N = W.shape
+        _expect(W, (self.K, self.N), _BF16, "W")
+        self.data = torch.empty(_size(int(lib().i8_weight_bytes(self.K, self.N)), "i8_weight"), dtype=torch.uint8, device=W.device)
+        _check(lib().i8_weight(_ptr(W), self.K, self.N, 0, _ptr(self.data), _stream()), "i8_weight")
+
+
+def quantise_i8(X, codes=None, scales=None):
+    """X [T, K] (bf16) -> (codes [T, K] int8, scales [T] fp32): X = codes * scales to within half a scale."""
+    T, K = X.shape
+    _expect(X, (T, K), _BF16, "X")
+    codes = torch.empty((T, K), dtype=torch.int8, device=X.device) if codes is None else codes
+    scales = torch.empty((T,), dtype=torch.float32, device=X.device) if scales is None else scales
+    _expect(codes, (T, K), _I8, "codes")
+    _expect(scales, (T,), _F32, "scales")
+    _check(lib().quantise_i8(_ptr(X), T, K, _ptr(codes), _ptr(scales), _stream()), "quantise_i8")
+    return codes, scales
+
+
+def matmul_i8(codes, scales, W: I8Weight, Y=None):
+    """Y [T, N] (bf16) from the codes and scales of quantise_i8."""
+    T = codes.shape[0]
+    _expect(codes, (T, W.K), _I8, "codes")
+    _expect(scales, (T,), _F32, "scales")
+    Y = torch.empty((T, W.N), dtype=torch.bfloat16, device=codes.device) if Y is None else Y
+    _expect(Y, (T, W.N), _BF16, "Y")
+    _check(lib().matmul_i8(_ptr(codes), _ptr(scales), T, _ptr(W.data), W.K, W.N, _ptr(Y), _stream()), "matmul_i8")
+    return Y
+
+
+def linear_i8(X, W: I8Weight, Y=None):
+    """Y [T, N] = X W with X [T, K] (bf16) quantised per token on the way."""
+    T = X.shape[0]
+    _expect(X, (T, W.K), _BF16, "X")
+    Y = torch.empty((T, W.N), dtype=torch.bfloat16, device=X.device) if Y is None else Y
+    _expect(Y, (T, W.N), _BF16, "Y")
+    scratch = torch.empty(_size(int(lib().linear_i8_scratch(T, W.K)), "linear_i8"), dtype=torch.uint8, device=X.device)
+    _check(lib().linear_i8(_ptr(X), T, _ptr(W.data), W.K, W.N, _ptr(Y), _ptr(scratch), _stream()), "linear_i8")
+    return Y
+
+
+class GatedI8Context(_Handle):
+    """The gated feed-forward block on int8 weights (see gated_i8_ctx in the header) for up to T tokens; Wgu [D, 2 F] and Wd [F, D] are bf16 and not needed
+    after the constructor's work on the stream."""
+    _destroy = "gated_i8_ctx_destroy"
+
+    def __init__(self, T: int, Wgu, Wd, act: str = "silu"):
+        F, D = Wd.shape
+        self.T, self.D, self.F = T, D, F
+        gate = _gate(act)
+        h = ctypes.c_void_p()
+        _expect(Wgu, (D, 2 * F), _BF16, "Wgu")
+        _expect(Wd, (F, D), _BF16, "Wd")
+        _check(lib().gated_i8_ctx_create(ctypes.byref(h), T, D, F, gate), "gated_i8_ctx_create")
+        self._h = h
+        self.set_weights(Wgu, Wd)
+
+    def set_weights(self, Wgu, Wd):
+        _expect(Wgu, (self.D, 2 * self.F), _BF16, "Wgu")
+        _expect(Wd, (self.F, self.D), _BF16, "Wd")
+        _check(lib().gated_i8_set_weights(self._h, _ptr(Wgu), _ptr(Wd), _stream()), "gated_i8_set_weights")
+
+    def fwd(self, X, Y=None):
+        """X [t, D] with any t up to T -> Y [t, D]."""
+        t = X.shape[0]
+        _expect(X, (t, self.D), _BF16, "X")
+        Y = torch.empty_like(X) if Y is None else Y
+        _expect(Y, (t, self.D), _BF16, "Y")
+        _check(lib().gated_i8_fwd(self._h, _ptr(X), t, _ptr(Y), _stream()), "gated_i8_fwd")
+        return Y

@@ -38,6 +38,22 @@ struct gated_ctx {
   void *H, *GU, *dGU;          // [T][F], and in training [T][2 F] twice
 };
 
+struct gated_i8_ctx {
+  int64_t T, D, F;
+  GateCoefficients gate;
+  int device, have_weights;
+  void *Wgu, *Wd;              // laid out by i8_weight
+  void *X8, *H, *H8;           // [T][D] codes, [T][F] bf16, [T][F] codes
+  float *sx, *sh; uint32_t* tops;
+};
+
+namespace {
+constexpr int64_t MAX_I8_K = 1 << 17, MAX_I8_N = 1 << 20;
+bool i8_sizes(int64_t K, int64_t N) { return K >= 16 && K <= MAX_I8_K && K % 16 == 0 && N >= 8 && N <= MAX_I8_N && N % 8 == 0; }
+bool i8_rows(int64_t T, int64_t K) { return T >= 0 && T <= MAX_CTX_TOKENS && K >= 16 && K <= MAX_I8_K && K % 16 == 0; }
+int64_t up16(int64_t x) { return (x + 15) & ~(int64_t)15; }
+}  // namespace
+
 extern "C" {
 
 int layer_norm_fwd(const void* X, const void* R, const float* weight, const float* bias, int64_t T, int64_t D, float eps, ffn24_norm_dtype dtype, void* S,
@@ -122,6 +138,101 @@ int gated_bwd(gated_ctx* c, const void* dY, const void* X, const void* Wgu, cons
   if (launch_gated_dgate(dY, Wd, c->GU, t, D, F, c->gate.c1, c->gate.c3, c->dGU, s)) return FFN24_ERR_HIP;
   if (launch_gated_dx(c->dGU, Wgu, t, D, F, dX, s)) return FFN24_ERR_HIP;
   return done(launch_gated_wgrad(X, dY, c->H, c->dGU, t, D, F, dWgu, dWd, s));
+}
+
+int64_t i8_weight_bytes(int64_t K, int64_t N) { return i8_sizes(K, N) ? i8_weight_size(K, N) : -1; }
+
+int i8_weight(const void* W, int64_t K, int64_t N, int halves, void* out, void* stream) {
+  if (!i8_sizes(K, N) || (halves && N % 16)) return FFN24_ERR_SHAPE;
+  if (!W || !out) return FFN24_ERR_NULL;
+  if (misaligned(W, out)) return FFN24_ERR_ALIGN;
+  return done(launch_i8_weight(W, (int)K, (int)N, halves != 0, out, static_cast<hipStream_t>(stream)));
+}
+
+int quantise_i8(const void* X, int64_t T, int64_t K, void* codes, float* scales, void* stream) {
+  if (!i8_rows(T, K)) return FFN24_ERR_SHAPE;
+  if (T == 0) return FFN24_OK;
+  if (!X || !codes || !scales) return FFN24_ERR_NULL;
+  if (misaligned(X, codes, scales)) return FFN24_ERR_ALIGN;
+  return done(launch_quantise_i8(X, (int)T, (int)K, codes, scales, nullptr, static_cast<hipStream_t>(stream)));
+}
+
+int matmul_i8(const void* codes, const float* scales, int64_t T, const void* weight, int64_t K, int64_t N, void* Y, void* stream) {
+  if (!i8_rows(T, K) || !i8_sizes(K, N)) return FFN24_ERR_SHAPE;
+  if (T == 0) return FFN24_OK;
+  if (!codes || !scales || !weight || !Y) return FFN24_ERR_NULL;
+  if (misaligned(codes, scales, weight, Y)) return FFN24_ERR_ALIGN;
+  return done(launch_matmul_i8(codes, scales, (int)T, i8_layout(weight, (int)K, (int)N), Y, static_cast<hipStream_t>(stream)));
+}
+
+int64_t linear_i8_scratch(int64_t T, int64_t K) { return i8_rows(T, K) ? T * K + up16(4 * T) : -1; }
+
+int linear_i8(const void* X, int64_t T, const void* weight, int64_t K, int64_t N, void* Y, void* scratch, void* stream) {
+  if (!i8_rows(T, K) || !i8_sizes(K, N)) return FFN24_ERR_SHAPE;
+  if (T == 0) return FFN24_OK;
+  if (!X || !weight || !Y || !scratch) return FFN24_ERR_NULL;
+  if (misaligned(X, weight, Y, scratch)) return FFN24_ERR_ALIGN;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  float* sx = reinterpret_cast<float*>(static_cast<char*>(scratch) + T * K);
+  if (launch_quantise_i8(X, (int)T, (int)K, scratch, sx, nullptr, s)) return FFN24_ERR_HIP;
+  return done(launch_matmul_i8(scratch, sx, (int)T, i8_layout(weight, (int)K, (int)N), Y, s));
+}
+
+int gated_i8_ctx_create(gated_i8_ctx** out, int64_t T, int64_t D, int64_t F, ffn24_gate gate) {
+  if (!out) return FFN24_ERR_NULL;
+  if (int rc = check_sizes(T, D, F, gate)) return rc;
+  if (D > MAX_I8_K || F > MAX_I8_K) return FFN24_ERR_SHAPE;
+  gated_i8_ctx* c = new (std::nothrow) gated_i8_ctx();
+  if (!c) return FFN24_ERR_HIP;
+  c->T = T; c->D = D; c->F = F; c->gate = coefficients(gate);
+  const size_t td = (size_t)T * (size_t)D, tf = (size_t)T * (size_t)F, t4 = 4 * (size_t)T;
+  const bool ok = hipGetDevice(&c->device) == hipSuccess && hipMalloc(&c->Wgu, (size_t)i8_weight_size(D, 2 * F)) == hipSuccess &&
+                  hipMalloc(&c->Wd, (size_t)i8_weight_size(F, D)) == hipSuccess && hipMalloc(&c->X8, td) == hipSuccess && hipMalloc(&c->H, 2 * tf) == hipSuccess &&
+                  hipMalloc(&c->H8, tf) == hipSuccess && hipMalloc(reinterpret_cast<void**>(&c->sx), t4) == hipSuccess &&
+                  hipMalloc(reinterpret_cast<void**>(&c->sh), t4) == hipSuccess && hipMalloc(reinterpret_cast<void**>(&c->tops), t4) == hipSuccess;
+  if (!ok) {
+    (void)hipGetLastError();
+    gated_i8_ctx_destroy(c);
+    return FFN24_ERR_HIP;
+  }
+  *out = c;
+  return FFN24_OK;
+}
+
+int gated_i8_ctx_destroy(gated_i8_ctx* c) {
+  if (!c) return FFN24_OK;
+  int bad = 0;
+  void* bufs[] = {c->Wgu, c->Wd, c->X8, c->H, c->H8, c->sx, c->sh, c->tops};
+  for (void* p : bufs) if (p && hipFree(p) != hipSuccess) bad = 1;
+  delete c;
+  return bad ? FFN24_ERR_HIP : FFN24_OK;
+}
+
+int gated_i8_set_weights(gated_i8_ctx* c, const void* Wgu, const void* Wd, void* stream) {
+  if (!c || !Wgu || !Wd) return FFN24_ERR_NULL;
+  if (misaligned(Wgu, Wd)) return FFN24_ERR_ALIGN;
+  if (int rc = check_device(c->device)) return rc;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  c->have_weights = 0;
+  if (launch_i8_weight(Wgu, (int)c->D, (int)(2 * c->F), true, c->Wgu, s) || launch_i8_weight(Wd, (int)c->F, (int)c->D, false, c->Wd, s)) return FFN24_ERR_HIP;
+  c->have_weights = 1;
+  return FFN24_OK;
+}
+
+int gated_i8_fwd(gated_i8_ctx* c, const void* X, int64_t T, void* Y, void* stream) {
+  if (!c) return FFN24_ERR_NULL;
+  if (T < 0 || T > c->T) return FFN24_ERR_SHAPE;
+  if (!c->have_weights) return FFN24_ERR_STATE;
+  if (T == 0) return FFN24_OK;
+  if (!X || !Y) return FFN24_ERR_NULL;
+  if (misaligned(X, Y)) return FFN24_ERR_ALIGN;
+  if (int rc = check_device(c->device)) return rc;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const int t = (int)T, D = (int)c->D, F = (int)c->F;
+  if (launch_quantise_i8(X, t, D, c->X8, c->sx, c->tops, s)) return FFN24_ERR_HIP;
+  if (launch_gated_up_i8(c->X8, c->sx, t, i8_layout(c->Wgu, D, 2 * F), c->gate.c1, c->gate.c3, c->H, c->tops, s)) return FFN24_ERR_HIP;
+  if (launch_quantise_i8_given(c->H, c->tops, t, F, c->H8, c->sh, s)) return FFN24_ERR_HIP;
+  return done(launch_matmul_i8(c->H8, c->sh, t, i8_layout(c->Wd, F, D), Y, s));
 }
 
 }  // extern "C"

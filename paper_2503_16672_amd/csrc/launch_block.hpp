@@ -22,4 +22,14 @@ int launch_gated_dx(const void* dGU, const void* Wgu, int T, int D, int F, void*
 int launch_gated_wgrad(const void* X, const void* dY, const void* H, const void* dGU, int T, int D, int F, void* dWgu, void* dWd, hipStream_t s);
 int launch_zero(void* p, size_t bytes, hipStream_t s);   // 16-byte aligned, a multiple of 16 bytes
 
+// k_i8.hip: K a multiple of 16, N of 8 (with two halves: of 16); T >= 1
+struct I8Layout { const char* panels; const float* scales; int K, N; };   // weights as i8_weight lays them out
+int64_t i8_weight_size(int64_t K, int64_t N);
+I8Layout i8_layout(const void* p, int K, int N);
+int launch_i8_weight(const void* W, int K, int N, bool halves, void* out, hipStream_t s);
+int launch_quantise_i8(const void* X, int T, int K, void* codes, float* scales, uint32_t* zero, hipStream_t s);
+int launch_quantise_i8_given(const void* H, const uint32_t* tops, int T, int F, void* codes, float* scales, hipStream_t s);
+int launch_matmul_i8(const void* codes, const float* sx, int T, const I8Layout& w, void* Y, hipStream_t s);
+int launch_gated_up_i8(const void* codes, const float* sx, int T, const I8Layout& w, float c1, float c3, void* H, uint32_t* rowmax, hipStream_t s);
+
 }  // namespace ffn24
