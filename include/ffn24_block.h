@@ -45,13 +45,14 @@ typedef enum { FFN24_GATE_SILU = 0, FFN24_GATE_GELU_TANH = 1 } ffn24_gate;
 typedef struct gated_ctx gated_ctx; /* opaque; owns only its device workspace */
 
 /* A context for up to T tokens (1 <= T <= 2^20; every call says how many it has, any number up to T), D and F multiples of 64, at most 2^18.
- * flags: 0 or FFN24_TRAINING (gated_bwd).  Workspace, allocated on the current device: 2 T F bytes; 10 T F with FFN24_TRAINING.  A context belongs to that
+ * flags: 0 or FFN24_TRAINING (gated_bwd).  Workspace, allocated on the current device: 2 T F bytes; 12 T F with FFN24_TRAINING.  A context belongs to that
  * device and to one thread at a time; calls on different streams are the caller's to order.  *out is untouched on error. */
 FFN24_API int gated_ctx_create(gated_ctx** out, int64_t T, int64_t D, int64_t F, ffn24_gate gate, int flags);
 /* The caller must have synchronised every stream that used the context.  NULL is allowed. */
 FFN24_API int gated_ctx_destroy(gated_ctx* ctx);
 
-/* X [T][D] -> Y [T][D], 0 <= T <= the context's.  The weights are read where they lie.  A training context keeps G, U and H in bf16 for gated_bwd. */
+/* X [T][D] -> Y [T][D], 0 <= T <= the context's.  The weights are read where they lie.  A training context keeps H in bf16 and G, U in 24
+ * bits for gated_bwd. */
 FFN24_API int gated_fwd(gated_ctx* ctx, const void* X, int64_t T, const void* Wgu, const void* Wd, void* Y, void* stream);
 
 /* Backward of the context's last gated_fwd (FFN24_ERR_STATE without one, or without FFN24_TRAINING): dY [T][D] with that call's T, and its X, Wgu, Wd again:

@@ -35,7 +35,7 @@ struct gated_ctx {
   GateCoefficients gate;
   int training, device;
   int64_t fwd_T;               // tokens of the last forward, -1: none yet
-  void *H, *GU, *dGU;          // [T][F], and in training [T][2 F] twice
+  void *H, *GU, *GUx, *dGU;    // [T][F] bf16; in training G and U ([T][2 F] bf16 and bytes) and their gradients [T][2 F]
 };
 
 struct gated_i8_ctx {
@@ -91,7 +91,7 @@ int gated_ctx_create(gated_ctx** out, int64_t T, int64_t D, int64_t F, ffn24_gat
   c->training = flags & FFN24_TRAINING; c->fwd_T = -1;
   const size_t tf = (size_t)T * (size_t)F;
   bool ok = hipGetDevice(&c->device) == hipSuccess && hipMalloc(&c->H, 2 * tf) == hipSuccess;
-  if (ok && c->training) ok = hipMalloc(&c->GU, 4 * tf) == hipSuccess && hipMalloc(&c->dGU, 4 * tf) == hipSuccess;
+  if (ok && c->training) ok = hipMalloc(&c->GU, 4 * tf) == hipSuccess && hipMalloc(&c->GUx, 2 * tf) == hipSuccess && hipMalloc(&c->dGU, 4 * tf) == hipSuccess;
   if (!ok) {
     (void)hipGetLastError();
     gated_ctx_destroy(c);
@@ -104,7 +104,7 @@ int gated_ctx_create(gated_ctx** out, int64_t T, int64_t D, int64_t F, ffn24_gat
 int gated_ctx_destroy(gated_ctx* c) {
   if (!c) return FFN24_OK;
   int bad = 0;
-  for (void* p : {c->H, c->GU, c->dGU}) if (p && hipFree(p) != hipSuccess) bad = 1;
+  for (void* p : {c->H, c->GU, c->GUx, c->dGU}) if (p && hipFree(p) != hipSuccess) bad = 1;
   delete c;
   return bad ? FFN24_ERR_HIP : FFN24_OK;
 }
@@ -119,7 +119,7 @@ int gated_fwd(gated_ctx* c, const void* X, int64_t T, const void* Wgu, const voi
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int t = (int)T, D = (int)c->D, F = (int)c->F;
   if (T > 0) {
-    if (launch_gated_up(X, Wgu, t, D, F, c->gate.c1, c->gate.c3, c->H, c->GU, s)) return FFN24_ERR_HIP;
+    if (launch_gated_up(X, Wgu, t, D, F, c->gate.c1, c->gate.c3, c->H, c->GU, c->GUx, s)) return FFN24_ERR_HIP;
     if (launch_gated_down(c->H, Wd, t, D, F, Y, s)) return FFN24_ERR_HIP;
   }
   c->fwd_T = T;
@@ -135,7 +135,7 @@ int gated_bwd(gated_ctx* c, const void* dY, const void* X, const void* Wgu, cons
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int t = (int)c->fwd_T, D = (int)c->D, F = (int)c->F;
   if (t == 0) return done(launch_zero(dWgu, (size_t)4 * D * F, s) || launch_zero(dWd, (size_t)2 * D * F, s));
-  if (launch_gated_dgate(dY, Wd, c->GU, t, D, F, c->gate.c1, c->gate.c3, c->dGU, s)) return FFN24_ERR_HIP;
+  if (launch_gated_dgate(dY, Wd, c->GU, c->GUx, t, D, F, c->gate.c1, c->gate.c3, c->dGU, s)) return FFN24_ERR_HIP;
   if (launch_gated_dx(c->dGU, Wgu, t, D, F, dX, s)) return FFN24_ERR_HIP;
   return done(launch_gated_wgrad(X, dY, c->H, c->dGU, t, D, F, dWgu, dWd, s));
 }

@@ -54,11 +54,11 @@ int launch_zero(void* p, size_t bytes, hipStream_t s) {
   return (int)hipGetLastError();
 }
 
-int launch_gated_up(const void* X, const void* Wgu, int T, int D, int F, float c1, float c3, void* H, void* GU, hipStream_t s) {
+int launch_gated_up(const void* X, const void* Wgu, int T, int D, int F, float c1, float c3, void* H, void* GU, void* GUx, hipStream_t s) {
   GemmArgs g = args(Wgu, D, 2 * F, X, T, D, 2 * F, T, D);
   g.gate = 2u * (uint32_t)F;
   using Epi = EpiGateUp<false, false>;
-  return launch_edge<Epi, TR_A | TR_GATE>(g, Epi::Args{static_cast<__bf16*>(H), static_cast<__bf16*>(GU), F, T, Gate{c1, c3}, I8Scales{}, nullptr}, s);
+  return launch_edge<Epi, TR_A | TR_GATE>(g, Epi::Args{static_cast<__bf16*>(H), static_cast<__bf16*>(GU), static_cast<uint8_t*>(GUx), F, T, Gate{c1, c3}, I8Scales{}, nullptr}, s);
 }
 
 int launch_gated_down(const void* H, const void* Wd, int T, int D, int F, void* Y, hipStream_t s) {
@@ -66,8 +66,8 @@ int launch_gated_down(const void* H, const void* Wd, int T, int D, int F, void* 
   return launch_edge<Epi, TR_A>(args(Wd, F, D, H, T, F, D, T, F), Epi::Args{static_cast<__bf16*>(Y), D, T, I8Scales{}}, s);
 }
 
-int launch_gated_dgate(const void* dY, const void* Wd, const void* GU, int T, int D, int F, float c1, float c3, void* dGU, hipStream_t s) {
-  return launch_edge<EpiDGate, 0>(args(Wd, F, D, dY, T, D, F, T, D), EpiDGate::Args{static_cast<const __bf16*>(GU), static_cast<__bf16*>(dGU), F, T, Gate{c1, c3}}, s);
+int launch_gated_dgate(const void* dY, const void* Wd, const void* GU, const void* GUx, int T, int D, int F, float c1, float c3, void* dGU, hipStream_t s) {
+  return launch_edge<EpiDGate, 0>(args(Wd, F, D, dY, T, D, F, T, D), EpiDGate::Args{static_cast<const __bf16*>(GU), static_cast<const uint8_t*>(GUx), static_cast<__bf16*>(dGU), F, T, Gate{c1, c3}}, s);
 }
 
 int launch_gated_dx(const void* dGU, const void* Wgu, int T, int D, int F, void* dX, hipStream_t s) {

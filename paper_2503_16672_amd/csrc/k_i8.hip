@@ -200,7 +200,7 @@ int launch_matmul_i8(const void* codes, const float* sx, int T, const I8Layout& 
 
 int launch_gated_up_i8(const void* codes, const float* sx, int T, const I8Layout& w, float c1, float c3, void* H, uint32_t* rowmax, hipStream_t s) {
   using Epi = EpiGateUp<true, true>;
-  return launch_edge<Epi, TR_I8>(args(w, codes, T), Epi::Args{static_cast<__bf16*>(H), nullptr, w.N / 2, T, Gate{c1, c3}, I8Scales{sx, w.scales}, rowmax}, s);
+  return launch_edge<Epi, TR_I8>(args(w, codes, T), Epi::Args{static_cast<__bf16*>(H), nullptr, nullptr, w.N / 2, T, Gate{c1, c3}, I8Scales{sx, w.scales}, rowmax}, s);
 }
 
 }  // namespace ffn24
