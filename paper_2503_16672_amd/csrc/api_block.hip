@@ -36,6 +36,8 @@ struct gated_ctx {
   int training, device;
   int64_t fwd_T;               // tokens of the last forward, -1: none yet
   void *H, *GU, *GUx, *dGU;    // [T][F] bf16; in training G and U ([T][2 F] bf16 and bytes) and their gradients [T][2 F]
+  void *Wgu_p;                 // in training: Wgu in panel form, made by a backward that reads it so
+  void *parts;                 // sums over parts of a reduction (few tokens)
 };
 
 struct gated_i8_ctx {
@@ -92,6 +94,8 @@ int gated_ctx_create(gated_ctx** out, int64_t T, int64_t D, int64_t F, ffn24_gat
   const size_t tf = (size_t)T * (size_t)F;
   bool ok = hipGetDevice(&c->device) == hipSuccess && hipMalloc(&c->H, 2 * tf) == hipSuccess;
   if (ok && c->training) ok = hipMalloc(&c->GU, 4 * tf) == hipSuccess && hipMalloc(&c->GUx, 2 * tf) == hipSuccess && hipMalloc(&c->dGU, 4 * tf) == hipSuccess;
+  if (ok && c->training && gated_dx_panels((int)T, (int)D, (int)F)) ok = hipMalloc(&c->Wgu_p, gated_panel_bytes((int)D, (int)(2 * F))) == hipSuccess;
+  if (ok && !c->training) ok = hipMalloc(&c->parts, few_gated_scratch((int)T, (int)D, (int)F)) == hipSuccess;
   if (!ok) {
     (void)hipGetLastError();
     gated_ctx_destroy(c);
@@ -104,7 +108,7 @@ int gated_ctx_create(gated_ctx** out, int64_t T, int64_t D, int64_t F, ffn24_gat
 int gated_ctx_destroy(gated_ctx* c) {
   if (!c) return FFN24_OK;
   int bad = 0;
-  for (void* p : {c->H, c->GU, c->GUx, c->dGU}) if (p && hipFree(p) != hipSuccess) bad = 1;
+  for (void* p : {c->H, c->GU, c->GUx, c->dGU, c->Wgu_p, c->parts}) if (p && hipFree(p) != hipSuccess) bad = 1;
   delete c;
   return bad ? FFN24_ERR_HIP : FFN24_OK;
 }
@@ -118,7 +122,10 @@ int gated_fwd(gated_ctx* c, const void* X, int64_t T, const void* Wgu, const voi
   c->fwd_T = -1;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int t = (int)T, D = (int)c->D, F = (int)c->F;
-  if (T > 0) {
+  if (T > 0 && !c->training && few_tokens(t)) {
+    float* parts = static_cast<float*>(c->parts);
+    if (launch_few_gated_up(X, Wgu, t, D, F, c->gate.c1, c->gate.c3, c->H, parts, s) || launch_few_gated_down(c->H, Wd, t, D, F, Y, parts, s)) return FFN24_ERR_HIP;
+  } else if (T > 0) {
     if (launch_gated_up(X, Wgu, t, D, F, c->gate.c1, c->gate.c3, c->H, c->GU, c->GUx, s)) return FFN24_ERR_HIP;
     if (launch_gated_down(c->H, Wd, t, D, F, Y, s)) return FFN24_ERR_HIP;
   }
@@ -135,8 +142,13 @@ int gated_bwd(gated_ctx* c, const void* dY, const void* X, const void* Wgu, cons
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int t = (int)c->fwd_T, D = (int)c->D, F = (int)c->F;
   if (t == 0) return done(launch_zero(dWgu, (size_t)4 * D * F, s) || launch_zero(dWd, (size_t)2 * D * F, s));
+  const bool panels = c->Wgu_p && gated_dx_panels(t, D, F);
+  if (panels) {
+    if (launch_gated_panels(Wgu, D, F, c->Wgu_p, s)) return FFN24_ERR_HIP;
+    Wgu = c->Wgu_p;
+  }
   if (launch_gated_dgate(dY, Wd, c->GU, c->GUx, t, D, F, c->gate.c1, c->gate.c3, c->dGU, s)) return FFN24_ERR_HIP;
-  if (launch_gated_dx(c->dGU, Wgu, t, D, F, dX, s)) return FFN24_ERR_HIP;
+  if (launch_gated_dx(c->dGU, Wgu, panels, t, D, F, dX, s)) return FFN24_ERR_HIP;
   return done(launch_gated_wgrad(X, dY, c->H, c->dGU, t, D, F, dWgu, dWd, s));
 }
 

@@ -47,7 +47,25 @@ int launch_wgrad_tile(GemmArgs ga, const EdgeRowMajor::Args& ea, GemmArgs gb, co
 __global__ void __launch_bounds__(256) zero_kernel(u32x4* p, size_t n) {
   for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) p[i] = u32x4{0u, 0u, 0u, 0u};
 }
+// A row-major matrix (K a multiple of 32) into the dense A panel form, 16 bytes a work item in the order of the output; rows beyond the last one are not written.
+__global__ void __launch_bounds__(256) gated_panelise_kernel(const u32x4* __restrict__ in, u32x4* __restrict__ out, int rows, int panels) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  const unsigned block = (unsigned)(i >> 10), kp = block % (unsigned)panels, r = block / (unsigned)panels * 256 + ((unsigned)(i >> 2) & 255u);
+  if ((int)r < rows) out[i] = ld_stream(in + ((size_t)r * (unsigned)panels + kp) * 4 + (i & 3));
+}
 }  // namespace
+
+// dX has two K-contiguous operands.  Row by row the 256 x 256 tile reads 64 bytes of a row a stage, half a line; of both operands that is as many L2 requests as
+// there can be, of one of them it is hidden.  So Wgu is copied into panel form first where that tile is taken and the tokens pay for the pass over the
+// weights: T 16384 D 4096 F 16384 4.28 -> 3.22 ms + 0.12 for the pass, T 8192 D 2048 F 8192 591 -> 479 us + 34; on 128 x 64 tiles (T 1000) 40.0 -> 38.5.  dH, whose epilogue
+// moves more than its operands, gains 2.18 -> 2.10 ms for a pass of 0.06 and 401 -> 405 us: it reads Wd row by row.
+bool gated_dx_panels(int T, int D, int F) { return T >= 2048 && pick_edge_tile(D, T, 2 * F) == 0; }
+size_t gated_panel_bytes(int rows, int K) { return 2 * (size_t)up_to(rows, 256) * (size_t)K; }
+int launch_gated_panels(const void* Wgu, int D, int F, void* panels, hipStream_t s) {
+  const size_t items = gated_panel_bytes(D, 2 * F) / 16;
+  hipLaunchKernelGGL(gated_panelise_kernel, dim3((unsigned)(items / 256)), dim3(256), 0, s, static_cast<const u32x4*>(Wgu), static_cast<u32x4*>(panels), D, 2 * F / 32);
+  return (int)hipGetLastError();
+}
 
 int launch_zero(void* p, size_t bytes, hipStream_t s) {
   hipLaunchKernelGGL(zero_kernel, dim3(1024), dim3(256), 0, s, static_cast<u32x4*>(p), bytes / 16);
@@ -70,9 +88,11 @@ int launch_gated_dgate(const void* dY, const void* Wd, const void* GU, const voi
   return launch_edge<EpiDGate, 0>(args(Wd, F, D, dY, T, D, F, T, D), EpiDGate::Args{static_cast<const __bf16*>(GU), static_cast<const uint8_t*>(GUx), static_cast<__bf16*>(dGU), F, T, Gate{c1, c3}}, s);
 }
 
-int launch_gated_dx(const void* dGU, const void* Wgu, int T, int D, int F, void* dX, hipStream_t s) {
+int launch_gated_dx(const void* dGU, const void* Wgu, bool panels, int T, int D, int F, void* dX, hipStream_t s) {
   using Epi = EdgeColMajor<false>;
-  return launch_edge<Epi, 0>(args(Wgu, D, 2 * F, dGU, T, 2 * F, D, T, 2 * F), Epi::Args{static_cast<__bf16*>(dX), D, T, I8Scales{}}, s);
+  GemmArgs g = args(Wgu, D, 2 * F, dGU, T, 2 * F, D, T, 2 * F);
+  g.a_panel = panels;
+  return launch_edge<Epi, 0>(g, Epi::Args{static_cast<__bf16*>(dX), D, T, I8Scales{}}, s);
 }
 
 int launch_gated_wgrad(const void* X, const void* dY, const void* H, const void* dGU, int T, int D, int F, void* dWgu, void* dWd, hipStream_t s) {

@@ -17,8 +17,11 @@ int launch_norm_bwd(const void* dY, const void* S, const float* w, const float* 
 // k_gated.hip: T >= 1, D and F multiples of 64; GU, GUx (EpiGateUp) NULL in a forward without a backward
 int launch_gated_up(const void* X, const void* Wgu, int T, int D, int F, float c1, float c3, void* H, void* GU, void* GUx, hipStream_t s);
 int launch_gated_down(const void* H, const void* Wd, int T, int D, int F, void* Y, hipStream_t s);
+bool gated_dx_panels(int T, int D, int F);   // whether dX reads Wgu in panel form (`panels` below: it is)
+size_t gated_panel_bytes(int rows, int K);
+int launch_gated_panels(const void* Wgu, int D, int F, void* panels, hipStream_t s);
 int launch_gated_dgate(const void* dY, const void* Wd, const void* GU, const void* GUx, int T, int D, int F, float c1, float c3, void* dGU, hipStream_t s);
-int launch_gated_dx(const void* dGU, const void* Wgu, int T, int D, int F, void* dX, hipStream_t s);
+int launch_gated_dx(const void* dGU, const void* Wgu, bool panels, int T, int D, int F, void* dX, hipStream_t s);
 int launch_gated_wgrad(const void* X, const void* dY, const void* H, const void* dGU, int T, int D, int F, void* dWgu, void* dWd, hipStream_t s);
 int launch_zero(void* p, size_t bytes, hipStream_t s);   // 16-byte aligned, a multiple of 16 bytes
 
@@ -31,5 +34,11 @@ int launch_quantise_i8(const void* X, int T, int K, void* codes, float* scales, 
 int launch_quantise_i8_given(const void* H, const uint32_t* tops, int T, int F, void* codes, float* scales, hipStream_t s);
 int launch_matmul_i8(const void* codes, const float* sx, int T, const I8Layout& w, void* Y, hipStream_t s);
 int launch_gated_up_i8(const void* codes, const float* sx, int T, const I8Layout& w, float c1, float c3, void* H, uint32_t* rowmax, hipStream_t s);
+
+// k_few.hip: few tokens, where the weights are what counts
+bool few_tokens(int T);
+size_t few_gated_scratch(int T, int D, int F);   // bytes of `parts` for any token count up to T
+int launch_few_gated_up(const void* X, const void* Wgu, int T, int D, int F, float c1, float c3, void* H, float* parts, hipStream_t s);
+int launch_few_gated_down(const void* H, const void* Wd, int T, int D, int F, void* Y, float* parts, hipStream_t s);
 
 }  // namespace ffn24

@@ -73,6 +73,23 @@ def test_gated_and_its_gradient(T, D, F, act):
     ctx.close()
 
 
+# few tokens on a serving context: strips of 64 and 128 channels, one to 16 parts of a reduction, one to four groups of 16 tokens
+@pytest.mark.gpu
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("D,F", [(64, 64), (192, 448), (1088, 2944), (320, 8192), (2048, 5440), (4096, 1024)])
+@pytest.mark.parametrize("T", [1, 3, 16, 17, 33, 64])
+def test_serving_few_tokens(T, D, F, act):
+    X, Wgu, Wd, dY = _inputs(T, D, F, seed=T + D + F)
+    ctx = block.GatedContext(64, D, F, act=act)
+    Y = ctx.fwd(X, Wgu, Wd)
+    check(Y, reference(X, Wgu, Wd, dY, act)["Y"], "Y")
+    assert torch.equal(ctx.fwd(X, Wgu, Wd), Y)
+    X2 = X.clone()
+    X2[T - 1] = float("nan")                     # the last token leaves the others alone
+    assert torch.equal(ctx.fwd(X2, Wgu, Wd)[:T - 1], Y[:T - 1])
+    ctx.close()
+
+
 @pytest.mark.gpu
 def test_gradient_by_differences():
     """The gradient of sum(Y dY) along a direction of every input, by central differences of the definition."""
