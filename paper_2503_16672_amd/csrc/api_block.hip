@@ -122,7 +122,7 @@ int gated_fwd(gated_ctx* c, const void* X, int64_t T, const void* Wgu, const voi
   c->fwd_T = -1;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int t = (int)T, D = (int)c->D, F = (int)c->F;
-  if (T > 0 && !c->training && few_tokens(t)) {
+  if (T > 0 && !c->training && few_tokens(t, D, F)) {
     float* parts = static_cast<float*>(c->parts);
     if (launch_few_gated_up(X, Wgu, t, D, F, c->gate.c1, c->gate.c3, c->H, parts, s) || launch_few_gated_down(c->H, Wd, t, D, F, Y, parts, s)) return FFN24_ERR_HIP;
   } else if (T > 0) {
@@ -185,6 +185,7 @@ int linear_i8(const void* X, int64_t T, const void* weight, int64_t K, int64_t N
   if (!X || !weight || !Y || !scratch) return FFN24_ERR_NULL;
   if (misaligned(X, weight, Y, scratch)) return FFN24_ERR_ALIGN;
   hipStream_t s = static_cast<hipStream_t>(stream);
+  if (few_i8_fuses((int)T, (int)K)) return done(launch_few_linear_i8(X, (int)T, i8_layout(weight, (int)K, (int)N), Y, s));
   float* sx = reinterpret_cast<float*>(static_cast<char*>(scratch) + T * K);
   if (launch_quantise_i8(X, (int)T, (int)K, scratch, sx, nullptr, s)) return FFN24_ERR_HIP;
   return done(launch_matmul_i8(scratch, sx, (int)T, i8_layout(weight, (int)K, (int)N), Y, s));
@@ -197,11 +198,11 @@ int gated_i8_ctx_create(gated_i8_ctx** out, int64_t T, int64_t D, int64_t F, ffn
   gated_i8_ctx* c = new (std::nothrow) gated_i8_ctx();
   if (!c) return FFN24_ERR_HIP;
   c->T = T; c->D = D; c->F = F; c->gate = coefficients(gate);
-  const size_t td = (size_t)T * (size_t)D, tf = (size_t)T * (size_t)F, t4 = 4 * (size_t)T;
+  const size_t td = (size_t)T * (size_t)D, tf = (size_t)T * (size_t)F, t4 = 4 * (size_t)T, few = few_i8_tops((int)T, (int)F), tops = few > t4 ? few : t4;
   const bool ok = hipGetDevice(&c->device) == hipSuccess && hipMalloc(&c->Wgu, (size_t)i8_weight_size(D, 2 * F)) == hipSuccess &&
                   hipMalloc(&c->Wd, (size_t)i8_weight_size(F, D)) == hipSuccess && hipMalloc(&c->X8, td) == hipSuccess && hipMalloc(&c->H, 2 * tf) == hipSuccess &&
                   hipMalloc(&c->H8, tf) == hipSuccess && hipMalloc(reinterpret_cast<void**>(&c->sx), t4) == hipSuccess &&
-                  hipMalloc(reinterpret_cast<void**>(&c->sh), t4) == hipSuccess && hipMalloc(reinterpret_cast<void**>(&c->tops), t4) == hipSuccess;
+                  hipMalloc(reinterpret_cast<void**>(&c->sh), t4) == hipSuccess && hipMalloc(reinterpret_cast<void**>(&c->tops), tops) == hipSuccess;
   if (!ok) {
     (void)hipGetLastError();
     gated_i8_ctx_destroy(c);
@@ -241,6 +242,8 @@ int gated_i8_fwd(gated_i8_ctx* c, const void* X, int64_t T, void* Y, void* strea
   if (int rc = check_device(c->device)) return rc;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int t = (int)T, D = (int)c->D, F = (int)c->F;
+  if (few_gated_i8_tokens(t, D, F))
+    return done(launch_few_gated_i8(X, t, i8_layout(c->Wgu, D, 2 * F), i8_layout(c->Wd, F, D), c->gate.c1, c->gate.c3, c->X8, c->sx, c->H, c->tops, c->H8, c->sh, Y, s));
   if (launch_quantise_i8(X, t, D, c->X8, c->sx, c->tops, s)) return FFN24_ERR_HIP;
   if (launch_gated_up_i8(c->X8, c->sx, t, i8_layout(c->Wgu, D, 2 * F), c->gate.c1, c->gate.c3, c->H, c->tops, s)) return FFN24_ERR_HIP;
   if (launch_quantise_i8_given(c->H, c->tops, t, F, c->H8, c->sh, s)) return FFN24_ERR_HIP;

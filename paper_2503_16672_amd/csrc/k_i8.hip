@@ -7,26 +7,10 @@
 // zeros, then the scales of the panel's rows, then the words the largest magnitudes are found in.
 #include "launch_block.hpp"
 #include "launch_edge.hpp"
+#include "i8_codes.hpp"
 
 namespace ffn24 {
 namespace {
-
-__device__ __forceinline__ float i8_scale(uint32_t top) { return top ? __builtin_bit_cast(float, top) * (1.f / 127.f) : 1.f; }
-__device__ __forceinline__ uint32_t i8_code(float x, float s) { return (uint32_t)(int)fminf(fmaxf(rintf(x / s), -127.f), 127.f) & 0xFFu; }
-__device__ __forceinline__ uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7FFFFFFFu; }
-__device__ __forceinline__ uint32_t top8(const u32x4& w, uint32_t top) {
-#pragma unroll
-  for (int i = 0; i < 4; i++) top = max(top, max(w[i] << 16 & 0x7FFF0000u, w[i] & 0x7FFF0000u));
-  return top;
-}
-__device__ __forceinline__ u32x2 codes8(const u32x4& w, float s) {
-  u32x2 o;
-#pragma unroll
-  for (int i = 0; i < 2; i++)
-    o[i] = i8_code(bf16_lo_to_f32(w[2 * i]), s) | i8_code(bf16_hi_to_f32(w[2 * i]), s) << 8 | i8_code(bf16_lo_to_f32(w[2 * i + 1]), s) << 16 |
-           i8_code(bf16_hi_to_f32(w[2 * i + 1]), s) << 24;
-  return o;
-}
 
 // Rows of K values (a multiple of 8) to codes, W waves a row, P pieces of 8 values a lane in registers; P = 0: any K, the row read twice (the second time from
 // the caches).  zero: a word a row to be cleared, for what a later kernel collects there.
@@ -47,9 +31,9 @@ __global__ void __launch_bounds__(256) quantise_i8_kernel(const uint16_t* __rest
       w[p] = i < K ? *reinterpret_cast<const u32x4*>(x + i) : u32x4{0u, 0u, 0u, 0u};
     }
 #pragma unroll
-    for (int p = 0; p < P; p++) top = top8(w[p], top);
+    for (int p = 0; p < P; p++) top = i8_top8(w[p], top);
   } else {
-    for (int i = 8 * l; i < K; i += 8 * LANES) top = top8(*reinterpret_cast<const u32x4*>(x + i), top);
+    for (int i = 8 * l; i < K; i += 8 * LANES) top = i8_top8(*reinterpret_cast<const u32x4*>(x + i), top);
   }
 #pragma unroll
   for (int s = 1; s < 64; s <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, s, 64));
@@ -69,10 +53,10 @@ __global__ void __launch_bounds__(256) quantise_i8_kernel(const uint16_t* __rest
 #pragma unroll
     for (int p = 0; p < P; p++) {
       const int i = 8 * (p * LANES + l);
-      if (i < K) *reinterpret_cast<u32x2*>(o + i) = codes8(w[p], s);
+      if (i < K) *reinterpret_cast<u32x2*>(o + i) = i8_codes8(w[p], s);
     }
   } else {
-    for (int i = 8 * l; i < K; i += 8 * LANES) *reinterpret_cast<u32x2*>(o + i) = codes8(*reinterpret_cast<const u32x4*>(x + i), s);
+    for (int i = 8 * l; i < K; i += 8 * LANES) *reinterpret_cast<u32x2*>(o + i) = i8_codes8(*reinterpret_cast<const u32x4*>(x + i), s);
   }
 }
 
@@ -85,7 +69,7 @@ __global__ void __launch_bounds__(256) quantise_i8_given_kernel(const uint16_t* 
   if (i == 0) scales[row] = s;
   if (i >= per) return;
   const u32x4* p = reinterpret_cast<const u32x4*>(H + (size_t)row * F + 16 * i);
-  const u32x2 a = codes8(p[0], s), b = codes8(p[1], s);
+  const u32x2 a = i8_codes8(p[0], s), b = i8_codes8(p[1], s);
   *reinterpret_cast<u32x4*>(codes + (size_t)row * F + 16 * i) = u32x4{a[0], a[1], b[0], b[1]};
 }
 
@@ -194,6 +178,7 @@ int launch_quantise_i8_given(const void* H, const uint32_t* tops, int T, int F, 
 }
 
 int launch_matmul_i8(const void* codes, const float* sx, int T, const I8Layout& w, void* Y, hipStream_t s) {
+  if (few_i8_tokens(T, w.K)) return launch_few_matmul_i8(codes, sx, T, w, Y, s);
   using Epi = EdgeColMajor<true>;
   return launch_edge<Epi, TR_I8>(args(w, codes, T), Epi::Args{static_cast<__bf16*>(Y), w.N, T, I8Scales{sx, w.scales}}, s);
 }

@@ -47,7 +47,8 @@ def test_codes_and_scales(T, K):
 # the GEMM core's five tiles, token counts from one, channels and reductions that end inside a tile and a stage
 @pytest.mark.gpu
 @pytest.mark.parametrize("T,K,N", [(1, 16, 8), (1, 2048, 520), (3, 80, 24), (17, 144, 264), (64, 1088, 1000), (65, 208, 256), (333, 1088, 4168), (1000, 640, 3000),
-                                   (1500, 512, 2048), (2100, 1552, 5000), (4099, 272, 4104), (2, 16400, 16)])
+                                   (1500, 512, 2048), (2100, 1552, 5000), (4099, 272, 4104), (2, 16400, 16),
+                                   (16, 1040, 40), (1, 17000, 264), (29, 8208, 200), (32, 8192, 16392), (5, 4112, 32768)])
 def test_product(T, K, N):
     X, W = _normal((T, K), T), _normal((K, N), N, K ** -0.5)
     W[:, N - 1] = 0
@@ -95,7 +96,7 @@ def _act(x, act):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("act", ["silu", "gelu"])
-@pytest.mark.parametrize("T,D,F", [(1, 64, 64), (2, 128, 192), (16, 576, 1344), (33, 192, 448), (64, 512, 2048), (65, 256, 512), (700, 320, 704), (1609, 640, 640), (2500, 512, 2816)])
+@pytest.mark.parametrize("T,D,F", [(1, 64, 64), (2, 128, 192), (16, 576, 1344), (33, 192, 448), (64, 512, 2048), (65, 256, 512), (24, 2048, 4160), (4, 3968, 16384), (700, 320, 704), (1609, 640, 640), (2500, 512, 2816)])
 def test_gated_block(T, D, F, act):
     X, Wgu, Wd = _normal((T, D), 1).cuda(), _normal((D, 2 * F), 2, D ** -0.5).cuda(), _normal((F, D), 3, F ** -0.5).cuda()
     ctx = block.GatedI8Context(T + 5, Wgu, Wd, act=act)
