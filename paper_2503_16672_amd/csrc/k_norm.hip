@@ -4,68 +4,102 @@
 //   backward  xh = (s - mean) rstd, p = dy w:  dx = rstd (p - sum p / D - xh sum (p xh) / D) + ds;  dw = sum_t dy xh;  db = sum_t dy
 //
 // A row lives in the registers of the waves that share it, so the variance is of centred values without a second read.  Lane l of the W waves of
-// a row holds P pieces of 8 elements.  V = 8: a piece is 8 neighbouring elements, 16-byte accesses (D a multiple of 8); V = 1: elements 64 W apart, any D.
+// a row holds P pieces of 8 neighbouring elements.  EVEN: D is a multiple of 8, rows are 16-byte aligned; otherwise a row starts at any element and its last piece
+// is a part of one: 16-byte accesses at the alignment of an element, which global memory takes; the part is read as the row's last 8 elements and moved into place,
+// and stored element by element.
 #include "launch_block.hpp"
 #include "stream_core.hpp"
 
 namespace ffn24 {
 namespace {
 
+template <class T, int ALIGN> struct Unaligned { T v; } __attribute__((packed, aligned(ALIGN)));
+// 16 bytes at the alignment of an E, or (EVEN) at their own, with the streaming hint (HINT) or without
+template <class T, class E, bool EVEN, bool HINT>
+__device__ __forceinline__ T ld16(const void* p) {
+  if constexpr (EVEN) return HINT ? ld_stream(static_cast<const T*>(p)) : *static_cast<const T*>(p);
+  else return static_cast<const Unaligned<T, sizeof(E)>*>(p)->v;
+}
+template <class E, bool EVEN, class T>
+__device__ __forceinline__ void st16(void* p, T x) {
+  if constexpr (EVEN) st_keep(static_cast<T*>(p), x);
+  else static_cast<Unaligned<T, sizeof(E)>*>(p)->v = x;
+}
+
 template <class E> struct Elem;
 template <> struct Elem<uint16_t> {                          // bf16
   static __device__ __forceinline__ float up(uint16_t x) { return __builtin_bit_cast(float, (uint32_t)x << 16); }
   static __device__ __forceinline__ uint16_t down(float x) { return (uint16_t)pack_bf16x2(x, 0.f); }
   static __device__ __forceinline__ float round(float x) { return up(down(x)); }
-  static __device__ __forceinline__ void ld8(const uint16_t* p, float (&v)[8]) {
-    const u32x4 w = ld_stream(reinterpret_cast<const u32x4*>(p));
+  typedef u32x4 Raw;                                         // 8 elements as they lie in memory
+  template <bool EVEN, bool HINT> static __device__ __forceinline__ Raw ld8(const uint16_t* p) { return ld16<u32x4, uint16_t, EVEN, HINT>(p); }
+  static __device__ __forceinline__ void put(Raw& w, int j, uint16_t x) { w[j / 2] |= (uint32_t)x << (16 * (j % 2)); }
+  static __device__ __forceinline__ void up8(const Raw& w, float (&v)[8]) {
 #pragma unroll
     for (int i = 0; i < 4; i++) { v[2 * i] = bf16_lo_to_f32(w[i]); v[2 * i + 1] = bf16_hi_to_f32(w[i]); }
   }
-  static __device__ __forceinline__ void st8(uint16_t* p, const float (&v)[8]) {
-    st_keep(reinterpret_cast<u32x4*>(p), u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])});
+  template <bool EVEN> static __device__ __forceinline__ void st8(uint16_t* p, const float (&v)[8]) {
+    st16<uint16_t, EVEN>(p, u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])});
   }
 };
 template <> struct Elem<float> {
   static __device__ __forceinline__ float up(float x) { return x; }
   static __device__ __forceinline__ float down(float x) { return x; }
   static __device__ __forceinline__ float round(float x) { return x; }
-  static __device__ __forceinline__ void ld8(const float* p, float (&v)[8]) {
-    const f32x4 a = ld_stream(reinterpret_cast<const f32x4*>(p)), b = ld_stream(reinterpret_cast<const f32x4*>(p) + 1);
+  struct Raw { f32x4 a, b; };
+  template <bool EVEN, bool HINT> static __device__ __forceinline__ Raw ld8(const float* p) { return Raw{ld16<f32x4, float, EVEN, HINT>(p), ld16<f32x4, float, EVEN, HINT>(p + 4)}; }
+  static __device__ __forceinline__ void put(Raw& w, int j, float x) { if (j < 4) w.a[j] = x; else w.b[j - 4] = x; }
+  static __device__ __forceinline__ void up8(const Raw& w, float (&v)[8]) {
 #pragma unroll
-    for (int i = 0; i < 4; i++) { v[i] = a[i]; v[4 + i] = b[i]; }
+    for (int i = 0; i < 4; i++) { v[i] = w.a[i]; v[4 + i] = w.b[i]; }
   }
-  static __device__ __forceinline__ void st8(float* p, const float (&v)[8]) {
-    st_keep(reinterpret_cast<f32x4*>(p), f32x4{v[0], v[1], v[2], v[3]});
-    st_keep(reinterpret_cast<f32x4*>(p) + 1, f32x4{v[4], v[5], v[6], v[7]});
+  template <bool EVEN> static __device__ __forceinline__ void st8(float* p, const float (&v)[8]) {
+    st16<float, EVEN>(p, f32x4{v[0], v[1], v[2], v[3]});
+    st16<float, EVEN>(p + 4, f32x4{v[4], v[5], v[6], v[7]});
   }
 };
 
 // A row among the lanes of W waves; l: the lane's number among them.
-template <int V, int W>
+template <bool EVEN, int W>
 struct RowMap {
   static constexpr int LANES = 64 * W;
-  // element j of piece p, and whether a piece (V = 8) or an element (V = 1) is inside the row
-  static __device__ __forceinline__ int at(int p, int j, int l) { return V == 8 ? 8 * (p * LANES + l) + j : (8 * p + j) * LANES + l; }
-  template <class E>
-  static __device__ __forceinline__ void load(const E* row, int p, int l, int D, float (&v)[8]) {
-    if constexpr (V == 8) {
-      if (at(p, 0, l) < D) Elem<E>::ld8(row + at(p, 0, l), v);
-      else {
+  static __device__ __forceinline__ int at(int p, int l) { return 8 * (p * LANES + l); }   // the first element of piece p
+  // a piece as it lies in memory, on its way; zeros outside the row
+  template <bool HINT = false, class E>
+  static __device__ __forceinline__ void fetch(typename Elem<E>::Raw& x, const E* row, int p, int l, int D) {
+    const int i = at(p, l);
+    x = typename Elem<E>::Raw{};
+    if (i >= D) return;
+    if (EVEN || D >= 8) x = Elem<E>::template ld8<EVEN, HINT>(row + (EVEN ? i : min(i, D - 8)));
+    else {
 #pragma unroll
-        for (int j = 0; j < 8; j++) v[j] = 0.f;
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; j++) v[j] = at(p, j, l) < D ? Elem<E>::up(row[at(p, j, l)]) : 0.f;
+      for (int j = 0; j < 7; j++) if (i + j < D) Elem<E>::put(x, j, row[i + j]);
     }
   }
   template <class E>
-  static __device__ __forceinline__ void store(E* row, int p, int l, int D, const float (&v)[8]) {
-    if constexpr (V == 8) {
-      if (at(p, 0, l) < D) Elem<E>::st8(row + at(p, 0, l), v);
-    } else {
+  static __device__ __forceinline__ void unpack(const typename Elem<E>::Raw& x, int p, int l, int D, float (&v)[8]) {
+    Elem<E>::up8(x, v);
+    const int over = at(p, l) + 8 - D;
+    if (!EVEN && over > 0 && D >= 8) {                       // (only the wave that has the row's end comes here)
 #pragma unroll
-      for (int j = 0; j < 8; j++) if (at(p, j, l) < D) row[at(p, j, l)] = Elem<E>::down(v[j]);
+      for (int by = 4; by >= 1; by /= 2)
+#pragma unroll
+        for (int j = 0; j < 8; j++) v[j] = over & by ? (j + by < 8 ? v[j + by] : 0.f) : v[j];
+    }
+  }
+  template <class E>
+  static __device__ __forceinline__ void load(const E* row, int p, int l, int D, float (&v)[8]) {
+    typename Elem<E>::Raw x;
+    fetch(x, row, p, l, D);
+    unpack<E>(x, p, l, D, v);
+  }
+  template <class E>
+  static __device__ __forceinline__ void store(E* row, int p, int l, int D, const float (&v)[8]) {
+    const int i = at(p, l);
+    if (EVEN ? i < D : i + 8 <= D) Elem<E>::template st8<EVEN>(row + i, v);
+    else if (!EVEN && i < D) {
+#pragma unroll
+      for (int j = 0; j < 7; j++) if (i + j < D) row[i + j] = Elem<E>::down(v[j]);
     }
   }
 };
@@ -88,89 +122,134 @@ __device__ __forceinline__ float row_sum(float x, float* part, int wave) {
   return s;
 }
 
-constexpr int NORM_THREADS = 256;
-
-template <class E, int V, int P, int W>
-__global__ void __launch_bounds__(NORM_THREADS) norm_fwd_kernel(const E* X, const E* R, const float* weight, const float* bias, int T, int D, float eps, E* S,
-                                                                E* Y, float* mean_out, float* rstd_out) {
-  using M = RowMap<V, W>;
-  __shared__ float part[2][4];
-  const int wave = threadIdx.x >> 6, l = threadIdx.x & (M::LANES - 1), w0 = wave & ~(W - 1);
-  const int row = blockIdx.x * (4 / W) + wave / W;
-  if (W == 1 && row >= T) return;                            // (W = 4: the grid has T workgroups)
-  const size_t o = (size_t)row * D;
-  float v[P][8], sum = 0.f;
+// Rows blockIdx.x R + r, + gridDim.x R, ...; R rows a workgroup at a time, the next ones on their way while these are worked on.
+template <class E, bool EVEN, bool HINT, int P, int W, int R>
+__global__ void __launch_bounds__(64 * W * R) norm_fwd_kernel(const E* X, const E* res, const float* weight, const float* bias, int T, int D, float eps, E* S, E* Y,
+                                                              float* mean_out, float* rstd_out) {
+  using M = RowMap<EVEN, W>;
+  constexpr bool HOLD = P <= 2;                              // weights and bias stay in registers
+  __shared__ float part[2][W * R];
+  const int wave = threadIdx.x >> 6, r = wave / W, l = threadIdx.x & (M::LANES - 1), w0 = r * W;
+  float w[P][8], b[P][8];
+  auto weights = [&](int p) {
+    M::load(weight, p, l, D, w[p]);
+    if (bias) M::load(bias, p, l, D, b[p]);
+    else {
 #pragma unroll
-  for (int p = 0; p < P; p++) M::load(X + o, p, l, D, v[p]);
-  if (R) {
+      for (int j = 0; j < 8; j++) b[p][j] = 0.f;
+    }
+  };
+  typename Elem<E>::Raw sx[P], sr[P];
+  auto ask = [&](int row) {
+    const size_t o = (size_t)min(row, T - 1) * D;
 #pragma unroll
     for (int p = 0; p < P; p++) {
-      float r[8];
-      M::load(R + o, p, l, D, r);
-#pragma unroll
-      for (int j = 0; j < 8; j++) v[p][j] = Elem<E>::round(v[p][j] + r[j]);
-      M::store(S + o, p, l, D, v[p]);
+      M::template fetch<HINT>(sx[p], X + o, p, l, D);
+      if (res) M::template fetch<HINT>(sr[p], res + o, p, l, D);
     }
-  }
-#pragma unroll
-  for (int p = 0; p < P; p++)
-#pragma unroll
-    for (int j = 0; j < 8; j++) sum += v[p][j];
-  const float mean = row_sum<W>(sum, part[0] + w0, wave - w0) / (float)D;
-  float sq = 0.f;
-#pragma unroll
-  for (int p = 0; p < P; p++)
-#pragma unroll
-    for (int j = 0; j < 8; j++) {
-      v[p][j] = M::at(p, j, l) < D ? v[p][j] - mean : 0.f;
-      sq += v[p][j] * v[p][j];
-    }
-  const float rstd = 1.f / sqrtf(row_sum<W>(sq, part[1] + w0, wave - w0) / (float)D + eps);
-  if (l == 0 && mean_out) { mean_out[row] = mean; rstd_out[row] = rstd; }
-#pragma unroll
-  for (int p = 0; p < P; p++) {
-    float w[8], b[8] = {};
-    M::load(weight, p, l, D, w);
-    if (bias) M::load(bias, p, l, D, b);
-#pragma unroll
-    for (int j = 0; j < 8; j++) v[p][j] = v[p][j] * rstd * w[j] + b[j];
-    M::store(Y + o, p, l, D, v[p]);
-  }
-}
-
-// A workgroup of R rows at a time walks rows blockIdx.x R + r, + gridDim.x R, ...; every lane adds up its columns' dy xh and dy, and at the end the workgroup's sums
-// go to `parts` [gridDim.x][2][D].
-template <class E, int V, int P, int W, int R>
-__global__ void __launch_bounds__(64 * W * R) norm_bwd_kernel(const E* dY, const E* S, const float* weight, const float* mean, const float* rstd, const E* dS, int T,
-                                                              int D, E* dX, float* parts) {
-  using M = RowMap<V, W>;
-  __shared__ float part[2][2][W * R];                        // [parity of the step][which sum]
-  const int wave = threadIdx.x >> 6, r = wave / W, l = threadIdx.x & (M::LANES - 1), w0 = r * W;
-  constexpr bool HOLD = W < 16;                              // (a workgroup of 16 waves has 128 registers a lane: the weights are read again for every row)
-  float w[P][8], dw[P][8], db[P][8];
-#pragma unroll
-  for (int p = 0; p < P; p++) {
-    if (HOLD) M::load(weight, p, l, D, w[p]);
-#pragma unroll
-    for (int j = 0; j < 8; j++) dw[p][j] = db[p][j] = 0.f;
-  }
-  const float inv = 1.f / (float)D;
+  };
   const int step = gridDim.x * R;
-  int parity = 0;
-  for (int row0 = blockIdx.x * R; row0 < T; row0 += step, parity ^= 1) {   // (uniform: the barriers below are met by all)
+  ask(blockIdx.x * R + r);
+  if constexpr (HOLD) {
+#pragma unroll
+    for (int p = 0; p < P; p++) weights(p);
+  }
+  for (int row0 = blockIdx.x * R; row0 < T; row0 += step) {  // (uniform: the barriers below are met by all)
     const int row = row0 + r;
     const bool here = row < T;
-    const size_t o = (size_t)(here ? row : T - 1) * D;
-    float x[P][8], g[P][8], s1 = 0.f, s2 = 0.f;
-    const float mu = mean[here ? row : T - 1], rs = rstd[here ? row : T - 1];
+    const size_t o = (size_t)row * D;
+    float v[P][8], sum = 0.f;
 #pragma unroll
-    for (int p = 0; p < P; p++) { M::load(S + o, p, l, D, x[p]); M::load(dY + o, p, l, D, g[p]); }
+    for (int p = 0; p < P; p++) M::template unpack<E>(sx[p], p, l, D, v[p]);
+    if (res) {
+#pragma unroll
+      for (int p = 0; p < P; p++) {
+        float x[8];
+        M::template unpack<E>(sr[p], p, l, D, x);
+#pragma unroll
+        for (int j = 0; j < 8; j++) v[p][j] = Elem<E>::round(v[p][j] + x[j]);
+      }
+    }
+    if (row0 + step < T) ask(row + step);
+#pragma unroll
+    for (int p = 0; p < P; p++) {
+      if (res && here) M::store(S + o, p, l, D, v[p]);
+#pragma unroll
+      for (int j = 0; j < 8; j++) sum += v[p][j];
+    }
+    const float mean = row_sum<W>(sum, part[0] + w0, wave - w0) / (float)D;
+    float sq = 0.f;
 #pragma unroll
     for (int p = 0; p < P; p++)
 #pragma unroll
       for (int j = 0; j < 8; j++) {
-        if (!HOLD && j == 0) M::load(weight, p, l, D, w[p]);
-        x[p][j] = (x[p][j] - mu) * rs;                       // (outside the row the weight and dY are 0: nothing is added)
+        v[p][j] = M::at(p, l) + (EVEN ? 0 : j) < D ? v[p][j] - mean : 0.f;
+        sq += v[p][j] * v[p][j];
+      }
+    const float rstd = 1.f / sqrtf(row_sum<W>(sq, part[1] + w0, wave - w0) / (float)D + eps);
+    if (l == 0 && here && mean_out) { mean_out[row] = mean; rstd_out[row] = rstd; }
+#pragma unroll
+    for (int p = 0; p < P; p++) {
+      if constexpr (!HOLD) weights(p);
+#pragma unroll
+      for (int j = 0; j < 8; j++) v[p][j] = v[p][j] * rstd * w[p][j] + b[p][j];
+      if (here) M::store(Y + o, p, l, D, v[p]);
+    }
+  }
+}
+
+constexpr int NORM_FWD_WAVES = 16;                           // a CU
+
+// A workgroup of R rows at a time walks rows blockIdx.x R + r, + gridDim.x R, ...; every lane adds up its columns' dy xh and dy, and at the end the workgroup's sums
+// go to `parts` [gridDim.x][2][D].
+template <class E, bool EVEN, bool HINT, int P, int W, int R>
+__global__ void __launch_bounds__(64 * W * R) norm_bwd_kernel(const E* dY, const E* S, const float* weight, const float* mean, const float* rstd, const E* dS, int T,
+                                                              int D, E* dX, float* parts) {
+  using M = RowMap<EVEN, W>;
+  __shared__ float part[2][2][W * R];                        // [parity of the step][which sum]
+  const int wave = threadIdx.x >> 6, r = wave / W, l = threadIdx.x & (M::LANES - 1), w0 = r * W;
+  constexpr bool ROOM = W < 16;                              // (a workgroup of 16 waves has 128 registers a lane: no weights and no next row in them)
+  float w[P][8], dw[P][8], db[P][8];
+#pragma unroll
+  for (int p = 0; p < P; p++) {
+    if (ROOM) M::load(weight, p, l, D, w[p]);
+#pragma unroll
+    for (int j = 0; j < 8; j++) dw[p][j] = db[p][j] = 0.f;
+  }
+  const float inv = 1.f / (float)D;
+  const int step = gridDim.x * R, row_first = blockIdx.x * R + r;
+  // The next row is on its way while this one is worked on: a workgroup has a barrier a row, and without it every row waited out a round trip to memory.
+  typename Elem<E>::Raw sx[P], sg[P], sd[P];
+  float mu, rs;
+  auto ask = [&](int row, bool tokens) {
+    const size_t o = (size_t)min(row, T - 1) * D;
+#pragma unroll
+    for (int p = 0; p < P; p++) {
+      if (tokens) { M::template fetch<HINT>(sx[p], S + o, p, l, D); M::template fetch<HINT>(sg[p], dY + o, p, l, D); }
+      else if (dS) M::template fetch<HINT>(sd[p], dS + o, p, l, D);
+    }
+    if (tokens) { mu = mean[min(row, T - 1)]; rs = rstd[min(row, T - 1)]; }
+  };
+  if (ROOM) {
+    ask(row_first, true);
+    ask(row_first, false);
+  }
+  int parity = 0;
+  for (int row0 = blockIdx.x * R; row0 < T; row0 += step, parity ^= 1) {   // (uniform: the barriers below are met by all)
+    const int row = row0 + r;
+    const bool here = row < T;
+    float x[P][8], g[P][8], s1 = 0.f, s2 = 0.f;
+    if (!ROOM) ask(row, true);
+    const float scale = rs, center = mu;
+#pragma unroll
+    for (int p = 0; p < P; p++) { M::template unpack<E>(sx[p], p, l, D, x[p]); M::template unpack<E>(sg[p], p, l, D, g[p]); }
+    if (ROOM && row0 + step < T) ask(row + step, true);
+#pragma unroll
+    for (int p = 0; p < P; p++)
+#pragma unroll
+      for (int j = 0; j < 8; j++) {
+        if (!ROOM && j == 0) M::load(weight, p, l, D, w[p]);
+        x[p][j] = (x[p][j] - center) * scale;                // (outside the row the weight and dY are 0: nothing is added)
         if (here) { dw[p][j] += g[p][j] * x[p][j]; db[p][j] += g[p][j]; }
         g[p][j] *= w[p][j];
         s1 += g[p][j];
@@ -185,16 +264,16 @@ __global__ void __launch_bounds__(64 * W * R) norm_bwd_kernel(const E* dY, const
       for (int i = 0; i < W; i++) { s1 += part[parity][0][w0 + i]; s2 += part[parity][1][w0 + i]; }
     }
     s1 *= inv; s2 *= inv;
-    if (here) {
+    if (!ROOM) ask(row, false);
 #pragma unroll
-      for (int p = 0; p < P; p++) {
-        float d[8] = {};
-        if (dS) M::load(dS + o, p, l, D, d);
+    for (int p = 0; p < P; p++) {
+      float d[8] = {};
+      if (dS) M::template unpack<E>(sd[p], p, l, D, d);
 #pragma unroll
-        for (int j = 0; j < 8; j++) d[j] += rs * (g[p][j] - s1 - x[p][j] * s2);
-        M::store(dX + o, p, l, D, d);
-      }
+      for (int j = 0; j < 8; j++) d[j] += scale * (g[p][j] - s1 - x[p][j] * s2);
+      if (here) M::store(dX + (size_t)row * D, p, l, D, d);
     }
+    if (ROOM && row0 + step < T) ask(row + step, false);
   }
   // the workgroup's R rows of sums, one after the other
   float* mine = parts + (size_t)blockIdx.x * 2 * D;
@@ -225,84 +304,100 @@ __global__ void __launch_bounds__(64 * W * R) norm_bwd_kernel(const E* dY, const
   }
 }
 
-// Column c of the n partial sums [n][2 D]: 16 groups of rows a workgroup, 64 columns each; dweight, then dbias.
-__global__ void __launch_bounds__(1024) norm_sum_kernel(const float* parts, int n, int D, float* dweight, float* dbias) {
-  __shared__ float sums[16][64];
-  const int c = blockIdx.x * 64 + (threadIdx.x & 63), g = threadIdx.x >> 6;
+// Column c of the n partial sums [n][2 D]: 32 groups of rows a workgroup, 32 columns each; dweight, then dbias.
+__global__ void __launch_bounds__(1024) norm_sum_kernel(const float* __restrict__ parts, int n, int D, float* dweight, float* dbias) {
+  __shared__ float sums[32][33];
+  const int x = threadIdx.x & 31, c = blockIdx.x * 32 + x, g = threadIdx.x >> 5;
   float s = 0.f;
-  if (c < 2 * D)
-    for (int i = g; i < n; i += 16) s += parts[(size_t)i * 2 * D + c];
-  sums[g][threadIdx.x & 63] = s;
+  if (c < 2 * D) {
+    const float* p = parts + c;
+    const size_t row = 2 * (size_t)D;
+    int i = g;
+    for (; i + 96 < n; i += 128) {                           // four rows on their way at a time
+      const float a = p[i * row], b = p[(i + 32) * row], d = p[(i + 64) * row], e = p[(i + 96) * row];
+      s += (a + b) + (d + e);
+    }
+    for (; i < n; i += 32) s += p[i * row];
+  }
+  sums[g][x] = s;
   __syncthreads();
   if (g == 0 && c < 2 * D) {
 #pragma unroll
-    for (int i = 1; i < 16; i++) s += sums[i][threadIdx.x];
+    for (int i = 1; i < 32; i++) s += sums[i][x];
     if (c < D) dweight[c] = s;
     else if (dbias) dbias[c - D] = s;
   }
 }
 
-template <class E, int V, int P, int W>
-void fwd(const void* X, const void* R, const float* w, const float* b, int T, int D, float eps, void* S, void* Y, float* mean, float* rstd, hipStream_t s) {
-  hipLaunchKernelGGL((norm_fwd_kernel<E, V, P, W>), dim3((unsigned)((T + 4 / W - 1) / (4 / W))), dim3(NORM_THREADS), 0, s, static_cast<const E*>(X),
-                     static_cast<const E*>(R), w, b, T, D, eps, static_cast<E*>(S), static_cast<E*>(Y), mean, rstd);
+// The streaming hint from tensors of 128 MiB on, four of which the caches do not hold (T x D, bf16, with / without, us: forward 16384 x 4096 87, 101; 4096 x 8192 46.6, 43.5; 16384 x 1024
+// 26.7, 23.4; backward 100, 112; 64, 61.5; 37, 35.7; 2000 x 16384 forward 82, 54).
+template <class E> bool hint(int T, int D) { return sizeof(E) * (size_t)T * (size_t)D >= (size_t)1 << 27; }
+
+// Workgroups: 16 waves a CU, each with rows to walk (T x D, bf16, 12 / 16 / 32 / 64 waves: 16384 x 4096 88.8, 87.0, 90.4, 94.0 us; 4096 x 8192 51, 46.7, 49.6, 61.2; a row a workgroup and
+// no prefetch 114).
+template <class E, bool EVEN, int P, int W, int R>
+void fwd(const void* X, const void* res, const float* w, const float* b, int T, int D, float eps, void* S, void* Y, float* mean, float* rstd, hipStream_t s) {
+  constexpr int most = 256 * NORM_FWD_WAVES / (W * R);
+  const int n = (T + R - 1) / R;
+  const auto kern = EVEN && hint<E>(T, D) ? norm_fwd_kernel<E, EVEN, EVEN, P, W, R> : norm_fwd_kernel<E, EVEN, false, P, W, R>;
+  hipLaunchKernelGGL(kern, dim3((unsigned)(n < most ? n : most)), dim3(64 * W * R), 0, s, static_cast<const E*>(X),
+                     static_cast<const E*>(res), w, b, T, D, eps, static_cast<E*>(S), static_cast<E*>(Y), mean, rstd);
 }
-template <class E, int V>
-void fwd_any(const void* X, const void* R, const float* w, const float* b, int T, int D, float eps, void* S, void* Y, float* mean, float* rstd, hipStream_t s) {
-  if (D <= 4096 && T >= 1024) {
-    if (D <= 512) return fwd<E, V, 1, 1>(X, R, w, b, T, D, eps, S, Y, mean, rstd, s);
-    if (D <= 1024) return fwd<E, V, 2, 1>(X, R, w, b, T, D, eps, S, Y, mean, rstd, s);
-    if (D <= 2048) return fwd<E, V, 4, 1>(X, R, w, b, T, D, eps, S, Y, mean, rstd, s);
-    return fwd<E, V, 8, 1>(X, R, w, b, T, D, eps, S, Y, mean, rstd, s);
-  }
-  if (D <= 2048) return fwd<E, V, 1, 4>(X, R, w, b, T, D, eps, S, Y, mean, rstd, s);
-  if (D <= 4096) return fwd<E, V, 2, 4>(X, R, w, b, T, D, eps, S, Y, mean, rstd, s);
-  if (D <= 8192) return fwd<E, V, 4, 4>(X, R, w, b, T, D, eps, S, Y, mean, rstd, s);
-  return fwd<E, V, 8, 4>(X, R, w, b, T, D, eps, S, Y, mean, rstd, s);
+template <class E, bool EVEN>
+void fwd_any(const void* X, const void* res, const float* w, const float* b, int T, int D, float eps, void* S, void* Y, float* mean, float* rstd, hipStream_t s) {
+  if (D <= 512) return fwd<E, EVEN, 1, 1, 4>(X, res, w, b, T, D, eps, S, Y, mean, rstd, s);
+  if (D <= 1024) return fwd<E, EVEN, 2, 1, 4>(X, res, w, b, T, D, eps, S, Y, mean, rstd, s);
+  if (D <= 2048) return fwd<E, EVEN, 1, 4, 1>(X, res, w, b, T, D, eps, S, Y, mean, rstd, s);
+  if (D <= 4096) return fwd<E, EVEN, 2, 4, 1>(X, res, w, b, T, D, eps, S, Y, mean, rstd, s);
+  if (D <= 8192) return fwd<E, EVEN, 2, 8, 1>(X, res, w, b, T, D, eps, S, Y, mean, rstd, s);
+  return fwd<E, EVEN, 4, 8, 1>(X, res, w, b, T, D, eps, S, Y, mean, rstd, s);
 }
 
-template <class E, int V, int P, int W, int R>
+template <class E, bool EVEN, int P, int W, int R>
 void bwd(const void* dY, const void* S, const float* w, const float* mean, const float* rstd, const void* dS, int T, int D, void* dX, float* parts, int n, hipStream_t s) {
-  hipLaunchKernelGGL((norm_bwd_kernel<E, V, P, W, R>), dim3((unsigned)n), dim3(64 * W * R), 0, s, static_cast<const E*>(dY), static_cast<const E*>(S), w, mean, rstd,
+  const auto kern = EVEN && hint<E>(T, D) ? norm_bwd_kernel<E, EVEN, EVEN, P, W, R> : norm_bwd_kernel<E, EVEN, false, P, W, R>;
+  hipLaunchKernelGGL(kern, dim3((unsigned)n), dim3(64 * W * R), 0, s, static_cast<const E*>(dY), static_cast<const E*>(S), w, mean, rstd,
                      static_cast<const E*>(dS), T, D, static_cast<E*>(dX), parts);
 }
 // waves a row (and pieces a lane), rows a workgroup takes at a time: at most two pieces a lane, whose columns' weights and sums stay in registers
 // beside the row; with four, 220-256 registers and two waves a SIMD
 int bwd_rows(int D) { return D <= 1024 ? 4 : 1; }
-template <class E, int V>
+template <class E, bool EVEN>
 void bwd_any(const void* dY, const void* S, const float* w, const float* mean, const float* rstd, const void* dS, int T, int D, void* dX, float* parts, int n, hipStream_t s) {
-  if (D <= 512) return bwd<E, V, 1, 1, 4>(dY, S, w, mean, rstd, dS, T, D, dX, parts, n, s);
-  if (D <= 1024) return bwd<E, V, 2, 1, 4>(dY, S, w, mean, rstd, dS, T, D, dX, parts, n, s);
-  if (D <= 2048) return bwd<E, V, 1, 4, 1>(dY, S, w, mean, rstd, dS, T, D, dX, parts, n, s);
-  if (D <= 4096) return bwd<E, V, 2, 4, 1>(dY, S, w, mean, rstd, dS, T, D, dX, parts, n, s);
-  if (D <= 8192) return bwd<E, V, 2, 8, 1>(dY, S, w, mean, rstd, dS, T, D, dX, parts, n, s);
-  return bwd<E, V, 2, 16, 1>(dY, S, w, mean, rstd, dS, T, D, dX, parts, n, s);
+  if (D <= 512) return bwd<E, EVEN, 1, 1, 4>(dY, S, w, mean, rstd, dS, T, D, dX, parts, n, s);
+  if (D <= 1024) return bwd<E, EVEN, 2, 1, 4>(dY, S, w, mean, rstd, dS, T, D, dX, parts, n, s);
+  if (D <= 2048) return bwd<E, EVEN, 1, 4, 1>(dY, S, w, mean, rstd, dS, T, D, dX, parts, n, s);
+  if (D <= 4096) return bwd<E, EVEN, 2, 4, 1>(dY, S, w, mean, rstd, dS, T, D, dX, parts, n, s);
+  if (D <= 8192) return bwd<E, EVEN, 2, 8, 1>(dY, S, w, mean, rstd, dS, T, D, dX, parts, n, s);
+  return bwd<E, EVEN, 2, 16, 1>(dY, S, w, mean, rstd, dS, T, D, dX, parts, n, s);
 }
 }  // namespace
 
 int launch_norm_fwd(const void* X, const void* R, const float* w, const float* b, int T, int D, float eps, bool f32, void* S, void* Y, float* mean, float* rstd,
                     hipStream_t s) {
-  if (D % 8 == 0) f32 ? fwd_any<float, 8>(X, R, w, b, T, D, eps, S, Y, mean, rstd, s) : fwd_any<uint16_t, 8>(X, R, w, b, T, D, eps, S, Y, mean, rstd, s);
-  else f32 ? fwd_any<float, 1>(X, R, w, b, T, D, eps, S, Y, mean, rstd, s) : fwd_any<uint16_t, 1>(X, R, w, b, T, D, eps, S, Y, mean, rstd, s);
+  if (D % 8 == 0) f32 ? fwd_any<float, true>(X, R, w, b, T, D, eps, S, Y, mean, rstd, s) : fwd_any<uint16_t, true>(X, R, w, b, T, D, eps, S, Y, mean, rstd, s);
+  else f32 ? fwd_any<float, false>(X, R, w, b, T, D, eps, S, Y, mean, rstd, s) : fwd_any<uint16_t, false>(X, R, w, b, T, D, eps, S, Y, mean, rstd, s);
   return (int)hipGetLastError();
 }
 
-// workgroups of the backward, each with its partial sums
+// Workgroups of the backward, each with its partial sums: the chip's CUs, twice from 1025 to 4096 columns, where a workgroup is four waves (T x D, bf16, 256 / 512 / 1024: 16384 x 4096
+// 119, 100, 113 us; 8192 x 2048 50, 40, 46; 4096 x 8192 53, 64, 85; 16384 x 1024 36, 37, 51; 2000 x 16384 86, 100, 217).
 int norm_bwd_parts(int64_t T, int D) {
   const int R = bwd_rows(D);
   const int64_t n = (T + R - 1) / R;
-  return (int)(n < 512 ? n : 512);
+  const int most = D > 1024 && D <= 4096 ? 512 : 256;
+  return (int)(n < most ? n : most);
 }
 
 int launch_norm_bwd(const void* dY, const void* S, const float* w, const float* mean, const float* rstd, const void* dS, int T, int D, bool f32, void* dX,
                     float* dweight, float* dbias, float* parts, hipStream_t s) {
   const int n = norm_bwd_parts(T, D);
   if (n > 0) {
-    if (D % 8 == 0) f32 ? bwd_any<float, 8>(dY, S, w, mean, rstd, dS, T, D, dX, parts, n, s) : bwd_any<uint16_t, 8>(dY, S, w, mean, rstd, dS, T, D, dX, parts, n, s);
-    else f32 ? bwd_any<float, 1>(dY, S, w, mean, rstd, dS, T, D, dX, parts, n, s) : bwd_any<uint16_t, 1>(dY, S, w, mean, rstd, dS, T, D, dX, parts, n, s);
+    if (D % 8 == 0) f32 ? bwd_any<float, true>(dY, S, w, mean, rstd, dS, T, D, dX, parts, n, s) : bwd_any<uint16_t, true>(dY, S, w, mean, rstd, dS, T, D, dX, parts, n, s);
+    else f32 ? bwd_any<float, false>(dY, S, w, mean, rstd, dS, T, D, dX, parts, n, s) : bwd_any<uint16_t, false>(dY, S, w, mean, rstd, dS, T, D, dX, parts, n, s);
     if (int rc = (int)hipGetLastError()) return rc;
   }
-  hipLaunchKernelGGL(norm_sum_kernel, dim3((unsigned)((2 * D + 63) / 64)), dim3(1024), 0, s, parts, n, D, dweight, dbias);
+  hipLaunchKernelGGL(norm_sum_kernel, dim3((unsigned)((2 * D + 31) / 32)), dim3(1024), 0, s, parts, n, D, dweight, dbias);
   return (int)hipGetLastError();
 }
 
