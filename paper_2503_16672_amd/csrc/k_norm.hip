@@ -127,7 +127,7 @@ template <class E, bool EVEN, bool HINT, int P, int W, int R>
 __global__ void __launch_bounds__(64 * W * R) norm_fwd_kernel(const E* X, const E* res, const float* weight, const float* bias, int T, int D, float eps, E* S, E* Y,
                                                               float* mean_out, float* rstd_out) {
   using M = RowMap<EVEN, W>;
-  constexpr bool HOLD = P <= 2;                              // weights and bias stay in registers
+  constexpr bool HOLD = W < 16;                              // weights and bias stay in registers (a workgroup of 16 waves has 128 of them a lane)
   __shared__ float part[2][W * R];
   const int wave = threadIdx.x >> 6, r = wave / W, l = threadIdx.x & (M::LANES - 1), w0 = r * W;
   float w[P][8], b[P][8];
@@ -350,7 +350,7 @@ void fwd_any(const void* X, const void* res, const float* w, const float* b, int
   if (D <= 2048) return fwd<E, EVEN, 1, 4, 1>(X, res, w, b, T, D, eps, S, Y, mean, rstd, s);
   if (D <= 4096) return fwd<E, EVEN, 2, 4, 1>(X, res, w, b, T, D, eps, S, Y, mean, rstd, s);
   if (D <= 8192) return fwd<E, EVEN, 2, 8, 1>(X, res, w, b, T, D, eps, S, Y, mean, rstd, s);
-  return fwd<E, EVEN, 4, 8, 1>(X, res, w, b, T, D, eps, S, Y, mean, rstd, s);
+  return fwd<E, EVEN, 2, 16, 1>(X, res, w, b, T, D, eps, S, Y, mean, rstd, s);
 }
 
 template <class E, bool EVEN, int P, int W, int R>
