@@ -148,8 +148,7 @@ int gated_bwd(gated_ctx* c, const void* dY, const void* X, const void* Wgu, cons
     Wgu = c->Wgu_p;
   }
   if (launch_gated_dgate(dY, Wd, c->GU, c->GUx, t, D, F, c->gate.c1, c->gate.c3, c->dGU, s)) return FFN24_ERR_HIP;
-  if (launch_gated_dx(c->dGU, Wgu, panels, t, D, F, dX, s)) return FFN24_ERR_HIP;
-  return done(launch_gated_wgrad(X, dY, c->H, c->dGU, t, D, F, dWgu, dWd, s));
+  return done(launch_gated_grads(X, dY, c->H, c->dGU, Wgu, panels, t, D, F, dX, dWgu, dWd, s));
 }
 
 int64_t i8_weight_bytes(int64_t K, int64_t N) { return i8_sizes(K, N) ? i8_weight_size(K, N) : -1; }

@@ -44,6 +44,34 @@ int launch_wgrad_tile(GemmArgs ga, const EdgeRowMajor::Args& ea, GemmArgs gb, co
   return (int)hipGetLastError();
 }
 
+// dX and both weight gradients, which do not need one another, in one launch: the long reductions of dX (K = 2 F) first, the others fill what they leave of the chip.
+template <int MI, int NI>
+__global__ void __launch_bounds__(GEMM_THREADS, (Geo<false, false, MI, NI>::PER_CU)) gated_grads_kernel(GemmArgs gx, EdgeColMajor<false>::Args ex, int n_x, GemmArgs ga,
+                                                                                                        EdgeRowMajor::Args ea, int n_first, GemmArgs gb, EdgeRowMajor::Args eb) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int id = (int)blockIdx.x - n_x;
+  if (id < 0) { gemm_tile<false, EdgeColMajor<false>, false, 0, MI, NI, TR_EDGE>(gx, ex, smem, (int)blockIdx.x); return; }
+  const bool second = id >= n_first;
+  const GemmArgs g = second ? gb : ga;
+  const EdgeRowMajor::Args e = second ? eb : ea;
+  gemm_tile<false, EdgeRowMajor, false, 0, MI, NI, TR_A | TR_B | TR_EDGE>(g, e, smem, second ? id - n_first : id);
+}
+template <int MI, int NI>
+int launch_grads_tile(GemmArgs gx, const EdgeColMajor<false>::Args& ex, GemmArgs ga, const EdgeRowMajor::Args& ea, GemmArgs gb, const EdgeRowMajor::Args& eb, hipStream_t s) {
+  using G = Geo<false, false, MI, NI>;
+  auto kern = gated_grads_kernel<MI, NI>;
+  static std::atomic<bool> configured[MAX_DEVICES] = {};
+  if (int rc = ensure_dynamic_lds(reinterpret_cast<const void*>(kern), G::LDS_TOTAL, configured)) return rc;
+  int n[3], i = 0;
+  for (GemmArgs* g : {&gx, &ga, &gb}) {
+    g->M = up_to(g->M, G::BM);
+    g->N = up_to(g->N, G::BN);
+    n[i++] = (g->M / G::BM) * (g->N / G::BN);
+  }
+  hipLaunchKernelGGL(kern, dim3((unsigned)(n[0] + n[1] + n[2])), dim3(GEMM_THREADS), G::LDS_TOTAL, s, gx, ex, n[0], ga, ea, n[1], gb, eb);
+  return (int)hipGetLastError();
+}
+
 __global__ void __launch_bounds__(256) zero_kernel(u32x4* p, size_t n) {
   for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) p[i] = u32x4{0u, 0u, 0u, 0u};
 }
@@ -60,6 +88,23 @@ __global__ void __launch_bounds__(256) gated_panelise_kernel(const u32x4* __rest
 // weights: T 16384 D 4096 F 16384 4.28 -> 3.22 ms + 0.12 for the pass, T 8192 D 2048 F 8192 591 -> 479 us + 34; on 128 x 64 tiles (T 1000) 40.0 -> 38.5.  dH, whose epilogue
 // moves more than its operands, gains 2.18 -> 2.10 ms for a pass of 0.06 and 401 -> 405 us: it reads Wd row by row.
 bool gated_dx_panels(int T, int D, int F) { return T >= 2048 && pick_edge_tile(D, T, 2 * F) == 0; }
+// The tile of dX and the weight gradients in one launch, 0: apart.  Together they take all their tiles over the CUs and one tile of the shorter kind more, or the dX tiles'
+// own rounds if that is longer.
+int pick_grads_tile(int T, int D, int F, int K) {
+  const int tx = pick_edge_tile(D, T, 2 * F), tw = pick_edge_tile(D, 2 * F, K, F, D);
+  const auto rounds = [](long long n) { return (n + CHIP_CUS - 1) / CHIP_CUS; };
+  const auto weights = [&](const TileCost& t) { return edge_tiles(t, D, 2 * F) + edge_tiles(t, F, D); };
+  long long best_time = rounds(edge_tiles(TILES_DENSE[tx], D, T)) * tile_time(TILES_DENSE[tx], 2 * F, false) +
+                        rounds(weights(TILES_DENSE[tw])) * tile_time(TILES_DENSE[tw], K, false) + 3000;
+  int best = 0;
+  for (int i = 1; i < NUM_TILES; i++) {
+    const TileCost& t = TILES_DENSE[i];
+    const long long nx = edge_tiles(t, D, T), one_x = tile_time(t, 2 * F, false), one_w = tile_time(t, K, false);
+    const long long all = (nx * one_x + weights(t) * one_w) / CHIP_CUS + one_w, time = all > rounds(nx) * one_x ? all : rounds(nx) * one_x;
+    if (time < best_time) { best = i; best_time = time; }
+  }
+  return best;
+}
 size_t gated_panel_bytes(int rows, int K) { return 2 * (size_t)up_to(rows, 256) * (size_t)K; }
 int launch_gated_panels(const void* Wgu, int D, int F, void* panels, hipStream_t s) {
   const size_t items = gated_panel_bytes(D, 2 * F) / 16;
@@ -88,17 +133,23 @@ int launch_gated_dgate(const void* dY, const void* Wd, const void* GU, const voi
   return launch_edge<EpiDGate, 0>(args(Wd, F, D, dY, T, D, F, T, D), EpiDGate::Args{static_cast<const __bf16*>(GU), static_cast<const uint8_t*>(GUx), static_cast<__bf16*>(dGU), F, T, Gate{c1, c3}}, s);
 }
 
-int launch_gated_dx(const void* dGU, const void* Wgu, bool panels, int T, int D, int F, void* dX, hipStream_t s) {
-  using Epi = EdgeColMajor<false>;
-  GemmArgs g = args(Wgu, D, 2 * F, dGU, T, 2 * F, D, T, 2 * F);
-  g.a_panel = panels;
-  return launch_edge<Epi, 0>(g, Epi::Args{static_cast<__bf16*>(dX), D, T, I8Scales{}}, s);
-}
-
-int launch_gated_wgrad(const void* X, const void* dY, const void* H, const void* dGU, int T, int D, int F, void* dWgu, void* dWd, hipStream_t s) {
+int launch_gated_grads(const void* X, const void* dY, const void* H, const void* dGU, const void* Wgu, bool panels, int T, int D, int F, void* dX, void* dWgu, void* dWd,
+                       hipStream_t s) {
+  using EpiX = EdgeColMajor<false>;
   const int K = up_to(T, 64);
+  GemmArgs gx = args(Wgu, D, 2 * F, dGU, T, 2 * F, D, T, 2 * F);
+  gx.a_panel = panels;
   const GemmArgs ga = args(X, T, D, dGU, T, 2 * F, D, 2 * F, K), gb = args(H, T, F, dY, T, D, F, D, K);
+  const EpiX::Args ex{static_cast<__bf16*>(dX), D, T, I8Scales{}};
   const EdgeRowMajor::Args ea{static_cast<__bf16*>(dWgu), D, 2 * F}, eb{static_cast<__bf16*>(dWd), F, D};
+  switch (panels ? 0 : pick_grads_tile(T, D, F, K)) {
+    case 1: return launch_grads_tile<4, 2>(gx, ex, ga, ea, gb, eb, s);
+    case 2: return launch_grads_tile<2, 2>(gx, ex, ga, ea, gb, eb, s);
+    case 3: return launch_grads_tile<2, 1>(gx, ex, ga, ea, gb, eb, s);
+    case 4: return launch_grads_tile<1, 1>(gx, ex, ga, ea, gb, eb, s);
+    default: break;                        // apart
+  }
+  if (int rc = launch_edge<EpiX, 0>(gx, ex, s)) return rc;
   switch (pick_edge_tile(D, 2 * F, K, F, D)) {
     case 0: return launch_wgrad_tile<4, 4>(ga, ea, gb, eb, s);
     case 1: return launch_wgrad_tile<4, 2>(ga, ea, gb, eb, s);

@@ -21,8 +21,8 @@ bool gated_dx_panels(int T, int D, int F);   // whether dX reads Wgu in panel fo
 size_t gated_panel_bytes(int rows, int K);
 int launch_gated_panels(const void* Wgu, int D, int F, void* panels, hipStream_t s);
 int launch_gated_dgate(const void* dY, const void* Wd, const void* GU, const void* GUx, int T, int D, int F, float c1, float c3, void* dGU, hipStream_t s);
-int launch_gated_dx(const void* dGU, const void* Wgu, bool panels, int T, int D, int F, void* dX, hipStream_t s);
-int launch_gated_wgrad(const void* X, const void* dY, const void* H, const void* dGU, int T, int D, int F, void* dWgu, void* dWd, hipStream_t s);
+int launch_gated_grads(const void* X, const void* dY, const void* H, const void* dGU, const void* Wgu, bool panels, int T, int D, int F, void* dX, void* dWgu, void* dWd,
+                       hipStream_t s);
 int launch_zero(void* p, size_t bytes, hipStream_t s);   // 16-byte aligned, a multiple of 16 bytes
 
 // k_i8.hip: K a multiple of 16, N of 8 (with two halves: of 16); T >= 1
