@@ -45,7 +45,8 @@ typedef enum { FFN24_GATE_SILU = 0, FFN24_GATE_GELU_TANH = 1 } ffn24_gate;
 typedef struct gated_ctx gated_ctx; /* opaque; owns only its device workspace */
 
 /* A context for up to T tokens (1 <= T <= 2^20; every call says how many it has, any number up to T), D and F multiples of 64, at most 2^18.
- * flags: 0 or FFN24_TRAINING (gated_bwd).  Workspace, allocated on the current device: 2 T F bytes; 12 T F with FFN24_TRAINING.  A context belongs to that
+ * flags: 0 or FFN24_TRAINING (gated_bwd).  Workspace, allocated on the current device: 2 T F bytes, 12 T F with FFN24_TRAINING, and besides
+ * what a split reduction takes (some tens of MiB at most) and, in training, the size of Wgu.  A context belongs to that
  * device and to one thread at a time; calls on different streams are the caller's to order.  *out is untouched on error. */
 FFN24_API int gated_ctx_create(gated_ctx** out, int64_t T, int64_t D, int64_t F, ffn24_gate gate, int flags);
 /* The caller must have synchronised every stream that used the context.  NULL is allowed. */
@@ -74,13 +75,13 @@ FFN24_API int i8_weight(const void* W, int64_t K, int64_t N, int halves, void* o
 FFN24_API int quantise_i8(const void* X, int64_t T, int64_t K, void* codes, float* scales, void* stream);
 /* Y [T][N] (bf16) from codes and scales of quantise_i8 and weights of i8_weight */
 FFN24_API int matmul_i8(const void* codes, const float* scales, int64_t T, const void* weight, int64_t K, int64_t N, void* Y, void* stream);
-/* The two in one call: Y from bf16 X.  scratch: linear_i8_scratch(T, K) bytes, used until the call's last kernel has run. */
-FFN24_API int64_t linear_i8_scratch(int64_t T, int64_t K);   /* or -1 */
+/* The two in one call: Y from bf16 X.  scratch: linear_i8_scratch(T, K, N) bytes, used until the call's last kernel has run. */
+FFN24_API int64_t linear_i8_scratch(int64_t T, int64_t K, int64_t N);   /* or -1 */
 FFN24_API int linear_i8(const void* X, int64_t T, const void* weight, int64_t K, int64_t N, void* Y, void* scratch, void* stream);
 
 /* The gated block on int8 weights: G, U in fp32 from such products of X and [Wg | Wu];  h = a(G) U;  sh[t] = max_f |h[t][f]| * (1 / 127) (1 if zero);
  * H8 = rint(bf16(h) / sh), held to -127 .. 127;  Y = bf16(sh[t] sw[d] sum_f H8 Wd8).  T, D, F, gate as for gated_ctx_create, F at most 2^17.
- * Workspace: T (D + 3 F + 12) bytes and the weights (3 D F and a little).  gated_i8_set_weights quantises Wgu [D][2 F] and Wd [F][D] (bf16) into the context, which
+ * Workspace: T (D + 3 F + 12) bytes, the weights (3 D F and a little) and what a split reduction takes (some tens of MiB at most).  gated_i8_set_weights quantises Wgu [D][2 F] and Wd [F][D] (bf16) into the context, which
  * does not need them afterwards; gated_i8_fwd before it returns FFN24_ERR_STATE. */
 typedef struct gated_i8_ctx gated_i8_ctx;
 FFN24_API int gated_i8_ctx_create(gated_i8_ctx** out, int64_t T, int64_t D, int64_t F, ffn24_gate gate);

@@ -41,7 +41,7 @@ def lib() -> ctypes.CDLL:
         L.i8_weight.argtypes = [vp, i64, i64, ci, vp, vp]
         L.quantise_i8.argtypes = [vp, i64, i64, vp, vp, vp]
         L.matmul_i8.argtypes = [vp, vp, i64, vp, i64, i64, vp, vp]
-        L.linear_i8_scratch.argtypes = [i64, i64]
+        L.linear_i8_scratch.argtypes = [i64, i64, i64]
         L.linear_i8.argtypes = [vp, i64, vp, i64, i64, vp, vp, vp]
         L.gated_i8_ctx_create.argtypes = [ctypes.POINTER(vp), i64, i64, i64, ci]
         L.gated_i8_ctx_destroy.argtypes = [vp]
@@ -210,7 +210,7 @@ def linear_i8(X, W: I8Weight, Y=None):
     _expect(X, (T, W.K), _BF16, "X")
     Y = torch.empty((T, W.N), dtype=torch.bfloat16, device=X.device) if Y is None else Y
     _expect(Y, (T, W.N), _BF16, "Y")
-    scratch = torch.empty(_size(int(lib().linear_i8_scratch(T, W.K)), "linear_i8"), dtype=torch.uint8, device=X.device)
+    scratch = torch.empty(_size(int(lib().linear_i8_scratch(T, W.K, W.N)), "linear_i8"), dtype=torch.uint8, device=X.device)
     _check(lib().linear_i8(_ptr(X), T, _ptr(W.data), W.K, W.N, _ptr(Y), _ptr(scratch), _stream(X)), "linear_i8")
     return Y
 

@@ -37,7 +37,7 @@ struct gated_ctx {
   int64_t fwd_T;               // tokens of the last forward, -1: none yet
   void *H, *GU, *GUx, *dGU;    // [T][F] bf16; in training G and U ([T][2 F] bf16 and bytes) and their gradients [T][2 F]
   void *Wgu_p;                 // in training: Wgu in panel form, made by a backward that reads it so
-  void *parts;                 // sums over parts of a reduction (few tokens)
+  Scratch scratch;             // sums over parts of a reduction
 };
 
 struct gated_i8_ctx {
@@ -47,6 +47,7 @@ struct gated_i8_ctx {
   void *Wgu, *Wd;              // laid out by i8_weight
   void *X8, *H, *H8;           // [T][D] codes, [T][F] bf16, [T][F] codes
   float *sx, *sh; uint32_t* tops;
+  Scratch scratch;             // sums over parts of a reduction
 };
 
 namespace {
@@ -95,7 +96,9 @@ int gated_ctx_create(gated_ctx** out, int64_t T, int64_t D, int64_t F, ffn24_gat
   bool ok = hipGetDevice(&c->device) == hipSuccess && hipMalloc(&c->H, 2 * tf) == hipSuccess;
   if (ok && c->training) ok = hipMalloc(&c->GU, 4 * tf) == hipSuccess && hipMalloc(&c->GUx, 2 * tf) == hipSuccess && hipMalloc(&c->dGU, 4 * tf) == hipSuccess;
   if (ok && c->training && gated_dx_panels((int)T, (int)D, (int)F)) ok = hipMalloc(&c->Wgu_p, gated_panel_bytes((int)D, (int)(2 * F))) == hipSuccess;
-  if (ok && !c->training) ok = hipMalloc(&c->parts, few_gated_scratch((int)T, (int)D, (int)F)) == hipSuccess;
+  const size_t few = few_gated_scratch((int)T, (int)D, (int)F), most = gated_scratch((int)T, (int)D, (int)F, c->training);
+  c->scratch.bytes = few > most ? few : most;
+  if (ok) ok = hipMalloc(&c->scratch.p, c->scratch.bytes) == hipSuccess;
   if (!ok) {
     (void)hipGetLastError();
     gated_ctx_destroy(c);
@@ -108,7 +111,7 @@ int gated_ctx_create(gated_ctx** out, int64_t T, int64_t D, int64_t F, ffn24_gat
 int gated_ctx_destroy(gated_ctx* c) {
   if (!c) return FFN24_OK;
   int bad = 0;
-  for (void* p : {c->H, c->GU, c->GUx, c->dGU, c->Wgu_p, c->parts}) if (p && hipFree(p) != hipSuccess) bad = 1;
+  for (void* p : {c->H, c->GU, c->GUx, c->dGU, c->Wgu_p, c->scratch.p}) if (p && hipFree(p) != hipSuccess) bad = 1;
   delete c;
   return bad ? FFN24_ERR_HIP : FFN24_OK;
 }
@@ -122,12 +125,12 @@ int gated_fwd(gated_ctx* c, const void* X, int64_t T, const void* Wgu, const voi
   c->fwd_T = -1;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int t = (int)T, D = (int)c->D, F = (int)c->F;
-  if (T > 0 && !c->training && few_tokens(t, D, F)) {
-    float* parts = static_cast<float*>(c->parts);
-    if (launch_few_gated_up(X, Wgu, t, D, F, c->gate.c1, c->gate.c3, c->H, parts, s) || launch_few_gated_down(c->H, Wd, t, D, F, Y, parts, s)) return FFN24_ERR_HIP;
-  } else if (T > 0) {
-    if (launch_gated_up(X, Wgu, t, D, F, c->gate.c1, c->gate.c3, c->H, c->GU, c->GUx, s)) return FFN24_ERR_HIP;
-    if (launch_gated_down(c->H, Wd, t, D, F, Y, s)) return FFN24_ERR_HIP;
+  if (T > 0) {
+    const bool few = few_tokens(t, D, F);        // (the kernel for few tokens keeps nothing for a backward)
+    float* parts = static_cast<float*>(c->scratch.p);
+    if (few && !c->training ? launch_few_gated_up(X, Wgu, t, D, F, c->gate.c1, c->gate.c3, c->H, parts, s)
+                            : launch_gated_up(X, Wgu, t, D, F, c->gate.c1, c->gate.c3, c->H, c->GU, c->GUx, s)) return FFN24_ERR_HIP;
+    if (few ? launch_few_gated_down(c->H, Wd, t, D, F, Y, parts, s) : launch_gated_down(c->H, Wd, t, D, F, Y, c->scratch, s)) return FFN24_ERR_HIP;
   }
   c->fwd_T = T;
   return FFN24_OK;
@@ -148,7 +151,7 @@ int gated_bwd(gated_ctx* c, const void* dY, const void* X, const void* Wgu, cons
     Wgu = c->Wgu_p;
   }
   if (launch_gated_dgate(dY, Wd, c->GU, c->GUx, t, D, F, c->gate.c1, c->gate.c3, c->dGU, s)) return FFN24_ERR_HIP;
-  return done(launch_gated_grads(X, dY, c->H, c->dGU, Wgu, panels, t, D, F, dX, dWgu, dWd, s));
+  return done(launch_gated_grads(X, dY, c->H, c->dGU, Wgu, panels, t, D, F, dX, dWgu, dWd, c->scratch, s));
 }
 
 int64_t i8_weight_bytes(int64_t K, int64_t N) { return i8_sizes(K, N) ? i8_weight_size(K, N) : -1; }
@@ -173,10 +176,12 @@ int matmul_i8(const void* codes, const float* scales, int64_t T, const void* wei
   if (T == 0) return FFN24_OK;
   if (!codes || !scales || !weight || !Y) return FFN24_ERR_NULL;
   if (misaligned(codes, scales, weight, Y)) return FFN24_ERR_ALIGN;
-  return done(launch_matmul_i8(codes, scales, (int)T, i8_layout(weight, (int)K, (int)N), Y, static_cast<hipStream_t>(stream)));
+  return done(launch_matmul_i8(codes, scales, (int)T, i8_layout(weight, (int)K, (int)N), Y, Scratch{}, static_cast<hipStream_t>(stream)));
 }
 
-int64_t linear_i8_scratch(int64_t T, int64_t K) { return i8_rows(T, K) ? T * K + up16(4 * T) : -1; }
+int64_t linear_i8_scratch(int64_t T, int64_t K, int64_t N) {
+  return i8_rows(T, K) && i8_sizes(K, N) ? T * K + up16(4 * T) + (T > 0 ? (int64_t)matmul_i8_scratch((int)T, (int)K, (int)N) : 0) : -1;
+}
 
 int linear_i8(const void* X, int64_t T, const void* weight, int64_t K, int64_t N, void* Y, void* scratch, void* stream) {
   if (!i8_rows(T, K) || !i8_sizes(K, N)) return FFN24_ERR_SHAPE;
@@ -187,7 +192,8 @@ int linear_i8(const void* X, int64_t T, const void* weight, int64_t K, int64_t N
   if (few_i8_fuses((int)T, (int)K)) return done(launch_few_linear_i8(X, (int)T, i8_layout(weight, (int)K, (int)N), Y, s));
   float* sx = reinterpret_cast<float*>(static_cast<char*>(scratch) + T * K);
   if (launch_quantise_i8(X, (int)T, (int)K, scratch, sx, nullptr, s)) return FFN24_ERR_HIP;
-  return done(launch_matmul_i8(scratch, sx, (int)T, i8_layout(weight, (int)K, (int)N), Y, s));
+  const Scratch rest{static_cast<char*>(scratch) + T * K + up16(4 * T), matmul_i8_scratch((int)T, (int)K, (int)N)};
+  return done(launch_matmul_i8(scratch, sx, (int)T, i8_layout(weight, (int)K, (int)N), Y, rest, s));
 }
 
 int gated_i8_ctx_create(gated_i8_ctx** out, int64_t T, int64_t D, int64_t F, ffn24_gate gate) {
@@ -198,7 +204,9 @@ int gated_i8_ctx_create(gated_i8_ctx** out, int64_t T, int64_t D, int64_t F, ffn
   if (!c) return FFN24_ERR_HIP;
   c->T = T; c->D = D; c->F = F; c->gate = coefficients(gate);
   const size_t td = (size_t)T * (size_t)D, tf = (size_t)T * (size_t)F, t4 = 4 * (size_t)T, few = few_i8_tops((int)T, (int)F), tops = few > t4 ? few : t4;
-  const bool ok = hipGetDevice(&c->device) == hipSuccess && hipMalloc(&c->Wgu, (size_t)i8_weight_size(D, 2 * F)) == hipSuccess &&
+  c->scratch.bytes = gated_i8_scratch((int)T, (int)D, (int)F);
+  const bool ok = hipGetDevice(&c->device) == hipSuccess && (!c->scratch.bytes || hipMalloc(&c->scratch.p, c->scratch.bytes) == hipSuccess) &&
+                  hipMalloc(&c->Wgu, (size_t)i8_weight_size(D, 2 * F)) == hipSuccess &&
                   hipMalloc(&c->Wd, (size_t)i8_weight_size(F, D)) == hipSuccess && hipMalloc(&c->X8, td) == hipSuccess && hipMalloc(&c->H, 2 * tf) == hipSuccess &&
                   hipMalloc(&c->H8, tf) == hipSuccess && hipMalloc(reinterpret_cast<void**>(&c->sx), t4) == hipSuccess &&
                   hipMalloc(reinterpret_cast<void**>(&c->sh), t4) == hipSuccess && hipMalloc(reinterpret_cast<void**>(&c->tops), tops) == hipSuccess;
@@ -214,7 +222,7 @@ int gated_i8_ctx_create(gated_i8_ctx** out, int64_t T, int64_t D, int64_t F, ffn
 int gated_i8_ctx_destroy(gated_i8_ctx* c) {
   if (!c) return FFN24_OK;
   int bad = 0;
-  void* bufs[] = {c->Wgu, c->Wd, c->X8, c->H, c->H8, c->sx, c->sh, c->tops};
+  void* bufs[] = {c->Wgu, c->Wd, c->X8, c->H, c->H8, c->sx, c->sh, c->tops, c->scratch.p};
   for (void* p : bufs) if (p && hipFree(p) != hipSuccess) bad = 1;
   delete c;
   return bad ? FFN24_ERR_HIP : FFN24_OK;
@@ -246,7 +254,7 @@ int gated_i8_fwd(gated_i8_ctx* c, const void* X, int64_t T, void* Y, void* strea
   if (launch_quantise_i8(X, t, D, c->X8, c->sx, c->tops, s)) return FFN24_ERR_HIP;
   if (launch_gated_up_i8(c->X8, c->sx, t, i8_layout(c->Wgu, D, 2 * F), c->gate.c1, c->gate.c3, c->H, c->tops, s)) return FFN24_ERR_HIP;
   if (launch_quantise_i8_given(c->H, c->tops, t, F, c->H8, c->sh, s)) return FFN24_ERR_HIP;
-  return done(launch_matmul_i8(c->H8, c->sh, t, i8_layout(c->Wd, F, D), Y, s));
+  return done(launch_matmul_i8(c->H8, c->sh, t, i8_layout(c->Wd, F, D), Y, c->scratch, s));
 }
 
 }  // extern "C"

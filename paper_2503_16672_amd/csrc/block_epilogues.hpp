@@ -36,7 +36,7 @@ constexpr uint32_t OUTSIDE = 0x80000000u;   // an offset that no descriptor hold
 // out[n][m], m contiguous, through LDS (ColMajorStage)
 template <bool I8>
 struct EdgeColMajor {
-  static constexpr bool STAGED = true;
+  static constexpr bool STAGED = true, INTEGER = I8;
   struct Args { __bf16* C; int M, N; I8Scales sc; };
   template <int MI, int NI, class Acc>
   static __device__ __forceinline__ void run(const Args& e, Acc& acc, int m_lane, int n_lane, char* wbuf) {
@@ -66,6 +66,49 @@ struct EdgeColMajor {
     }
   }
 };
+
+// The accumulators as they are (fp32, or 32-bit integers), out[n][m]: the sums of a part of the reduction
+struct EdgePart {
+  struct Args { uint32_t* parts; int M, N; };
+  template <int MI, int NI, class Acc>
+  static __device__ __forceinline__ void run(const Args& e, Acc& acc, int m_lane, int n_lane) {
+#pragma unroll
+    for (int ni = 0; ni < NI; ni++) {
+      if (n_lane + ni >= e.N) continue;
+      uint32_t* out = e.parts + (size_t)(n_lane + ni) * e.M + m_lane;
+#pragma unroll
+      for (int mi = 0; mi < MI; mi++)
+#pragma unroll
+        for (int v = 0; v < 16; v += 4) {
+          u32x4 o;
+#pragma unroll
+          for (int d = 0; d < 4; d++) o[d] = __builtin_bit_cast(uint32_t, (float)acc[mi][ni][v + d]);
+          if (m_lane + 16 * mi + v < e.M) *reinterpret_cast<u32x4*>(out + 16 * mi + v) = o;
+        }
+    }
+  }
+};
+// The sums of `splits` parts, four values a work item; integers are scaled
+template <bool I8>
+__global__ void __launch_bounds__(256) edge_sum_kernel(const uint32_t* __restrict__ parts, int splits, int M, int N, I8Scales sc, uint16_t* __restrict__ out) {
+  const size_t n = (size_t)M * N;
+  const unsigned i = blockIdx.x * 256 + threadIdx.x, per = (unsigned)M / 4, t = i / per, col = 4 * (i - t * per);
+  if (t >= (unsigned)N) return;
+  const uint32_t* p = parts + (size_t)t * M + col;
+  float y[4];
+  if constexpr (I8) {
+    i32x4 a = *reinterpret_cast<const i32x4*>(p);
+    for (int s = 1; s < splits; s++) a += *reinterpret_cast<const i32x4*>(p + s * n);
+#pragma unroll
+    for (int j = 0; j < 4; j++) y[j] = (float)a[j] * (sc.sx[t] * sc.sw[col + j]);
+  } else {
+    f32x4 a = *reinterpret_cast<const f32x4*>(p);
+    for (int s = 1; s < splits; s++) a += *reinterpret_cast<const f32x4*>(p + s * n);
+#pragma unroll
+    for (int j = 0; j < 4; j++) y[j] = a[j];
+  }
+  *reinterpret_cast<u32x2*>(out + (size_t)t * M + col) = u32x2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
+}
 
 // out[m][n], n contiguous, N a multiple of 8
 struct EdgeRowMajor {

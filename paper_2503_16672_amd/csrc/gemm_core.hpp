@@ -77,7 +77,7 @@ struct GemmArgs {
   unsigned long long* clk;   // optional (profiling): workgroup i < CLK_SLOTS stores its own {shader-clock ticks, 100 MHz ticks} at 2 i
   // TR_EDGE only: what is really there of the operands; M, N and K above are then rounded up to whole tiles and stages
   int a_rows, b_rows;    // rows of A, of B (K-contiguous), or k's (k-major)
-  int a_pitch, b_pitch;  // bytes from one of them to the next
+  int a_pitch, b_pitch;  // bytes from one of them to the next (panel form: of a whole row)
   uint32_t gate;         // TR_GATE: bytes from a gate column of A to the up column of the same feature
 };
 
@@ -290,7 +290,7 @@ struct Dma {
     const int ma = MI == 4 ? 0 : m0 & 255, mb = m0 - ma;
     const uint32_t a_pitch = panel ? 64u : (uint32_t)g.a_pitch, b_pitch = (uint32_t)g.b_pitch;
     // the first byte of the block, and one behind the tensor's last
-    const int64_t a0 = TRA ? (int64_t)m0 * (GATE ? 1 : G::ESIZE) : panel ? (int64_t)mb * g.K * G::ESIZE + ma * 64 : (int64_t)m0 * a_pitch;
+    const int64_t a0 = TRA ? (int64_t)m0 * (GATE ? 1 : G::ESIZE) : panel ? (int64_t)mb * g.a_pitch + ma * 64 : (int64_t)m0 * a_pitch;
     const int64_t b0 = TRB ? (int64_t)n0 * G::ESIZE : (int64_t)n0 * b_pitch;
     ea = static_cast<const char*>(g.A) + a0;
     eb = static_cast<const char*>(g.B) + b0;

@@ -88,14 +88,22 @@ __global__ void __launch_bounds__(256) gated_panelise_kernel(const u32x4* __rest
 // weights: T 16384 D 4096 F 16384 4.28 -> 3.22 ms + 0.12 for the pass, T 8192 D 2048 F 8192 591 -> 479 us + 34; on 128 x 64 tiles (T 1000) 40.0 -> 38.5.  dH, whose epilogue
 // moves more than its operands, gains 2.18 -> 2.10 ms for a pass of 0.06 and 401 -> 405 us: it reads Wd row by row.
 bool gated_dx_panels(int T, int D, int F) { return T >= 2048 && pick_edge_tile(D, T, 2 * F) == 0; }
+// for any token count up to T: what the splits of Y and dX need (beyond 2^24 values a result has 4096 of the smallest tiles)
+size_t gated_scratch(int T, int D, int F, bool training) {
+  size_t most = 0;
+  for (int t = 64; t <= up_to(T, 64) && (long long)D * t <= 1 << 24; t += 64) {
+    const size_t y = edge_split_scratch(D, t, F), x = training ? edge_split_scratch(D, t, 2 * F) : 0, top = y > x ? y : x;
+    if (top > most) most = top;
+  }
+  return most;
+}
 // The tile of dX and the weight gradients in one launch, 0: apart.  Together they take all their tiles over the CUs and one tile of the shorter kind more, or the dX tiles'
 // own rounds if that is longer.
 int pick_grads_tile(int T, int D, int F, int K) {
-  const int tx = pick_edge_tile(D, T, 2 * F), tw = pick_edge_tile(D, 2 * F, K, F, D);
+  const int tw = pick_edge_tile(D, 2 * F, K, F, D);
   const auto rounds = [](long long n) { return (n + CHIP_CUS - 1) / CHIP_CUS; };
   const auto weights = [&](const TileCost& t) { return edge_tiles(t, D, 2 * F) + edge_tiles(t, F, D); };
-  long long best_time = rounds(edge_tiles(TILES_DENSE[tx], D, T)) * tile_time(TILES_DENSE[tx], 2 * F, false) +
-                        rounds(weights(TILES_DENSE[tw])) * tile_time(TILES_DENSE[tw], K, false) + 3000;
+  long long best_time = edge_split_time(D, T, 2 * F) + rounds(weights(TILES_DENSE[tw])) * tile_time(TILES_DENSE[tw], K, false) + 3000;
   int best = 0;
   for (int i = 1; i < NUM_TILES; i++) {
     const TileCost& t = TILES_DENSE[i];
@@ -124,9 +132,9 @@ int launch_gated_up(const void* X, const void* Wgu, int T, int D, int F, float c
   return launch_edge<Epi, TR_A | TR_GATE>(g, Epi::Args{static_cast<__bf16*>(H), static_cast<__bf16*>(GU), static_cast<uint8_t*>(GUx), F, T, Gate{c1, c3}, I8Scales{}, nullptr}, s);
 }
 
-int launch_gated_down(const void* H, const void* Wd, int T, int D, int F, void* Y, hipStream_t s) {
+int launch_gated_down(const void* H, const void* Wd, int T, int D, int F, void* Y, const Scratch& scratch, hipStream_t s) {
   using Epi = EdgeColMajor<false>;
-  return launch_edge<Epi, TR_A>(args(Wd, F, D, H, T, F, D, T, F), Epi::Args{static_cast<__bf16*>(Y), D, T, I8Scales{}}, s);
+  return launch_edge_split<Epi, TR_A>(args(Wd, F, D, H, T, F, D, T, F), Epi::Args{static_cast<__bf16*>(Y), D, T, I8Scales{}}, scratch, s);
 }
 
 int launch_gated_dgate(const void* dY, const void* Wd, const void* GU, const void* GUx, int T, int D, int F, float c1, float c3, void* dGU, hipStream_t s) {
@@ -134,7 +142,7 @@ int launch_gated_dgate(const void* dY, const void* Wd, const void* GU, const voi
 }
 
 int launch_gated_grads(const void* X, const void* dY, const void* H, const void* dGU, const void* Wgu, bool panels, int T, int D, int F, void* dX, void* dWgu, void* dWd,
-                       hipStream_t s) {
+                       const Scratch& scratch, hipStream_t s) {
   using EpiX = EdgeColMajor<false>;
   const int K = up_to(T, 64);
   GemmArgs gx = args(Wgu, D, 2 * F, dGU, T, 2 * F, D, T, 2 * F);
@@ -149,7 +157,7 @@ int launch_gated_grads(const void* X, const void* dY, const void* H, const void*
     case 4: return launch_grads_tile<1, 1>(gx, ex, ga, ea, gb, eb, s);
     default: break;                        // apart
   }
-  if (int rc = launch_edge<EpiX, 0>(gx, ex, s)) return rc;
+  if (int rc = launch_edge_split<EpiX, 0>(gx, ex, scratch, s)) return rc;
   switch (pick_edge_tile(D, 2 * F, K, F, D)) {
     case 0: return launch_wgrad_tile<4, 4>(ga, ea, gb, eb, s);
     case 1: return launch_wgrad_tile<4, 2>(ga, ea, gb, eb, s);

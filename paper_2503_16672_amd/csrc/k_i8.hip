@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(256) i8_weight_codes_kernel(const uint16_t* __
 int64_t pad(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 GemmArgs args(const I8Layout& w, const void* codes, int T) {
   GemmArgs g{};
-  g.A = w.panels; g.a_panel = 1;
+  g.A = w.panels; g.a_panel = 1; g.a_pitch = (int)pad(w.K, 128);
   g.B = codes; g.b_rows = T; g.b_pitch = w.K;
   g.M = w.N; g.N = T; g.K = (int)pad(w.K, 128) / 2;           // in pairs of bytes
   return g;
@@ -177,10 +177,19 @@ int launch_quantise_i8_given(const void* H, const uint32_t* tops, int T, int F, 
   return (int)hipGetLastError();
 }
 
-int launch_matmul_i8(const void* codes, const float* sx, int T, const I8Layout& w, void* Y, hipStream_t s) {
+size_t matmul_i8_scratch(int T, int K, int N) { return few_i8_tokens(T, K) ? 0 : edge_split_scratch(N, T, (int)pad(K, 128) / 2); }
+size_t gated_i8_scratch(int T, int D, int F) {
+  size_t most = 0;
+  for (int t = 64; t <= up_to(T, 64) && (long long)D * t <= 1 << 24; t += 64) {
+    const size_t y = edge_split_scratch(D, t, (int)pad(F, 128) / 2);
+    if (y > most) most = y;
+  }
+  return most;
+}
+int launch_matmul_i8(const void* codes, const float* sx, int T, const I8Layout& w, void* Y, const Scratch& scratch, hipStream_t s) {
   if (few_i8_tokens(T, w.K)) return launch_few_matmul_i8(codes, sx, T, w, Y, s);
   using Epi = EdgeColMajor<true>;
-  return launch_edge<Epi, TR_I8>(args(w, codes, T), Epi::Args{static_cast<__bf16*>(Y), w.N, T, I8Scales{sx, w.scales}}, s);
+  return launch_edge_split<Epi, TR_I8>(args(w, codes, T), Epi::Args{static_cast<__bf16*>(Y), w.N, T, I8Scales{sx, w.scales}}, scratch, s);
 }
 
 int launch_gated_up_i8(const void* codes, const float* sx, int T, const I8Layout& w, float c1, float c3, void* H, uint32_t* rowmax, hipStream_t s) {

@@ -7,6 +7,8 @@ namespace ffn24 {
 
 constexpr int NORM_MAX_D = 16384;
 
+struct Scratch { void* p; size_t bytes; };   // device memory of a call or a context
+
 // k_norm.hip
 int launch_norm_fwd(const void* X, const void* R, const float* w, const float* b, int T, int D, float eps, bool f32, void* S, void* Y, float* mean, float* rstd,
                     hipStream_t s);
@@ -16,13 +18,14 @@ int launch_norm_bwd(const void* dY, const void* S, const float* w, const float* 
 
 // k_gated.hip: T >= 1, D and F multiples of 64; GU, GUx (EpiGateUp) NULL in a forward without a backward
 int launch_gated_up(const void* X, const void* Wgu, int T, int D, int F, float c1, float c3, void* H, void* GU, void* GUx, hipStream_t s);
-int launch_gated_down(const void* H, const void* Wd, int T, int D, int F, void* Y, hipStream_t s);
+int launch_gated_down(const void* H, const void* Wd, int T, int D, int F, void* Y, const Scratch& scratch, hipStream_t s);
+size_t gated_scratch(int T, int D, int F, bool training);   // bytes of `scratch` for any token count up to T (with less, reductions are not split)
 bool gated_dx_panels(int T, int D, int F);   // whether dX reads Wgu in panel form (`panels` below: it is)
 size_t gated_panel_bytes(int rows, int K);
 int launch_gated_panels(const void* Wgu, int D, int F, void* panels, hipStream_t s);
 int launch_gated_dgate(const void* dY, const void* Wd, const void* GU, const void* GUx, int T, int D, int F, float c1, float c3, void* dGU, hipStream_t s);
 int launch_gated_grads(const void* X, const void* dY, const void* H, const void* dGU, const void* Wgu, bool panels, int T, int D, int F, void* dX, void* dWgu, void* dWd,
-                       hipStream_t s);
+                       const Scratch& scratch, hipStream_t s);
 int launch_zero(void* p, size_t bytes, hipStream_t s);   // 16-byte aligned, a multiple of 16 bytes
 
 // k_i8.hip: K a multiple of 16, N of 8 (with two halves: of 16); T >= 1
@@ -32,7 +35,9 @@ I8Layout i8_layout(const void* p, int K, int N);
 int launch_i8_weight(const void* W, int K, int N, bool halves, void* out, hipStream_t s);
 int launch_quantise_i8(const void* X, int T, int K, void* codes, float* scales, uint32_t* zero, hipStream_t s);
 int launch_quantise_i8_given(const void* H, const uint32_t* tops, int T, int F, void* codes, float* scales, hipStream_t s);
-int launch_matmul_i8(const void* codes, const float* sx, int T, const I8Layout& w, void* Y, hipStream_t s);
+size_t matmul_i8_scratch(int T, int K, int N);
+size_t gated_i8_scratch(int T, int D, int F);    // for any token count up to T
+int launch_matmul_i8(const void* codes, const float* sx, int T, const I8Layout& w, void* Y, const Scratch& scratch, hipStream_t s);
 int launch_gated_up_i8(const void* codes, const float* sx, int T, const I8Layout& w, float c1, float c3, void* H, uint32_t* rowmax, hipStream_t s);
 
 // k_few.hip: few tokens, where the weights are what counts

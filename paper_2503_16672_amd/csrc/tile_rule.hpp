@@ -73,6 +73,34 @@ inline int pick_edge_tile(int M, int N, int K, int M2 = 0, int N2 = 0) {
   return best;
 }
 
+// A reduction split over several workgroups a tile: tile, parts, k's of a part (a multiple of 64).  The smaller three tiles; a second launch adds the parts up, which are written and
+// read once.  One part unless the estimate is 10 % better.
+// N counts as the next multiple of 64, so that a workspace for some N holds what smaller ones take.
+struct EdgeSplit { int tile, splits, part; };
+constexpr int MOST_SPLITS = 16;
+inline EdgeSplit pick_edge_split(int M, int N_real, int K) {
+  const int N = (N_real + 63) / 64 * 64;
+  EdgeSplit best = {pick_edge_tile(M, N, K), 1, K};
+  const TileCost& whole = TILES_DENSE[best.tile];
+  long long best_time = (edge_tiles(whole, M, N) + CHIP_CUS - 1) / CHIP_CUS * tile_time(whole, K, false) * 9 / 10;
+  for (int i = 2; i < NUM_TILES; i++) {
+    const TileCost& t = TILES_DENSE[i];
+    for (int s = 2; s <= MOST_SPLITS && K / s >= 512; s++) {
+      const int part = (K / 64 + s - 1) / s * 64;
+      if ((long long)part * (s - 1) >= K) continue;         // (a part would be empty)
+      const long long time = (s * edge_tiles(t, M, N) + CHIP_CUS - 1) / CHIP_CUS * tile_time(t, part, false) + 5000 + 8LL * s * M * N / 5000;
+      if (time < best_time) { best = {i, s, part}; best_time = time; }
+    }
+  }
+  return best;
+}
+// what it takes
+inline long long edge_split_time(int M, int N, int K) {
+  const EdgeSplit p = pick_edge_split(M, N, K);
+  const TileCost& t = TILES_DENSE[p.tile];
+  return (p.splits * edge_tiles(t, M, N) + CHIP_CUS - 1) / CHIP_CUS * tile_time(t, p.part, false) + (p.splits > 1 ? 5000 + 8LL * p.splits * M * N / 5000 : 0);
+}
+
 // Two launches of n 256 x 256 tiles each (a weight gradient; with the split the dense and the sparse tiles of one) that could be one go out
 // one after the other where sharing saves no round of the chip and the reduction is long: the other's operands then no longer share the
 // L2 with the first's for as long as the launches overlap, and the gap between them is short beside them.  Measured, together -> apart:

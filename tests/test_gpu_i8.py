@@ -48,7 +48,7 @@ def test_codes_and_scales(T, K):
 @pytest.mark.gpu
 @pytest.mark.parametrize("T,K,N", [(1, 16, 8), (1, 2048, 520), (3, 80, 24), (17, 144, 264), (64, 1088, 1000), (65, 208, 256), (333, 1088, 4168), (1000, 640, 3000),
                                    (1500, 512, 2048), (2100, 1552, 5000), (4099, 272, 4104), (2, 16400, 16),
-                                   (16, 1040, 40), (1, 16992, 264), (29, 8208, 200), (32, 8192, 16392), (5, 4112, 32768)])
+                                   (16, 1040, 40), (1, 16992, 264), (29, 8208, 200), (32, 8192, 16392), (5, 4112, 32768), (100, 16384, 512), (130, 8992, 136), (300, 6000, 1000)])
 def test_product(T, K, N):
     X, W = _normal((T, K), T), _normal((K, N), N, K ** -0.5)
     W[:, N - 1] = 0
@@ -176,7 +176,7 @@ def test_refusals_without_a_gpu():
     assert L.quantise_i8(a, 1, 8, a, a, None) == -2 and L.quantise_i8(a, -1, 16, a, a, None) == -2 and L.quantise_i8(None, 1, 16, a, a, None) == -1
     assert L.quantise_i8(a, 1, 16, a + 4, a, None) == -3 and L.quantise_i8(None, 0, 16, None, None, None) == 0
     assert L.matmul_i8(a, a, 1, a, 16, 12, a, None) == -2 and L.matmul_i8(a, a, 1, None, 16, 8, a, None) == -1 and L.matmul_i8(a, a, 1, a, 16, 8, a + 2, None) == -3
-    assert L.linear_i8_scratch(3, 16) == 48 + 16 and L.linear_i8_scratch(-1, 16) == -1 and L.linear_i8_scratch(1, 20) == -1
+    assert L.linear_i8_scratch(3, 16, 8) == 48 + 16 and L.linear_i8_scratch(-1, 16, 8) == -1 and L.linear_i8_scratch(1, 20, 8) == -1 and L.linear_i8_scratch(1, 16, 4) == -1
     assert L.linear_i8(a, 1, a, 20, 8, a, a, None) == -2 and L.linear_i8(a, 1, a, 16, 8, a, None, None) == -1 and L.linear_i8(a, 1, a, 16, 8, a, a + 1, None) == -3
     h = ctypes.c_void_p()
     assert L.gated_i8_ctx_create(ctypes.byref(h), 8, 64, 64, 3) == -4 and L.gated_i8_ctx_create(ctypes.byref(h), 8, 60, 64, 0) == -2
