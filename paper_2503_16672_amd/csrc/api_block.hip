@@ -168,7 +168,7 @@ int quantise_i8(const void* X, int64_t T, int64_t K, void* codes, float* scales,
   if (T == 0) return FFN24_OK;
   if (!X || !codes || !scales) return FFN24_ERR_NULL;
   if (misaligned(X, codes, scales)) return FFN24_ERR_ALIGN;
-  return done(launch_quantise_i8(X, (int)T, (int)K, codes, scales, nullptr, static_cast<hipStream_t>(stream)));
+  return done(launch_quantise_i8(X, (int)T, (int)K, false, codes, scales, nullptr, static_cast<hipStream_t>(stream)));
 }
 
 int matmul_i8(const void* codes, const float* scales, int64_t T, const void* weight, int64_t K, int64_t N, void* Y, void* stream) {
@@ -176,7 +176,7 @@ int matmul_i8(const void* codes, const float* scales, int64_t T, const void* wei
   if (T == 0) return FFN24_OK;
   if (!codes || !scales || !weight || !Y) return FFN24_ERR_NULL;
   if (misaligned(codes, scales, weight, Y)) return FFN24_ERR_ALIGN;
-  return done(launch_matmul_i8(codes, scales, (int)T, i8_layout(weight, (int)K, (int)N), Y, Scratch{}, static_cast<hipStream_t>(stream)));
+  return done(launch_matmul_i8(codes, false, scales, (int)T, i8_layout(weight, (int)K, (int)N), Y, Scratch{}, static_cast<hipStream_t>(stream)));
 }
 
 int64_t linear_i8_scratch(int64_t T, int64_t K, int64_t N) {
@@ -191,9 +191,9 @@ int linear_i8(const void* X, int64_t T, const void* weight, int64_t K, int64_t N
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (few_i8_fuses((int)T, (int)K)) return done(launch_few_linear_i8(X, (int)T, i8_layout(weight, (int)K, (int)N), Y, s));
   float* sx = reinterpret_cast<float*>(static_cast<char*>(scratch) + T * K);
-  if (launch_quantise_i8(X, (int)T, (int)K, scratch, sx, nullptr, s)) return FFN24_ERR_HIP;
+  if (launch_quantise_i8(X, (int)T, (int)K, false, scratch, sx, nullptr, s)) return FFN24_ERR_HIP;
   const Scratch rest{static_cast<char*>(scratch) + T * K + up16(4 * T), matmul_i8_scratch((int)T, (int)K, (int)N)};
-  return done(launch_matmul_i8(scratch, sx, (int)T, i8_layout(weight, (int)K, (int)N), Y, rest, s));
+  return done(launch_matmul_i8(scratch, false, sx, (int)T, i8_layout(weight, (int)K, (int)N), Y, rest, s));
 }
 
 int gated_i8_ctx_create(gated_i8_ctx** out, int64_t T, int64_t D, int64_t F, ffn24_gate gate) {
@@ -203,12 +203,12 @@ int gated_i8_ctx_create(gated_i8_ctx** out, int64_t T, int64_t D, int64_t F, ffn
   gated_i8_ctx* c = new (std::nothrow) gated_i8_ctx();
   if (!c) return FFN24_ERR_HIP;
   c->T = T; c->D = D; c->F = F; c->gate = coefficients(gate);
-  const size_t td = (size_t)T * (size_t)D, tf = (size_t)T * (size_t)F, t4 = 4 * (size_t)T, few = few_i8_tops((int)T, (int)F), tops = few > t4 ? few : t4;
+  const size_t tf = (size_t)T * (size_t)F, t4 = 4 * (size_t)T, few = few_i8_tops((int)T, (int)F), tops = few > t4 ? few : t4;
   c->scratch.bytes = gated_i8_scratch((int)T, (int)D, (int)F);
   const bool ok = hipGetDevice(&c->device) == hipSuccess && (!c->scratch.bytes || hipMalloc(&c->scratch.p, c->scratch.bytes) == hipSuccess) &&
                   hipMalloc(&c->Wgu, (size_t)i8_weight_size(D, 2 * F)) == hipSuccess &&
-                  hipMalloc(&c->Wd, (size_t)i8_weight_size(F, D)) == hipSuccess && hipMalloc(&c->X8, td) == hipSuccess && hipMalloc(&c->H, 2 * tf) == hipSuccess &&
-                  hipMalloc(&c->H8, tf) == hipSuccess && hipMalloc(reinterpret_cast<void**>(&c->sx), t4) == hipSuccess &&
+                  hipMalloc(&c->Wd, (size_t)i8_weight_size(F, D)) == hipSuccess && hipMalloc(&c->X8, (size_t)i8_panel_size(T, D)) == hipSuccess && hipMalloc(&c->H, 2 * tf) == hipSuccess &&
+                  hipMalloc(&c->H8, (size_t)i8_panel_size(T, F)) == hipSuccess && hipMalloc(reinterpret_cast<void**>(&c->sx), t4) == hipSuccess &&
                   hipMalloc(reinterpret_cast<void**>(&c->sh), t4) == hipSuccess && hipMalloc(reinterpret_cast<void**>(&c->tops), tops) == hipSuccess;
   if (!ok) {
     (void)hipGetLastError();
@@ -251,10 +251,10 @@ int gated_i8_fwd(gated_i8_ctx* c, const void* X, int64_t T, void* Y, void* strea
   const int t = (int)T, D = (int)c->D, F = (int)c->F;
   if (few_gated_i8_tokens(t, D, F))
     return done(launch_few_gated_i8(X, t, i8_layout(c->Wgu, D, 2 * F), i8_layout(c->Wd, F, D), c->gate.c1, c->gate.c3, c->X8, c->sx, c->H, c->tops, c->H8, c->sh, Y, s));
-  if (launch_quantise_i8(X, t, D, c->X8, c->sx, c->tops, s)) return FFN24_ERR_HIP;
+  if (launch_quantise_i8(X, t, D, true, c->X8, c->sx, c->tops, s)) return FFN24_ERR_HIP;
   if (launch_gated_up_i8(c->X8, c->sx, t, i8_layout(c->Wgu, D, 2 * F), c->gate.c1, c->gate.c3, c->H, c->tops, s)) return FFN24_ERR_HIP;
   if (launch_quantise_i8_given(c->H, c->tops, t, F, c->H8, c->sh, s)) return FFN24_ERR_HIP;
-  return done(launch_matmul_i8(c->H8, c->sh, t, i8_layout(c->Wd, F, D), Y, c->scratch, s));
+  return done(launch_matmul_i8(c->H8, true, c->sh, t, i8_layout(c->Wd, F, D), Y, c->scratch, s));
 }
 
 }  // extern "C"

@@ -198,7 +198,7 @@ __device__ __forceinline__ int swz8_big(int i) { return (i & 2) | (((i >> 3) & 1
 // 16-byte reads then (221 against 256 B/clk in a loop of nothing else; 32 without the swizzle).  Inside the 256 x 256 loops, beside the DMA's writes, the counters
 // see conflicts in 0-1 % of the LDS-active cycles with B k-major, but in a third of them with A k-major (panels: none), T = F = 16384, D 4096.
 constexpr int TR_A = 1, TR_B = 2;
-// Operands of any extent (dense; row-major or k-major, A also in panel form, whose blocks are whole): rows, columns and k's beyond a tensor's end come as
+// Operands of any extent (dense; row-major or k-major, or in panel form, whose blocks are whole): rows, columns and k's beyond a tensor's end come as
 // zeros.  The buffer descriptor of a stage starts where the stage does and ends with the tensor, so the hardware's bounds check makes them and no offset passes 32
 // bits, however large the tensor: scalar arithmetic, once a stage.  What a k-major row has beyond the tile's columns, and a row-major row beyond K
 // (never read: K is a multiple of the stage there), lands in results that are not stored.
@@ -287,17 +287,18 @@ struct Dma {
     const int lane = tid & 63;
     wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const bool panel = g.a_panel != 0;
-    const int ma = MI == 4 ? 0 : m0 & 255, mb = m0 - ma;
+    const bool bp = g.b_panel != 0;
+    const int ma = MI == 4 ? 0 : m0 & 255, mb = m0 - ma, n_in = NI == 4 || !bp ? 0 : n0 & 255;
     const uint32_t a_pitch = panel ? 64u : (uint32_t)g.a_pitch, b_pitch = (uint32_t)g.b_pitch;
     // the first byte of the block, and one behind the tensor's last
     const int64_t a0 = TRA ? (int64_t)m0 * (GATE ? 1 : G::ESIZE) : panel ? (int64_t)mb * g.a_pitch + ma * 64 : (int64_t)m0 * a_pitch;
-    const int64_t b0 = TRB ? (int64_t)n0 * G::ESIZE : (int64_t)n0 * b_pitch;
+    const int64_t b0 = TRB ? (int64_t)n0 * G::ESIZE : (int64_t)(n0 - n_in) * b_pitch;
     ea = static_cast<const char*>(g.A) + a0;
     eb = static_cast<const char*>(g.B) + b0;
     na = !TRA && panel ? (int64_t)0x7FFFFFFF << 16 : (int64_t)g.a_rows * g.a_pitch - a0;
-    nb = (int64_t)g.b_rows * g.b_pitch - b0;
+    nb = !TRB && bp ? (int64_t)0x7FFFFFFF << 16 : (int64_t)g.b_rows * g.b_pitch - b0;
     a_stage = TRA ? (uint32_t)G::BK * a_pitch : panel ? 256u * (uint32_t)G::A_ROW : (uint32_t)G::A_ROW;
-    b_stage = TRB ? (uint32_t)G::BK * b_pitch : (uint32_t)G::B_ROW;
+    b_stage = TRB ? (uint32_t)G::BK * b_pitch : bp ? 256u * (uint32_t)G::B_ROW : (uint32_t)G::B_ROW;
 #pragma unroll
     for (int j = 0; j < NA; j++) {
       if constexpr (TRA) { va[j] = k_major<MI, GATE>(NA * wave + j, lane, a_pitch, [](int k) { return tr_swz_a<MI, NI>(k); }, g.gate); continue; }
@@ -310,7 +311,8 @@ struct Dma {
       if constexpr (TRB) { vb[j] = k_major<NI>(NVB * wave + j, lane, b_pitch, [](int k) { return tr_swz_b<MI, NI>(k); }); continue; }
       const int p = G::B_ROW == 128 ? 8 * (NVB * wave + j) + (lane >> 3) : 16 * (NVB * wave + j) + (lane >> 2);
       const int c = G::B_ROW == 128 ? (lane & 7) ^ (G::BIG ? swz8_big(big_n_col<SPARSE>(p)) : swz8(p)) : (lane & 3) ^ (G::BIG ? swz4_big<false>(big_n_col<SPARSE>(p)) : swz4(p));
-      vb[j] = (uint32_t)(G::BIG ? big_unperm_n<SPARSE>(p) : unperm_n<NI>(p)) * b_pitch + c * 16;
+      const int n = G::BIG ? big_unperm_n<SPARSE>(p) : unperm_n<NI>(p);
+      vb[j] = bp ? (uint32_t)(c >> 2) * (256u * 64u) + (uint32_t)b_panel_pos(n_in + n) * 64u + (c & 3) * 16 : (uint32_t)n * b_pitch + c * 16;
     }
   }
 

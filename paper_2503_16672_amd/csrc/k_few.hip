@@ -400,7 +400,7 @@ int launch_few_gated_i8(const void* X, int T, const I8Layout& wgu, const I8Layou
                         void* Y, hipStream_t s) {
   const bool fused = few_i8_fuses(T, wgu.K);
   if (!fused)
-    if (int rc = launch_quantise_i8(X, T, wgu.K, X8, sx, nullptr, s)) return rc;
+    if (int rc = launch_quantise_i8(X, T, wgu.K, false, X8, sx, nullptr, s)) return rc;
   FewI8Args up = few_i8_args(fused ? X : X8, sx, T, wgu, H);
   up.gate = Gate{c1, c3};
   up.tops_out = tops;

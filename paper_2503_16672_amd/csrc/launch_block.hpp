@@ -33,11 +33,13 @@ struct I8Layout { const char* panels; const float* scales; int K, N; };   // wei
 int64_t i8_weight_size(int64_t K, int64_t N);
 I8Layout i8_layout(const void* p, int K, int N);
 int launch_i8_weight(const void* W, int K, int N, bool halves, void* out, hipStream_t s);
-int launch_quantise_i8(const void* X, int T, int K, void* codes, float* scales, uint32_t* zero, hipStream_t s);
+int64_t i8_panel_size(int64_t T, int64_t K);     // bytes of codes in panel form
+int launch_quantise_i8(const void* X, int T, int K, bool panel_form, void* codes, float* scales, uint32_t* zero, hipStream_t s);
 int launch_quantise_i8_given(const void* H, const uint32_t* tops, int T, int F, void* codes, float* scales, hipStream_t s);
 size_t matmul_i8_scratch(int T, int K, int N);
 size_t gated_i8_scratch(int T, int D, int F);    // for any token count up to T
-int launch_matmul_i8(const void* codes, const float* sx, int T, const I8Layout& w, void* Y, const Scratch& scratch, hipStream_t s);
+int launch_matmul_i8(const void* codes, bool panel_form, const float* sx, int T, const I8Layout& w, void* Y, const Scratch& scratch, hipStream_t s);
+// (codes in panel form)
 int launch_gated_up_i8(const void* codes, const float* sx, int T, const I8Layout& w, float c1, float c3, void* H, uint32_t* rowmax, hipStream_t s);
 
 // k_few.hip: few tokens, where the weights are what counts
