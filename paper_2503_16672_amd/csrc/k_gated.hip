@@ -138,7 +138,15 @@ int launch_gated_down(const void* H, const void* Wd, int T, int D, int F, void* 
 }
 
 int launch_gated_dgate(const void* dY, const void* Wd, const void* GU, const void* GUx, int T, int D, int F, float c1, float c3, void* dGU, hipStream_t s) {
-  return launch_edge<EpiDGate, 0>(args(Wd, F, D, dY, T, D, F, T, D), EpiDGate::Args{static_cast<const __bf16*>(GU), static_cast<const uint8_t*>(GUx), static_cast<__bf16*>(dGU), F, T, Gate{c1, c3}}, s);
+  const GemmArgs g = args(Wd, F, D, dY, T, D, F, T, D);
+  const EpiDGate::Args e{static_cast<const __bf16*>(GU), static_cast<const uint8_t*>(GUx), static_cast<__bf16*>(dGU), F, T, Gate{c1, c3}};
+  // (no 128 x 64: 64 x 64 was faster wherever the rule took it, us, T D F: 128 4096 12288 39.3, 27.8; 256 4096 12288 67.8, 54.8; 1000 1088 2944 20.2, 18.3)
+  switch (pick_edge_tile(F, T, D)) {
+    case 0: return launch_edge_tile<EpiDGate, TR_EDGE, 4, 4>(g, e, s);
+    case 1: return launch_edge_tile<EpiDGate, TR_EDGE, 4, 2>(g, e, s);
+    case 2: return launch_edge_tile<EpiDGate, TR_EDGE, 2, 2>(g, e, s);
+    default: return launch_edge_tile<EpiDGate, TR_EDGE, 1, 1>(g, e, s);
+  }
 }
 
 int launch_gated_grads(const void* X, const void* dY, const void* H, const void* dGU, const void* Wgu, bool panels, int T, int D, int F, void* dX, void* dWgu, void* dWd,
