@@ -97,8 +97,9 @@ size_t gated_scratch(int T, int D, int F, bool training) {
   }
   return most;
 }
-// The tile of dX and the weight gradients in one launch, 0: apart.  Together they take all their tiles over the CUs and one tile of the shorter kind more, or the dX tiles'
-// own rounds if that is longer.
+// The tile of dX and the weight gradients in one launch, 0: apart (dX then may be split).  Together they take all their tiles over the CUs and one tile of the shorter kind
+// more, or the dX tiles' own rounds if that is longer, which beside other tiles on their CUs take a third more than alone.  Whole steps, together / apart, us (T D F):
+// 500 4096 8192 425, 449; 2000 1024 2816 155, 172; 1500 2048 5440 361, 378; 300 512 1536 33.0, 35.9; the other way 163 5312 14464 637, 554; 333 2816 8896 324, 238; 700 2048 8192 308, 298.
 int pick_grads_tile(int T, int D, int F, int K) {
   const int tw = pick_edge_tile(D, 2 * F, K, F, D);
   const auto rounds = [](long long n) { return (n + CHIP_CUS - 1) / CHIP_CUS; };
@@ -108,7 +109,7 @@ int pick_grads_tile(int T, int D, int F, int K) {
   for (int i = 1; i < NUM_TILES; i++) {
     const TileCost& t = TILES_DENSE[i];
     const long long nx = edge_tiles(t, D, T), one_x = tile_time(t, 2 * F, false), one_w = tile_time(t, K, false);
-    const long long all = (nx * one_x + weights(t) * one_w) / CHIP_CUS + one_w, time = all > rounds(nx) * one_x ? all : rounds(nx) * one_x;
+    const long long all = (nx * one_x + weights(t) * one_w) / CHIP_CUS + one_w, longest = rounds(nx) * one_x * 27 / 20, time = all > longest ? all : longest;
     if (time < best_time) { best = i; best_time = time; }
   }
   return best;
