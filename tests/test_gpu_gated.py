@@ -2,9 +2,11 @@
 
 Tolerances.  Rounding to bf16 moves a value by at most u = 2^-8 of it, u / sqrt(3) in the mean square if the error is uniform.  With independent errors an output's
 deviation is sigma = u / sqrt(3) sqrt(sum over its products of (number of roundings) x product^2 + output^2): H, dU and dG
-carry one rounding each.  An element may be off by 7 sigma, an output's norm by 1.1 of sigma's; fp32 sums and the approximate
-reciprocal and exponential (2^-22) vanish beside that.  G, cut to 24 bits for the backward, is off by at most 2^-15 of it, and the gate's slope by that times
-its derivative: this vanishes too, but for the elements whose slope is itself near its zero (G = -0.75 or -1.28) where no other token adds to them."""
+carry one rounding each.  An element may be off by 7 sigma, an output's norm by 1.1 of sigma's; the approximate
+reciprocal and exponential (2^-22) vanish beside that.  Two things vanish for most elements only, and have terms of their own:
+G, U and dH are sums of K products in fp32: the partial sums have k / K of the variance S^2 = sum of the products' squares, each addition rounds by 2^-24 of its
+partial sum (/ sqrt(3)), together 2^-24 S sqrt(K / 6), which shows where G is next to 0 and a(G) with it;
+and G, cut to 24 bits for the backward, is off by 2^-15 of it at most, which shows where the gate's slope is next to its zero (G = -0.75 or -1.28)."""
 import numpy as np
 import pytest
 import torch
@@ -47,12 +49,18 @@ def reference(X, Wgu, Wd, dY, act):
     dH = dY @ Wd.T
     dG, dU = dH * Up * slope, dH * a
     dGU = torch.cat((dG, dU), 1)
-    var = dGU ** 2
-    var[:, :F] += (dH * Up * _bend(G, act) * G * 2.0 ** -15 / U) ** 2
+    # deviations in units of that of one rounding, U / sqrt(3)
+    summed = lambda A, B: (2.0 ** -24 / U * 3 ** 0.5) * torch.sqrt((A ** 2) @ (B ** 2) * (A.shape[1] / 6))
+    eGU, eH = summed(X, Wgu), summed(dY, Wd.T)
+    eG, eU = eGU[:, :F], eGU[:, F:]
+    kept = eG ** 2 + (G * 2.0 ** -15 / U) ** 2
+    var = dGU ** 2 + torch.cat(((dH * Up * _bend(G, act)) ** 2 * kept + (dH * slope * eU) ** 2 + (Up * slope * eH) ** 2,
+                                (dH * slope) ** 2 * kept + (a * eH) ** 2), 1)
+    varH = H ** 2 + (Up * slope * eG) ** 2 + (a * eU) ** 2
     sig = lambda prod, out: U / 3 ** 0.5 * torch.sqrt(prod + out ** 2)
     dX, dWgu, dWd = dGU @ Wgu.T, X.T @ dGU, H.T @ dY
-    return {"Y": (Y, sig(H ** 2 @ Wd ** 2, Y)), "dX": (dX, sig(var @ (Wgu ** 2).T, dX)), "dWgu": (dWgu, sig((X ** 2).T @ var, dWgu)),
-            "dWd": (dWd, sig((H ** 2).T @ dY ** 2, dWd))}
+    return {"Y": (Y, sig(varH @ Wd ** 2, Y)), "dX": (dX, sig(var @ (Wgu ** 2).T, dX)), "dWgu": (dWgu, sig((X ** 2).T @ var, dWgu)),
+            "dWd": (dWd, sig(varH.T @ dY ** 2, dWd))}
 
 
 def check(got, ref, what):
