@@ -86,24 +86,33 @@ __global__ void __launch_bounds__(256) i8_weight_clear_kernel(uint32_t* tops, in
   const int i = blockIdx.x * 256 + threadIdx.x;
   if (i < n) tops[i] = 0u;
 }
-// largest magnitude of each column, 8 columns a work item, 64 rows a workgroup of 32 x 8; tops in panel order
+// largest magnitude of each column over TOP_ROWS rows a workgroup of 32 x 8, 8 columns a work item; tops in panel order.  One atomic a column and workgroup: with one a
+// column and 8 rows 4096 x 32768 took 660 us.
+constexpr int TOP_ROWS = 256;
 __global__ void __launch_bounds__(256) i8_weight_top_kernel(const uint16_t* __restrict__ W, int K, int N, int F, uint32_t* tops) {
-  const int n = 8 * (blockIdx.x * 32 + (threadIdx.x & 31)), k0 = blockIdx.y * 64 + (threadIdx.x >> 5);
-  if (n >= N) return;
+  __shared__ __attribute__((aligned(16))) uint32_t part[8][256];
+  const int tid = threadIdx.x, n0 = blockIdx.x * 256, n = n0 + 8 * (tid & 31), k0 = blockIdx.y * TOP_ROWS + (tid >> 5);
   uint32_t top[8] = {};
+  if (n < N) {
+    const uint16_t* w = W + (size_t)k0 * N + n;
+#pragma unroll 8
+    for (int k = k0; k < min(K, (int)blockIdx.y * TOP_ROWS + TOP_ROWS); k += 8, w += 8 * (size_t)N) {
+      const u32x4 v = *reinterpret_cast<const u32x4*>(w);
 #pragma unroll
-  for (int i = 0; i < 8; i++) {
-    const int k = k0 + 8 * i;
-    if (k >= K) break;
-    const u32x4 w = *reinterpret_cast<const u32x4*>(W + (size_t)k * N + n);
-#pragma unroll
-    for (int j = 0; j < 4; j++) {
-      top[2 * j] = max(top[2 * j], w[j] << 16 & 0x7FFF0000u);
-      top[2 * j + 1] = max(top[2 * j + 1], w[j] & 0x7FFF0000u);
+      for (int j = 0; j < 4; j++) {
+        top[2 * j] = max(top[2 * j], v[j] << 16 & 0x7FFF0000u);
+        top[2 * j + 1] = max(top[2 * j + 1], v[j] & 0x7FFF0000u);
+      }
     }
   }
+  u32x4* mine = reinterpret_cast<u32x4*>(&part[tid >> 5][8 * (tid & 31)]);
+  mine[0] = u32x4{top[0], top[1], top[2], top[3]};
+  mine[1] = u32x4{top[4], top[5], top[6], top[7]};
+  __syncthreads();
+  uint32_t most = part[0][tid];
 #pragma unroll
-  for (int j = 0; j < 8; j++) atomicMax(tops + channel_row(n + j, F), top[j]);
+  for (int i = 1; i < 8; i++) most = max(most, part[i][tid]);
+  if (n0 + tid < N) atomicMax(tops + channel_row(n0 + tid, F), most);
 }
 // 64 panel rows x 64 k a workgroup: read along the channels, through LDS, out as one run of 64 pieces
 __global__ void __launch_bounds__(256) i8_weight_codes_kernel(const uint16_t* __restrict__ W, int K, int N, int F, int panels, const uint32_t* __restrict__ tops,
@@ -153,7 +162,8 @@ int launch_i8_weight(const void* W, int K, int N, bool halves, void* out, hipStr
   float* scales = reinterpret_cast<float*>(codes + (size_t)rows * panels * 64);
   uint32_t* tops = reinterpret_cast<uint32_t*>(scales + rows);
   hipLaunchKernelGGL(i8_weight_clear_kernel, dim3((unsigned)(rows / 256)), dim3(256), 0, s, tops, rows);
-  hipLaunchKernelGGL(i8_weight_top_kernel, dim3((unsigned)((N + 255) / 256), (unsigned)((K + 63) / 64)), dim3(256), 0, s, static_cast<const uint16_t*>(W), K, N, F, tops);
+  hipLaunchKernelGGL(i8_weight_top_kernel, dim3((unsigned)((N + 255) / 256), (unsigned)((K + TOP_ROWS - 1) / TOP_ROWS)), dim3(256), 0, s, static_cast<const uint16_t*>(W), K,
+                     N, F, tops);
   hipLaunchKernelGGL(i8_weight_codes_kernel, dim3((unsigned)(rows / 64), (unsigned)panels), dim3(256), 0, s, static_cast<const uint16_t*>(W), K, N, F, panels, tops, codes,
                      scales);
   return (int)hipGetLastError();
