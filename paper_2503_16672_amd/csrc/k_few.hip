@@ -18,7 +18,6 @@ namespace {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int FEW_TOKENS = 64;
 constexpr int I8_FUSE_BYTES = 17 * 1024;   // of codes that a workgroup makes itself
 constexpr int RED = 17;                     // pitch of the sums' image: [channel][16 tokens]
 
@@ -365,10 +364,6 @@ FewI8Args few_i8_args(const void* X, const float* sx, int T, const I8Layout& w, 
 }
 }  // namespace
 
-// Few tokens: where these kernels are faster than the GEMM core's smallest tiles.  Both, us (T D F): 16 512 1536 12.1, 12.3; 32 512 1536 16.2, 12.4; 32 256 768 12.8,
-// 8.6; 17 1024 4096 18.6, 22.3; 32 1024 4096 20.6, 22.4; 32 2048 5440 30.8, 45.2; 48 512 1536 17.3, 12.4; 64 1024 4096 27.6, 22.7; 37 2048 5440 32.5, 46.1; 64 4096 16384 94, 146.
-bool few_tokens(int T, int D, int F) { return T <= 16 || (T <= FEW_TOKENS && (long long)D * F >= (T <= 32 ? 1 << 21 : 1 << 23)); }
-
 size_t few_gated_scratch(int T, int D, int F) {
   size_t most = 0;
   for (int t = 1; t <= (T < FEW_TOKENS ? T : FEW_TOKENS); t++) {
@@ -385,12 +380,6 @@ int launch_few_gated_down(const void* H, const void* Wd, int T, int D, int F, vo
   return launch_few_bf16<false>(H, Wd, T, F, D, Gate{}, Y, parts, s);
 }
 
-// Few tokens, against the GEMM core's smallest tiles, us.  One product (T K N): 1 2048 8192 8.9, 11.0; 16 4096 4096 11.8, 12.2; 1 8192 8192 14.5, 24.9; 32 4096 16384 20.8, 18.4; 24 8192 8192
-// 24.8, 25.5; 32 4096 4096 12.3, 12.2; 64 4096 16384 30.9, 19.4.  Gated block (T D F): 1 4096 16384 39.1, 69.5; 16 4096 16384 50, 70; 32 4096 16384 60, 71; 24 2048 8192 28.4, 33.5; 20
-// 1024 2816 21.9, 19.3; 32 512 1536 20.0, 15.9; 64 4096 16384 87, 78.
-constexpr int FEW_I8_TOKENS = 32;
-bool few_i8_tokens(int T, int K) { return T <= 16 || (T <= FEW_I8_TOKENS && K >= 8192); }
-bool few_gated_i8_tokens(int T, int D, int F) { return T <= 16 || (T <= FEW_I8_TOKENS && (long long)D * F >= 1 << 23); }
 bool few_i8_fuses(int T, int K) { return T <= 16 && T * (up_to(K, 64) + 16) <= I8_FUSE_BYTES; }
 size_t few_i8_tops(int T, int F) { return 4 * (size_t)(T < FEW_I8_TOKENS ? T : FEW_I8_TOKENS) * (size_t)((2 * F + 15) / 16); }
 

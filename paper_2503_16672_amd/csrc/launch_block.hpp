@@ -2,6 +2,7 @@
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include "tile_rule.hpp"
 
 namespace ffn24 {
 
@@ -42,14 +43,11 @@ int launch_matmul_i8(const void* codes, bool panel_form, const float* sx, int T,
 // (codes in panel form)
 int launch_gated_up_i8(const void* codes, const float* sx, int T, const I8Layout& w, float c1, float c3, void* H, uint32_t* rowmax, hipStream_t s);
 
-// k_few.hip: few tokens, where the weights are what counts
-bool few_tokens(int T, int D, int F);
+// k_few.hip: few tokens, where the weights are what counts (few_tokens, few_i8_tokens, few_gated_i8_tokens)
 size_t few_gated_scratch(int T, int D, int F);   // bytes of `parts` for any token count up to T
 int launch_few_gated_up(const void* X, const void* Wgu, int T, int D, int F, float c1, float c3, void* H, float* parts, hipStream_t s);
 int launch_few_gated_down(const void* H, const void* Wd, int T, int D, int F, void* Y, float* parts, hipStream_t s);
 
-bool few_i8_tokens(int T, int K);
-bool few_gated_i8_tokens(int T, int D, int F);
 bool few_i8_fuses(int T, int K);                 // whether the product's workgroups quantise the tokens themselves
 size_t few_i8_tops(int T, int F);                // bytes of the gated block's `tops`
 int launch_few_linear_i8(const void* X, int T, const I8Layout& w, void* Y, hipStream_t s);   // few_i8_fuses

@@ -35,10 +35,10 @@ __global__ void __launch_bounds__(GEMM_THREADS, (Geo<false, false, MI, NI>::PER_
   const int split = (int)blockIdx.x / tiles, k0 = split * part;
   constexpr bool TRA = (TR & TR_A) != 0;
   g.K = min(part, g.K - k0);
-  // (K-contiguous: a row's part starts 2 k0 bytes on; rows beyond the last one still start behind the tensor's extent)
+  // (K-contiguous: a row's part starts 2 k0 bytes on; rows beyond the last one still start behind the tensor's extent.  Panel form: k0 / 32 panels of 256 rows x 64 bytes on)
   g.A = static_cast<const char*>(g.A) + (TRA ? (size_t)k0 * g.a_pitch : g.a_panel ? (size_t)k0 * (2 * 256) : (size_t)k0 * 2);
   if constexpr (TRA) g.a_rows -= k0;
-  g.B = static_cast<const char*>(g.B) + (size_t)k0 * 2;
+  g.B = static_cast<const char*>(g.B) + (g.b_panel ? (size_t)k0 * (2 * 256) : (size_t)k0 * 2);
   ea.parts += (size_t)split * ea.M * ea.N;
   gemm_tile<false, EdgePart, false, 0, MI, NI, TR>(g, ea, smem, (int)blockIdx.x - split * tiles);
 }

@@ -101,6 +101,18 @@ inline long long edge_split_time(int M, int N, int K) {
   return (p.splits * edge_tiles(t, M, N) + CHIP_CUS - 1) / CHIP_CUS * tile_time(t, p.part, false) + (p.splits > 1 ? 5000 + 8LL * p.splits * M * N / 5000 : 0);
 }
 
+// Few tokens (k_few.hip): where its kernels are faster than the GEMM core's smallest tiles.  Both, us (T D F): 16 512 1536 12.1, 12.3; 32 512 1536 16.2, 12.4; 32 256 768 12.8,
+// 8.6; 17 1024 4096 18.6, 22.3; 32 1024 4096 20.6, 22.4; 32 2048 5440 30.8, 45.2; 48 512 1536 17.3, 12.4; 64 1024 4096 27.6, 22.7; 37 2048 5440 32.5, 46.1; 64 4096 16384 94, 146.
+constexpr int FEW_TOKENS = 64;
+inline bool few_tokens(int T, int D, int F) { return T <= 16 || (T <= FEW_TOKENS && (long long)D * F >= (T <= 32 ? 1 << 21 : 1 << 23)); }
+
+// The same for 8-bit integers, us.  One product (T K N): 1 2048 8192 8.9, 11.0; 16 4096 4096 11.8, 12.2; 1 8192 8192 14.5, 24.9; 32 4096 16384 20.8, 18.4; 24 8192 8192
+// 24.8, 25.5; 32 4096 4096 12.3, 12.2; 64 4096 16384 30.9, 19.4.  Gated block (T D F): 1 4096 16384 39.1, 69.5; 16 4096 16384 50, 70; 32 4096 16384 60, 71; 24 2048 8192 28.4, 33.5; 20
+// 1024 2816 21.9, 19.3; 32 512 1536 20.0, 15.9; 64 4096 16384 87, 78.
+constexpr int FEW_I8_TOKENS = 32;
+inline bool few_i8_tokens(int T, int K) { return T <= 16 || (T <= FEW_I8_TOKENS && K >= 8192); }
+inline bool few_gated_i8_tokens(int T, int D, int F) { return T <= 16 || (T <= FEW_I8_TOKENS && (long long)D * F >= 1 << 23); }
+
 // Two launches of n 256 x 256 tiles each (a weight gradient; with the split the dense and the sparse tiles of one) that could be one go out
 // one after the other where sharing saves no round of the chip and the reduction is long: the other's operands then no longer share the
 // L2 with the first's for as long as the launches overlap, and the gap between them is short beside them.  Measured, together -> apart:
