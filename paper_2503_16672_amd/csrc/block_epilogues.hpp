@@ -135,16 +135,20 @@ struct EdgeRowMajor {
 };
 
 // The gate's activation a(x) = x s, s = sigmoid(c1 x + c3 x^3): SiLU with (1, 0), GELU in its tanh form with (2 sqrt(2 / pi), 0.044715 times that).
-// sigmoid(p) = 1 / (1 + 2^(-p log2 e)); 2^x is infinite for p < -88 and s then 0.  In the slope s + x s (1 - s) (c1 + 3 c3 x^2) x is held to +-1e4,
-// where s (1 - s) is 0 long since and the factor stays finite.
+// sigmoid(p) = 1 / (1 + 2^(-p log2 e)); 2^x is infinite for p < -88 and s then 0.  In p, and in the slope s + x s (1 - s) (c1 + 3 c3 x^2), x is held to +-1e4,
+// where s is 0 or 1 long since and x^2 stays finite (SiLU: 0 times infinity otherwise, from 1.8e19 on).
 struct Gate { float c1, c3; };
 __device__ __forceinline__ float sigmoid(float p) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * p)); }
-__device__ __forceinline__ float gate_act(const Gate& g, float x) { return x * sigmoid(x * (g.c1 + g.c3 * (x * x))); }
+__device__ __forceinline__ float gate_hold(float x) { return fminf(fmaxf(x, -1e4f), 1e4f); }   // (takes NaN for a number)
+__device__ __forceinline__ float gate_act(const Gate& g, float x) {
+  const float y = gate_hold(x);
+  return x * sigmoid(y * (g.c1 + g.c3 * (y * y)));
+}
 __device__ __forceinline__ void gate_act_slope(const Gate& g, float x, float& a, float& slope) {
-  const float y = fminf(fmaxf(x, -1e4f), 1e4f), y2 = y * y, s = sigmoid(y * (g.c1 + g.c3 * y2));
+  const float y = gate_hold(x), y2 = y * y, s = sigmoid(y * (g.c1 + g.c3 * y2));
   a = x * s;
   slope = s + y * (s - s * s) * (g.c1 + 3.f * g.c3 * y2);
-  if (x != x) slope = x;                                      // (the clamp takes NaN for a number)
+  if (x != x) slope = x;                                      // (y is a number)
 }
 
 // What the backward needs of G and U is kept in 24 bits of the fp32 value: its upper 16 as a row-major [T][2 F], its next 8 as bytes [T][F / 8][16], 8 of G and
