@@ -1,7 +1,7 @@
 """ctypes binding of include/ffn24_block.h: layer norm, the gated feed-forward block, int8 products.
 
 Like the binding of ffn24.h it only marshals arguments: torch allocates and owns the tensors, every call enqueues on torch's current stream, and
-what does not fit is refused with ValueError (shapes, types, contiguity, checked here) or Ffn24Error (checked by the library).
+what does not fit is refused with ValueError (shapes, types, contiguity, the device, checked here) or Ffn24Error (checked by the library).
 """
 from __future__ import annotations
 
@@ -19,9 +19,14 @@ EXPORTS = ("layer_norm_fwd", "layer_norm_bwd_scratch", "layer_norm_bwd", "gated_
 _lib = None
 
 
-def _stream(t) -> int:
-    """torch's current stream on t's device, as a number (torch.cuda.current_stream builds an object first: 2.8 us a call, this 0.1)."""
-    return torch._C._cuda_getCurrentRawStream(t.device.index)
+def _stream(*tensors) -> int:
+    """torch's current stream, as a number (torch.cuda.current_stream builds an object first: 2.8 us a call, this 0.1).  The library launches on the current device, so all
+    tensors of the call have to be there."""
+    device = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"a tensor is on device {t.get_device()}, the current device is {device}")
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
 def lib() -> ctypes.CDLL:
@@ -72,7 +77,7 @@ def layer_norm_fwd(X, weight, bias=None, eps: float = 1e-5, residual=None):
     S = torch.empty_like(X) if residual is not None else None
     mean, rstd = torch.empty(T, dtype=torch.float32, device=X.device), torch.empty(T, dtype=torch.float32, device=X.device)
     _check(lib().layer_norm_fwd(_ptr(X), _ptr(residual), _ptr(weight), _ptr(bias), T, D, eps, _NORM_TYPES[X.dtype], _ptr(S), _ptr(Y), _ptr(mean), _ptr(rstd),
-                                _stream(X)), "layer_norm_fwd")
+                                _stream(X, residual, weight, bias)), "layer_norm_fwd")
     return Y, X if S is None else S, mean, rstd
 
 
@@ -89,7 +94,7 @@ def layer_norm_bwd(dY, S, weight, mean, rstd, dS=None):
     dw, db = torch.empty(D, dtype=torch.float32, device=S.device), torch.empty(D, dtype=torch.float32, device=S.device)
     scratch = torch.empty(max(int(lib().layer_norm_bwd_scratch(T, D)), 0), dtype=torch.uint8, device=S.device)
     _check(lib().layer_norm_bwd(_ptr(dY), _ptr(S), _ptr(weight), _ptr(mean), _ptr(rstd), _ptr(dS), T, D, _NORM_TYPES[S.dtype], _ptr(dX), _ptr(dw), _ptr(db),
-                                _ptr(scratch), _stream(S)), "layer_norm_bwd")
+                                _ptr(scratch), _stream(S, dY, dS, weight, mean, rstd)), "layer_norm_bwd")
     return dX, dw, db
 
 
@@ -143,7 +148,7 @@ class GatedContext(_Handle):
         self._expect_weights(Wgu, Wd)
         Y = torch.empty_like(X) if Y is None else Y
         _expect(Y, (t, self.D), _BF16, "Y")
-        _check(lib().gated_fwd(self._h, _ptr(X), t, _ptr(Wgu), _ptr(Wd), _ptr(Y), _stream(X)), "gated_fwd")
+        _check(lib().gated_fwd(self._h, _ptr(X), t, _ptr(Wgu), _ptr(Wd), _ptr(Y), _stream(X, Wgu, Wd, Y)), "gated_fwd")
         self._t = t
         return Y
 
@@ -157,7 +162,7 @@ class GatedContext(_Handle):
         _expect(dX, (t, self.D), _BF16, "dX")
         _expect(dWgu, (self.D, 2 * self.F), _BF16, "dWgu")
         _expect(dWd, (self.F, self.D), _BF16, "dWd")
-        _check(lib().gated_bwd(self._h, _ptr(dY), _ptr(X), _ptr(Wgu), _ptr(Wd), _ptr(dX), _ptr(dWgu), _ptr(dWd), _stream(X)), "gated_bwd")
+        _check(lib().gated_bwd(self._h, _ptr(dY), _ptr(X), _ptr(Wgu), _ptr(Wd), _ptr(dX), _ptr(dWgu), _ptr(dWd), _stream(dY, X, Wgu, Wd, dX, dWgu, dWd)), "gated_bwd")
         return dX, dWgu, dWd
 
 
@@ -189,7 +194,7 @@ def quantise_i8(X, codes=None, scales=None):
     scales = torch.empty((T,), dtype=torch.float32, device=X.device) if scales is None else scales
     _expect(codes, (T, K), _I8, "codes")
     _expect(scales, (T,), _F32, "scales")
-    _check(lib().quantise_i8(_ptr(X), T, K, _ptr(codes), _ptr(scales), _stream(X)), "quantise_i8")
+    _check(lib().quantise_i8(_ptr(X), T, K, _ptr(codes), _ptr(scales), _stream(X, codes, scales)), "quantise_i8")
     return codes, scales
 
 
@@ -200,7 +205,7 @@ def matmul_i8(codes, scales, W: I8Weight, Y=None):
     _expect(scales, (T,), _F32, "scales")
     Y = torch.empty((T, W.N), dtype=torch.bfloat16, device=codes.device) if Y is None else Y
     _expect(Y, (T, W.N), _BF16, "Y")
-    _check(lib().matmul_i8(_ptr(codes), _ptr(scales), T, _ptr(W.data), W.K, W.N, _ptr(Y), _stream(codes)), "matmul_i8")
+    _check(lib().matmul_i8(_ptr(codes), _ptr(scales), T, _ptr(W.data), W.K, W.N, _ptr(Y), _stream(codes, scales, W.data, Y)), "matmul_i8")
     return Y
 
 
@@ -211,7 +216,7 @@ def linear_i8(X, W: I8Weight, Y=None):
     Y = torch.empty((T, W.N), dtype=torch.bfloat16, device=X.device) if Y is None else Y
     _expect(Y, (T, W.N), _BF16, "Y")
     scratch = torch.empty(_size(int(lib().linear_i8_scratch(T, W.K, W.N)), "linear_i8"), dtype=torch.uint8, device=X.device)
-    _check(lib().linear_i8(_ptr(X), T, _ptr(W.data), W.K, W.N, _ptr(Y), _ptr(scratch), _stream(X)), "linear_i8")
+    _check(lib().linear_i8(_ptr(X), T, _ptr(W.data), W.K, W.N, _ptr(Y), _ptr(scratch), _stream(X, W.data, Y)), "linear_i8")
     return Y
 
 
@@ -234,7 +239,7 @@ class GatedI8Context(_Handle):
     def set_weights(self, Wgu, Wd):
         _expect(Wgu, (self.D, 2 * self.F), _BF16, "Wgu")
         _expect(Wd, (self.F, self.D), _BF16, "Wd")
-        _check(lib().gated_i8_set_weights(self._h, _ptr(Wgu), _ptr(Wd), _stream(Wd)), "gated_i8_set_weights")
+        _check(lib().gated_i8_set_weights(self._h, _ptr(Wgu), _ptr(Wd), _stream(Wgu, Wd)), "gated_i8_set_weights")
 
     def fwd(self, X, Y=None):
         """X [t, D] with any t up to T -> Y [t, D]."""
@@ -242,5 +247,5 @@ class GatedI8Context(_Handle):
         _expect(X, (t, self.D), _BF16, "X")
         Y = torch.empty_like(X) if Y is None else Y
         _expect(Y, (t, self.D), _BF16, "Y")
-        _check(lib().gated_i8_fwd(self._h, _ptr(X), t, _ptr(Y), _stream(X)), "gated_i8_fwd")
+        _check(lib().gated_i8_fwd(self._h, _ptr(X), t, _ptr(Y), _stream(X, Y)), "gated_i8_fwd")
         return Y
