@@ -109,13 +109,16 @@ def _gate(act: str) -> int:
 
 
 class _Handle:
-    """Owns a context of the library; the subclass names its destructor."""
+    """Owns a context of the library, on the device that was current at its creation; the subclass names its destructor."""
     _h = None
     _destroy = ""
 
+    def _own(self, h):
+        self._h, self._device = h, torch.cuda.current_device()
+
     def close(self):
         if self._h:
-            torch.cuda.synchronize()
+            torch.cuda.synchronize(self._device)
             _check(getattr(lib(), self._destroy)(self._h), self._destroy)
             self._h = None
 
@@ -135,7 +138,7 @@ class GatedContext(_Handle):
         self.T, self.D, self.F, self.training = T, D, F, training
         h = ctypes.c_void_p()
         _check(lib().gated_ctx_create(ctypes.byref(h), T, D, F, _gate(act), ffn24.FFN24_TRAINING if training else 0), "gated_ctx_create")
-        self._h = h
+        self._own(h)
 
     def _expect_weights(self, Wgu, Wd):
         _expect(Wgu, (self.D, 2 * self.F), _BF16, "Wgu")
@@ -233,7 +236,7 @@ class GatedI8Context(_Handle):
         _expect(Wgu, (D, 2 * F), _BF16, "Wgu")
         _expect(Wd, (F, D), _BF16, "Wd")
         _check(lib().gated_i8_ctx_create(ctypes.byref(h), T, D, F, gate), "gated_i8_ctx_create")
-        self._h = h
+        self._own(h)
         self.set_weights(Wgu, Wd)
 
     def set_weights(self, Wgu, Wd):

@@ -1,4 +1,6 @@
-"""The operators around the block run on the current device: the binding refuses tensors of another one before anything is launched."""
+"""The operators around the block run on the current device: the binding refuses tensors of another one before anything is launched, and a context waits for its own."""
+import ctypes
+
 import pytest
 import torch
 
@@ -87,3 +89,19 @@ def test_contexts_refuse_tensors_of_another_device(monkeypatch):
         for call in (lambda: bf16.fwd(X, Wgu, Wd), lambda: bf16.bwd(X, X, Wgu, Wd), lambda: i8.set_weights(Wgu, Wd), lambda: i8.fwd(X)):
             with pytest.raises(ValueError, match="device"):
                 call()
+
+
+def test_a_context_waits_for_its_own_device(monkeypatch):
+    waited, lib = [], _Lib()
+    monkeypatch.setattr(block, "lib", lambda: lib)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda device=None: waited.append(device))
+
+    def create(out, *args):
+        ctypes.cast(out, ctypes.POINTER(ctypes.c_void_p))[0] = 0x1000
+        return 0
+    lib.gated_ctx_create = create
+    ctx = block.GatedContext(4, 64, 64)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    ctx.close()
+    assert waited == [1] and lib.launched == ["gated_ctx_destroy"]
