@@ -87,11 +87,6 @@ __global__ void __launch_bounds__(256) gated_panelise_kernel(const u32x4* __rest
 }
 }  // namespace
 
-// dX has two K-contiguous operands.  Row by row the 256 x 256 tile reads 64 bytes of a row a stage, half a line; of both operands that is as many L2 requests as
-// there can be, of one of them it is hidden.  So Wgu is copied into panel form first where that tile is taken and the tokens pay for the pass over the
-// weights: T 16384 D 4096 F 16384 4.28 -> 3.22 ms + 0.12 for the pass, T 8192 D 2048 F 8192 591 -> 479 us + 34; on 128 x 64 tiles (T 1000) 40.0 -> 38.5.  dH, whose epilogue
-// moves more than its operands, gains 2.18 -> 2.10 ms for a pass of 0.06 and 401 -> 405 us: it reads Wd row by row.
-bool gated_dx_panels(int T, int D, int F) { return T >= 2048 && pick_edge_tile(D, T, 2 * F) == 0; }
 // for any token count up to T: what the splits of Y and dX need (beyond 2^24 values a result has 4096 of the smallest tiles)
 size_t gated_scratch(int T, int D, int F, bool training) {
   size_t most = 0;
@@ -100,23 +95,6 @@ size_t gated_scratch(int T, int D, int F, bool training) {
     if (top > most) most = top;
   }
   return most;
-}
-// The tile of dX and the weight gradients in one launch, 0: apart (dX then may be split).  Together they take all their tiles over the CUs and one tile of the shorter kind
-// more, or the dX tiles' own rounds if that is longer, which beside other tiles on their CUs take a third more than alone.  Whole steps, together / apart, us (T D F):
-// 500 4096 8192 425, 449; 2000 1024 2816 155, 172; 1500 2048 5440 361, 378; 300 512 1536 33.0, 35.9; the other way 163 5312 14464 637, 554; 333 2816 8896 324, 238; 700 2048 8192 308, 298.
-int pick_grads_tile(int T, int D, int F, int K) {
-  const int tw = pick_edge_tile(D, 2 * F, K, F, D);
-  const auto rounds = [](long long n) { return (n + CHIP_CUS - 1) / CHIP_CUS; };
-  const auto weights = [&](const TileCost& t) { return edge_tiles(t, D, 2 * F) + edge_tiles(t, F, D); };
-  long long best_time = edge_split_time(D, T, 2 * F) + rounds(weights(TILES_DENSE[tw])) * tile_time(TILES_DENSE[tw], K, false) + 3000;
-  int best = 0;
-  for (int i = 1; i < NUM_TILES; i++) {
-    const TileCost& t = TILES_DENSE[i];
-    const long long nx = edge_tiles(t, D, T), one_x = tile_time(t, 2 * F, false), one_w = tile_time(t, K, false);
-    const long long all = (nx * one_x + weights(t) * one_w) / CHIP_CUS + one_w, longest = rounds(nx) * one_x * 27 / 20, time = all > longest ? all : longest;
-    if (time < best_time) { best = i; best_time = time; }
-  }
-  return best;
 }
 size_t gated_panel_bytes(int rows, int K) { return 2 * (size_t)up_to(rows, 256) * (size_t)K; }
 int launch_gated_panels(const void* Wgu, int D, int F, void* panels, hipStream_t s) {

@@ -21,9 +21,8 @@ int launch_norm_bwd(const void* dY, const void* S, const float* w, const float* 
 int launch_gated_up(const void* X, const void* Wgu, int T, int D, int F, float c1, float c3, void* H, void* GU, void* GUx, hipStream_t s);
 int launch_gated_down(const void* H, const void* Wd, int T, int D, int F, void* Y, const Scratch& scratch, hipStream_t s);
 size_t gated_scratch(int T, int D, int F, bool training);   // bytes of `scratch` for any token count up to T (with less, reductions are not split)
-bool gated_dx_panels(int T, int D, int F);   // whether dX reads Wgu in panel form (`panels` below: it is)
 size_t gated_panel_bytes(int rows, int K);
-int launch_gated_panels(const void* Wgu, int D, int F, void* panels, hipStream_t s);
+int launch_gated_panels(const void* Wgu, int D, int F, void* panels, hipStream_t s);   // for dX (gated_dx_panels; `panels` below: it reads Wgu so)
 int launch_gated_dgate(const void* dY, const void* Wd, const void* GU, const void* GUx, int T, int D, int F, float c1, float c3, void* dGU, hipStream_t s);
 int launch_gated_grads(const void* X, const void* dY, const void* H, const void* dGU, const void* Wgu, bool panels, int T, int D, int F, void* dX, void* dWgu, void* dWd,
                        const Scratch& scratch, hipStream_t s);

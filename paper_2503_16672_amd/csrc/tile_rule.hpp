@@ -101,6 +101,29 @@ inline long long edge_split_time(int M, int N, int K) {
   return (p.splits * edge_tiles(t, M, N) + CHIP_CUS - 1) / CHIP_CUS * tile_time(t, p.part, false) + (p.splits > 1 ? 5000 + 8LL * p.splits * M * N / 5000 : 0);
 }
 
+// The gated block's backward (k_gated.hip).  dX has two K-contiguous operands.  Row by row the 256 x 256 tile reads 64 bytes of a row a stage, half a line; of both
+// operands that is as many L2 requests as there can be, of one of them it is hidden.  So Wgu is copied into panel form first where that tile is taken and the tokens pay for
+// the pass over the weights: T 16384 D 4096 F 16384 4.28 -> 3.22 ms + 0.12 for the pass, T 8192 D 2048 F 8192 591 -> 479 us + 34; on 128 x 64 tiles (T 1000) 40.0 -> 38.5.
+// dH, whose epilogue moves more than its operands, gains 2.18 -> 2.10 ms for a pass of 0.06 and 401 -> 405 us: it reads Wd row by row.
+inline bool gated_dx_panels(int T, int D, int F) { return T >= 2048 && pick_edge_tile(D, T, 2 * F) == 0; }
+// The tile of dX and the weight gradients in one launch, 0: apart (dX then may be split).  Together they take all their tiles over the CUs and one tile of the shorter kind
+// more, or the dX tiles' own rounds if that is longer, which beside other tiles on their CUs take a third more than alone.  Whole steps, together / apart, us (T D F):
+// 500 4096 8192 425, 449; 2000 1024 2816 155, 172; 1500 2048 5440 361, 378; 300 512 1536 33.0, 35.9; the other way 163 5312 14464 637, 554; 333 2816 8896 324, 238; 700 2048 8192 308, 298.
+inline int pick_grads_tile(int T, int D, int F, int K) {
+  const int tw = pick_edge_tile(D, 2 * F, K, F, D);
+  const auto rounds = [](long long n) { return (n + CHIP_CUS - 1) / CHIP_CUS; };
+  const auto weights = [&](const TileCost& t) { return edge_tiles(t, D, 2 * F) + edge_tiles(t, F, D); };
+  long long best_time = edge_split_time(D, T, 2 * F) + rounds(weights(TILES_DENSE[tw])) * tile_time(TILES_DENSE[tw], K, false) + 3000;
+  int best = 0;
+  for (int i = 1; i < NUM_TILES; i++) {
+    const TileCost& t = TILES_DENSE[i];
+    const long long nx = edge_tiles(t, D, T), one_x = tile_time(t, 2 * F, false), one_w = tile_time(t, K, false);
+    const long long all = (nx * one_x + weights(t) * one_w) / CHIP_CUS + one_w, longest = rounds(nx) * one_x * 27 / 20, time = all > longest ? all : longest;
+    if (time < best_time) { best = i; best_time = time; }
+  }
+  return best;
+}
+
 // Few tokens (k_few.hip): where its kernels are faster than the GEMM core's smallest tiles.  Both, us (T D F): 16 512 1536 12.1, 12.3; 32 512 1536 16.2, 12.4; 32 256 768 12.8,
 // 8.6; 17 1024 4096 18.6, 22.3; 32 1024 4096 20.6, 22.4; 32 2048 5440 30.8, 45.2; 48 512 1536 17.3, 12.4; 64 1024 4096 27.6, 22.7; 37 2048 5440 32.5, 46.1; 64 4096 16384 94, 146.
 constexpr int FEW_TOKENS = 64;
