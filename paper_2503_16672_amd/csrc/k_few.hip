@@ -6,9 +6,9 @@
 // bf16: the weights are k-major.  Lane (c, q) of a wave loads 16 bytes, 8 neighbouring channels, of rows k 8 q .. 8 q + 7 of a step of 32 k; transposed in
 // registers (byte permutes), channel t of every lane's eight is the row c of matrix op t.  16 lanes are 256 bytes of a row: 128 channels, or 64 gate channels and the
 // 64 up channels of the same numbers.
-// Measured, one token at 4096 x 16384: gate and up 47 us (268 MB, 5.7 TB/s), down 23 (134 MB, 5.8) and 4.6 for the sums of its 8 splits.
+// Measured, one token at 4096 x 16384: gate and up 48 us (268 MB, 5.6 TB/s), down 23.5 (134 MB, 5.7) and 4.6 for the sums of its 8 splits.
 // 8-bit integers: the panel form (gemm_core.hpp) has the 16 bytes of k that a lane of the 16 x 16 x 64 op takes next to each other: 16 rows are a contiguous KiB.
-// 16 tokens at 4096 x 16384: 22 us (134 MB, 6.1 TB/s), 15.5 (67 MB, 4.3), and 2 to 5 each for the two quantisations.
+// 16 tokens at 4096 x 16384: 22.4 us (134 MB, 6.0 TB/s), 16.5 (67 MB, 4.1), and 4.6 and 5.1 for the two quantisations.
 #include "launch_block.hpp"
 #include "launch_edge.hpp"
 #include "i8_codes.hpp"

@@ -1,13 +1,13 @@
 // Products of 8-bit integers with a scale for each token and each output channel, and the quantisation that makes their operands.
 //
 //   scale = max |row| * (1 / 127), the factor and the product rounded to fp32 (1 if the row is all zero; infinite or NaN if a value is, and with it every result of the row);  code = rint(x / scale)
-//   Y[t][n] = bf16(sum_k X8[t][k] W8[k][n] * (sx[t] * sw[n])), the sum in 32-bit integers: exact up to K = 133152, so results do not depend on its order
+//   Y[t][n] = bf16(sum_k X8[t][k] W8[k][n] * (sx[t] * sw[n])), the sum in 32-bit integers: exact up to K = 133144 ((2^31 - 1) / 127^2; 2^17 is the most a call takes), so results do not depend on its order
 //
 // The weights are laid out once: transposed, K-contiguous, in the A panel form of gemm_core.hpp (64-byte pieces), K filled up to 128 and the channels to 256 with
 // zeros, then the scales of the panel's rows, then the words the largest magnitudes are found in.
 //
-// The quantisation is a pass over the data (8192 x 4096 26 us, 3.9 TB/s; the hidden layer 8192 x 16384, whose maxima the epilogue before it collects, 81 us, 5.0 TB/s); the
-// products run at 2.3 (gated, with the gate in the epilogue) and 2.8 POP/s (plain) at 8192 x 4096 x 16384, twice the rate of bf16 on the same tiles.
+// The quantisation is a pass over the data (8192 x 4096 26 us, 3.8 TB/s; the hidden layer 8192 x 16384, whose maxima the epilogue before it collects, 84 us, 4.8 TB/s); the
+// products run at 2.2 (gated, with the gate in the epilogue) and 2.6 POP/s (plain) at 8192 x 4096 x 16384, 2.3 and 2.8 at best: twice the rate of bf16 on the same tiles.
 #include "launch_block.hpp"
 #include "launch_edge.hpp"
 #include "i8_codes.hpp"

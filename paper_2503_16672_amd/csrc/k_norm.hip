@@ -329,12 +329,13 @@ __global__ void __launch_bounds__(1024) norm_sum_kernel(const float* __restrict_
   }
 }
 
-// The streaming hint from tensors of 128 MiB on, four of which the caches do not hold (T x D, bf16, with / without, us: forward 16384 x 4096 87, 101; 4096 x 8192 46.6, 43.5; 16384 x 1024
-// 26.7, 23.4; backward 100, 112; 64, 61.5; 37, 35.7; 2000 x 16384 forward 82, 54).
+// The streaming hint from tensors of 128 MiB on, four of which the caches do not hold (T x D, with / without, whole calls, us: forward bf16 16384 x 4096 83.8, 105.9; 8192 x 8192 81.0, 98.6;
+// 32768 x 2048 90, 100; 4096 x 8192 43.6, 43.1; 16384 x 1024 23.2, 22.8; 2000 x 16384 49.2, 48.1; fp32 8192 x 4096 94, 100; 16384 x 4096 207, 199; backward in that order 91, 106; 89.5, 101.6; 97, 101;
+// 50.0, 49.7; 30.2, 29.1; 68, 76; 101, 103; 198, 200).
 template <class E> bool hint(int T, int D) { return sizeof(E) * (size_t)T * (size_t)D >= (size_t)1 << 27; }
 
-// Workgroups: 16 waves a CU, each with rows to walk (T x D, bf16, 12 / 16 / 32 / 64 waves: 16384 x 4096 88.8, 87.0, 90.4, 94.0 us; 4096 x 8192 51, 46.7, 49.6, 61.2; a row a workgroup and
-// no prefetch 114).
+// Workgroups: 16 waves a CU, each with rows to walk (T x D, bf16, 12 / 16 / 32 / 64 waves: 16384 x 4096 82.6, 83.8, 85.3, 82.9 us; 4096 x 8192 47.6, 43.1, 43.7, 45.8; a row a workgroup and
+// no prefetch 114 at the first).  fp32 16384 x 4096: 208 us, 5.2 TB/s.
 template <class E, bool EVEN, int P, int W, int R>
 void fwd(const void* X, const void* res, const float* w, const float* b, int T, int D, float eps, void* S, void* Y, float* mean, float* rstd, hipStream_t s) {
   constexpr int most = 256 * NORM_FWD_WAVES / (W * R);
@@ -380,8 +381,8 @@ int launch_norm_fwd(const void* X, const void* R, const float* w, const float* b
   return (int)hipGetLastError();
 }
 
-// Workgroups of the backward, each with its partial sums: the chip's CUs, twice from 1025 to 4096 columns, where a workgroup is four waves (T x D, bf16, 256 / 512 / 1024: 16384 x 4096
-// 119, 100, 113 us; 8192 x 2048 50, 40, 46; 4096 x 8192 53, 64, 85; 16384 x 1024 36, 37, 51; 2000 x 16384 86, 100, 217).
+// Workgroups of the backward, each with its partial sums: the chip's CUs, twice from 1025 to 4096 columns, where a workgroup is four waves (T x D, bf16, 256 / 512 / 1024,
+// whole calls: 16384 x 4096 115, 93, 100 us; 8192 x 2048 45, 30.4, 32.6; 4096 x 8192 50, 58, 76; 16384 x 1024 29.3, 27.8, 31.5; 2000 x 16384 76, 90, 121; fp32 16384 x 4096 198, 200, 204).
 int norm_bwd_parts(int64_t T, int D) {
   const int R = bwd_rows(D);
   const int64_t n = (T + R - 1) / R;

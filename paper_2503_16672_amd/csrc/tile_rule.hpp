@@ -124,14 +124,17 @@ inline int pick_grads_tile(int T, int D, int F, int K) {
   return best;
 }
 
-// Few tokens (k_few.hip): where its kernels are faster than the GEMM core's smallest tiles.  Both, us (T D F): 16 512 1536 12.1, 12.3; 32 512 1536 16.2, 12.4; 32 256 768 12.8,
-// 8.6; 17 1024 4096 18.6, 22.3; 32 1024 4096 20.6, 22.4; 32 2048 5440 30.8, 45.2; 48 512 1536 17.3, 12.4; 64 1024 4096 27.6, 22.7; 37 2048 5440 32.5, 46.1; 64 4096 16384 94, 146.
+// Few tokens: the kernels of k_few.hip or the GEMM core.  Whole forwards of the block, few tokens' kernels / core, us (T D F; weights from memory): 1 4096 16384 77.3, 75.3; 16 512 1536
+// 12.6, 12.4; 16 4096 16384 80.0, 79.0; 32 512 1536 16.2, 12.4; 32 256 768 12.9, 10.1; 17 1024 4096 18.8, 15.3; 32 1024 4096 20.8, 15.9; 32 2048 5440 30.8, 27.8; 48 512 1536 17.3, 12.7; 64 1024
+// 4096 26.6, 16.7; 37 2048 5440 30.8, 28.1; 64 2048 8192 51.7, 36.8; 64 4096 16384 94.4, 89.7.  The line was drawn when the core did not split long reductions (17 1024 4096 22.3, 37 2048
+// 5440 46.1, 64 4096 16384 146): it is due to be drawn again.
 constexpr int FEW_TOKENS = 64;
 inline bool few_tokens(int T, int D, int F) { return T <= 16 || (T <= FEW_TOKENS && (long long)D * F >= (T <= 32 ? 1 << 21 : 1 << 23)); }
 
-// The same for 8-bit integers, us.  One product (T K N): 1 2048 8192 8.9, 11.0; 16 4096 4096 11.8, 12.2; 1 8192 8192 14.5, 24.9; 32 4096 16384 20.8, 18.4; 24 8192 8192
-// 24.8, 25.5; 32 4096 4096 12.3, 12.2; 64 4096 16384 30.9, 19.4.  Gated block (T D F): 1 4096 16384 39.1, 69.5; 16 4096 16384 50, 70; 32 4096 16384 60, 71; 24 2048 8192 28.4, 33.5; 20
-// 1024 2816 21.9, 19.3; 32 512 1536 20.0, 15.9; 64 4096 16384 87, 78.
+// The same for 8-bit integers, us.  One product (T K N): 1 2048 8192 9.7, 12.9; 16 4096 4096 12.9, 13.0; 1 8192 8192 14.6, 26.1; 32 4096 16384 22.0, 19.5; 24 8192 8192
+// 25.7, 27.5; 32 8192 8192 28.3, 27.4; 32 4096 4096 12.9, 13.1; 32 16384 4096 30.1, 24.2.  Gated block (T D F): 1 4096 16384 39.1, 52.7; 16 4096 16384 49.5, 54.0; 24 4096 16384 56.0, 54.9; 32
+// 4096 16384 59.6, 54.2; 24 2048 8192 28.0, 31.9; 32 2048 8192 30.2, 32.0; 1 5120 13824 44.8, 54.9; 16 5120 13824 69.6, 56.3; 32 5120 13824 93.7, 56.7; 24 2048 5440 31.8, 25.0; 4 512 1536 14.0,
+// 17.1; 16 512 1536 25.1, 17.1; 20 1024 2816 21.9, 19.6; 32 512 1536 20.0, 16.9.  The block's line is of before the core read the codes in panel form (32 4096 16384 71) and is due to be drawn again.
 constexpr int FEW_I8_TOKENS = 32;
 inline bool few_i8_tokens(int T, int K) { return T <= 16 || (T <= FEW_I8_TOKENS && K >= 8192); }
 inline bool few_gated_i8_tokens(int T, int D, int F) { return T <= 16 || (T <= FEW_I8_TOKENS && (long long)D * F >= 1 << 23); }
