@@ -122,19 +122,19 @@ def prepare(case, seed):
     st = {"case": case, **_inputs(case, seed)}
     kind, T, X = case["kind"], case["T"], st["X"]
     if own:
-        from paper_2503_16672_amd import block
+        from paper_2503_16672_amd import serve
         if kind == "mx4_round":
             st["codes"] = torch.empty((T, case["K"] // 2), dtype=torch.uint8, device="cuda")
             st["scales"] = torch.empty((T, case["K"] // 32), dtype=torch.uint8, device="cuda")
             st["Y"] = torch.empty_like(X)
         elif kind == "linear_mx4":
-            st["W4"] = block.Mx4Weight(st["W"])
+            st["W4"] = serve.Mx4Weight(st["W"])
             st["Y"] = torch.empty((T, case["N"]), dtype=torch.bfloat16, device="cuda")
         elif kind == "gated_mx4":
-            st["ctx"] = block.GatedMx4Context(T, st["Wgu"], st["Wd"], act=case["act"])
+            st["ctx"] = serve.GatedMx4Context(T, st["Wgu"], st["Wd"], act=case["act"])
             st["Y"] = torch.empty_like(X)
         else:
-            st["ctx"] = block.MoeContext(T, st["Wr"], st["Wgu"], st["Wd"], case["k"], act=case["act"], renormalise=case["renormalise"], weights=case["weights"])
+            st["ctx"] = serve.MoeContext(T, st["Wr"], st["Wgu"], st["Wd"], case["k"], act=case["act"], renormalise=case["renormalise"], weights=case["weights"])
             st["Y"] = torch.empty_like(X)
     elif kind == "linear_mx4":
         st["W"] = _mx4(st["W"].float(), 0)
@@ -153,13 +153,13 @@ def run(state):
 
 
 def _run_own(st):
-    from paper_2503_16672_amd import block
+    from paper_2503_16672_amd import serve
     kind = st["case"]["kind"]
     if kind == "mx4_round":
-        codes, scales = block.quantise_mx4(st["X"], codes=st["codes"], scales=st["scales"])
-        return block.dequantise_mx4(codes, scales, Y=st["Y"])
+        codes, scales = serve.quantise_mx4(st["X"], codes=st["codes"], scales=st["scales"])
+        return serve.dequantise_mx4(codes, scales, Y=st["Y"])
     if kind == "linear_mx4":
-        return block.linear_mx4(st["X"], st["W4"], Y=st["Y"])
+        return serve.linear_mx4(st["X"], st["W4"], Y=st["Y"])
     return st["ctx"].fwd(st["X"], Y=st["Y"])
 
 
