@@ -54,4 +54,32 @@ int launch_few_matmul_i8(const void* codes, const float* sx, int T, const I8Layo
 int launch_few_gated_i8(const void* X, int T, const I8Layout& wgu, const I8Layout& wd, float c1, float c3, void* X8, float* sx, void* H, uint32_t* tops, void* H8, float* sh,
                         void* Y, hipStream_t s);
 
+// k_mx4.hip (the operand form: mx4_core.hpp); T, K, N >= 1, K a multiple of 32, N of 8
+struct Mx4Operand { const char* codes; const char* scales; int steps; };
+int launch_quantise_mx4(const void* X, bool f32, int64_t T, int64_t K, void* codes, void* scales, hipStream_t s);
+int launch_dequantise_mx4(const void* codes, const void* scales, bool f32, int64_t T, int64_t K, void* Y, hipStream_t s);
+int64_t mx4_operand_size(int64_t rows, int64_t K);
+int64_t bf16_operand_size(int64_t rows, int64_t K);      // bf16 weights in the same order, 32 k a step
+Mx4Operand mx4_operand(const void* p, int rows, int K);
+// `count` matrices W [K][N] one after the other
+int launch_mx4_weight(const void* W, int K, int N, bool halves, int count, void* out, hipStream_t s);
+int launch_bf16_weight(const void* W, int K, int N, bool halves, int count, void* out, hipStream_t s);
+int launch_mx4_weight_codes(const void* codes, const void* scales, int K, int N, bool halves, void* out, hipStream_t s);
+int launch_copy16(const void* from, void* to, size_t bytes, hipStream_t s);   // 16-byte aligned, a multiple of 16 bytes
+int launch_mx4_tokens(const void* X, int T, int K, const Mx4Operand& out, hipStream_t s);
+size_t mx4_split_scratch(int M, int N, int K);
+int launch_mx4_product(const Mx4Operand& w, int M, const Mx4Operand& x, int T, void* Y, const Scratch& scratch, hipStream_t s);
+int launch_mx4_gated_up(const Mx4Operand& w, int F, const Mx4Operand& x, int T, float c1, float c3, const Mx4Operand& h, hipStream_t s);
+
+// k_experts.hip: few tokens
+int launch_few_mx4_up(const Mx4Operand& w, const void* X, int T, int D, int F, float c1, float c3, const Mx4Operand& h, hipStream_t s);
+int launch_few_mx4_rows(const Mx4Operand& w, int K, int N, const void* X, const Mx4Operand* x, int T, void* Y, hipStream_t s);   // X: bf16 rows; x: instead of them
+// mixture of experts: T <= MOE_TOKENS, E <= 256, k <= 16; up and down: E matrices in the operand form of mx4 or bf16
+constexpr int MOE_TOKENS = 64, MOE_MAX_E = 256, MOE_MAX_K = 16;
+struct MoeWeights { bool mx4; const void *up, *down; size_t up_stride, down_stride, up_scales, down_scales; };
+size_t moe_parts_size(int T, int D, int E);
+int launch_moe_route(const void* X, const void* Wr, int T, int D, int E, int k, bool renormalise, void* parts, int* picks, float* shares, hipStream_t s);
+int launch_moe_experts(const MoeWeights& w, const void* X, int T, int D, int F, int E, int k, float c1, float c3, const int* picks, const float* shares, void* H, int h_rows,
+                       void* Y, hipStream_t s);
+
 }  // namespace ffn24
