@@ -73,11 +73,28 @@ struct Mx4Geo {
 };
 
 // The accumulator tied in place: through the builtin the compiler moves accumulators round the scaled op and runs at half its rate (4.9 against 7.1 PFLOP/s in a loop of nothing
-// else).  The scale is byte 0 of its registers.
+// else).  J: the byte of the scales' registers, the step's number of four.
+template <int J>
 __device__ __forceinline__ void op16_mx4(const u32x4& a, const u32x4& b, uint32_t sa, uint32_t sb, f32x4& c) {
-  asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[0,0,0] op_sel_hi:[0,0,0] cbsz:4 blgp:4" : "+a"(c) : "v"(a), "v"(b), "v"(sa), "v"(sb));
+#define FFN24_OP(lo, hi) \
+  asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[" lo "," lo ",0] op_sel_hi:[" hi "," hi ",0] cbsz:4 blgp:4" : "+a"(c) : "v"(a), "v"(b), "v"(sa), "v"(sb))
+  if constexpr (J == 0) FFN24_OP("0", "0");
+  else if constexpr (J == 1) FFN24_OP("1", "0");
+  else if constexpr (J == 2) FFN24_OP("0", "1");
+  else FFN24_OP("1", "1");
+#undef FFN24_OP
 }
 
+// item I of N on slots 1, 2, 5, 6, ... (of few slots: from the first one on)
+template <int N, int SLOTS, int M, class F>
+__device__ __forceinline__ void mx4_early(F&& f) {
+  if constexpr (SLOTS >= 2 * N + 2) {
+    constexpr int i = M % 4 == 1 ? M / 4 * 2 : M % 4 == 2 ? M / 4 * 2 + 1 : N;
+    if constexpr (i < N) f(std::integral_constant<int, i>{});
+  } else if constexpr (M < N) {
+    f(std::integral_constant<int, M>{});
+  }
+}
 // item I of N spread over SLOTS slots
 template <int N, int SLOTS, int M, class F>
 __device__ __forceinline__ void mx4_ride(F&& f) {
@@ -119,9 +136,9 @@ __device__ __forceinline__ void mx4_tile(const Mx4Gemm& g, const typename Epi::A
     else __builtin_amdgcn_raw_ptr_buffer_load_lds(sa_r, to, 16, lane * 16, (int)off, 0, 0);
   };
   // instruction J of stage kt
-  auto issue = [&](auto J, int kt) {
+  auto issue = [&](auto J, int kt, int slot) {                 // slot: kt & 3
     constexpr int j = decltype(J)::value;
-    char* const buf = smem + (kt & 3) * G::STAGE;
+    char* const buf = smem + slot * G::STAGE;
     if constexpr (j < AM / 2) {
       __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_char*)(buf + (wave * (AM / 2) + j) * 1024), 16, lane * 16, (int)(oa[j < AM / 2 ? j : 0] + (uint32_t)kt * MX4_PANEL), 0, 0);
     } else if constexpr (j < AM / 2 + BN / 2) {
@@ -129,14 +146,14 @@ __device__ __forceinline__ void mx4_tile(const Mx4Gemm& g, const typename Epi::A
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_char*)(buf + (2 * AM + wave * (BN / 2) + i) * 1024), 16, lane * 16, (int)(ob[i] + (uint32_t)kt * MX4_PANEL), 0, 0);
     } else {
       // a part of the next four steps' scales; the parts come round more often than there are any
-      issue_scales((4 * (kt & 3) + wave) % G::SCALES, min((kt >> 2) + 1, last));
+      issue_scales((4 * slot + wave) % G::SCALES, min((kt >> 2) + 1, last));
     }
   };
 
   const bool full = n >= 4;
   for (int i = wave; i < (G::SCALES + 3) / 4 * 4; i += 4) issue_scales(i % G::SCALES, 0);
-  for (int s = 0; s < min(n, 3); s++) static_for<D>([&](auto J) { issue(J, s); });
-  if (full) static_for<H1>([&](auto J) { issue(J, 3); });
+  for (int s = 0; s < min(n, 3); s++) static_for<D>([&](auto J) { issue(J, s, s); });
+  if (full) static_for<H1>([&](auto J) { issue(J, 3, 3); });
 
   f32x4 acc[AM][BN];
 #pragma unroll
@@ -166,59 +183,55 @@ __device__ __forceinline__ void mx4_tile(const Mx4Gemm& g, const typename Epi::A
   FFN24_FENCE();
   asm volatile("s_nop 4" ::: "memory");
 
-  // The step of stage kt, in two halves as the 256 x 256 tile of gemm_core.hpp: the other half's B fragments are read during the first; then one barrier, behind
-  // which this stage's buffer is free; during the second the next step's fragments are read and the stage that reuses the buffer is asked for.
-  auto step = [&](int kt, auto rest, auto ask, auto left) {
-    constexpr bool REST = decltype(rest)::value != 0, ASK = decltype(ask)::value != 0;
-    constexpr int LEFT = decltype(left)::value;
-    const int cur = (kt & 3) * G::STAGE, nxt = ((kt + 1) & 3) * G::STAGE;
-    const bool turn = (kt & 3) == 3;
+  // The step of stage kt, the J-th of its four, in two halves as the 256 x 256 tile of gemm_core.hpp: the other half's B fragments are read during the first; then one
+  // barrier, behind which this stage's buffer is free; during the second the next step's fragments are read and the stage that reuses the buffer is asked for.
+  // TAIL: there may be no stage left to ask for, or to read (what is read then is not used).
+  auto step = [&](int kt, auto j, auto tail) {
+    constexpr int J = decltype(j)::value, cur = J * G::STAGE, nxt = (J + 1) % 4 * G::STAGE;
+    constexpr bool TAIL = decltype(tail)::value != 0;
+    const bool rest = !TAIL || kt + 3 < n, ask = !TAIL || kt + 4 < n;
     FFN24_FENCE();
     static_for<HO>([&](auto M) {
       constexpr int mi = M / HB, ni = M % HB;
-      op16_mx4(a[mi], b[0][ni], sa[mi], sb[ni], acc[mi][ni]);
-      mx4_ride<HB, HO, M>([&](auto I) { b[1][I] = *reinterpret_cast<const u32x4*>(lb + cur + (HB + I) * 1024); });
-      if constexpr (REST) mx4_ride<D - H1, HO, M>([&](auto I) { issue(std::integral_constant<int, H1 + decltype(I)::value>{}, kt + 3); });
+      op16_mx4<J>(a[mi], b[0][ni], sa[mi], sb[ni], acc[mi][ni]);
+      mx4_early<HB, HO, M>([&](auto I) { b[1][I] = *reinterpret_cast<const u32x4*>(lb + cur + (HB + I) * 1024); });
+      mx4_ride<D - H1, HO, M>([&](auto I) { if (rest) issue(std::integral_constant<int, H1 + decltype(I)::value>{}, kt + 3, (J + 3) % 4); });
       FFN24_FENCE();
     });
-    if constexpr (LEFT >= 0) {
-      wait_vmcnt<(LEFT > 0 ? LEFT : 0)>();
-      wait_lgkmcnt0();
-      __builtin_amdgcn_s_barrier();
-    }
+    if (rest && ask) wait_vmcnt<2 * D>(); else wait_vmcnt<0>();
+    wait_lgkmcnt0();
+    __builtin_amdgcn_s_barrier();
     FFN24_FENCE();
     uint32_t na[AM], nb[BN];
-    if (LEFT >= 0 && turn) read_scales((kt >> 2) + 1, na, nb);
+    if constexpr (J == 3) read_scales((kt >> 2) + 1, na, nb);
     FFN24_FENCE();
     static_for<HO>([&](auto M) {
       constexpr int mi = M / HB, ni = M % HB;
-      op16_mx4(a[mi], b[1][ni], sa[mi], sb[HB + ni], acc[mi][HB + ni]);
-      if constexpr (LEFT >= 0) {
-        mx4_ride<HB, HO, M>([&](auto I) { b[0][I] = *reinterpret_cast<const u32x4*>(lb + nxt + I * 1024); });
-        if constexpr (ni == HB - 1) a[mi] = *reinterpret_cast<const u32x4*>(la + nxt + mi * 1024);
-      }
-      if constexpr (ASK) mx4_ride<H1, HO, M>([&](auto I) { issue(I, kt + 4); });
+      op16_mx4<J>(a[mi], b[1][ni], sa[mi], sb[HB + ni], acc[mi][HB + ni]);
+      mx4_early<HB, HO, M>([&](auto I) { b[0][I] = *reinterpret_cast<const u32x4*>(lb + nxt + I * 1024); });
+      if constexpr (ni == HB - 1) a[mi] = *reinterpret_cast<const u32x4*>(la + nxt + mi * 1024);
+      mx4_ride<H1, HO, M>([&](auto I) { if (ask) issue(I, kt + 4, J); });
       FFN24_FENCE();
     });
-    if constexpr (LEFT >= 0) {
-      // the next step's scales: the next byte, or the registers just read.  (a vector instruction may write an operand two states before its op at the latest)
+    if constexpr (J == 3) {
+      // (a vector instruction may write an operand two states before its op at the latest)
 #pragma unroll
-      for (int t = 0; t < AM; t++) sa[t] = turn ? na[t] : sa[t] >> 8;
+      for (int t = 0; t < AM; t++) sa[t] = na[t];
 #pragma unroll
-      for (int t = 0; t < BN; t++) sb[t] = turn ? nb[t] : sb[t] >> 8;
+      for (int t = 0; t < BN; t++) sb[t] = nb[t];
       FFN24_FENCE();
       asm volatile("s_nop 1" ::: "memory");
     }
   };
-  using I0 = std::integral_constant<int, 0>; using I1 = std::integral_constant<int, 1>; using None = std::integral_constant<int, -1>;
+  using I0 = std::integral_constant<int, 0>; using I1 = std::integral_constant<int, 1>;
   int kt = 0;
-  if (full) {
-    for (; kt < n - 4; kt++) step(kt, I1{}, I1{}, std::integral_constant<int, 2 * D>{});
-    step(kt, I1{}, I0{}, I0{});
-    kt++;
-  }
-  for (; kt < n - 1; kt++) step(kt, I0{}, I0{}, I0{});
-  step(kt, I0{}, I0{}, None{});
+  for (; kt + 8 <= n; kt += 4) static_for<4>([&](auto J) { step(kt + J, J, I0{}); });
+  while (kt < n) static_for<4>([&](auto J) {
+    if (kt < n) {
+      step(kt, J, I1{});
+      kt++;
+    }
+  });
 
   asm volatile("s_nop 15\n s_nop 15\n s_nop 15" ::: "memory");
 #pragma unroll
