@@ -265,8 +265,12 @@ int launch_mx4_product(const Mx4Operand& w, int M, const Mx4Operand& x, int T, v
 }
 int launch_mx4_gated_up(const Mx4Operand& w, int F, const Mx4Operand& x, int T, float c1, float c3, const Mx4Operand& h, hipStream_t s) {
   const Mx4Gemm g{w, x, 2 * F, T, 0, 0};
-  return launch_mx4<Mx4Gated>(g, Mx4Gated::Args{const_cast<char*>(h.codes), reinterpret_cast<uint8_t*>(const_cast<char*>(h.scales)), F, T, h.steps, Gate{c1, c3}},
-                              mx4_plan(2 * F, T, w.steps, false), s);
+  const Mx4Plan p = mx4_plan(2 * F, T, w.steps, false);
+  const auto go = [&](auto epi) {
+    using Epi = decltype(epi);
+    return launch_mx4<Epi>(g, typename Epi::Args{const_cast<char*>(h.codes), reinterpret_cast<uint8_t*>(const_cast<char*>(h.scales)), F, T, h.steps, Gate{c1, c3}}, p, s);
+  };
+  return c3 == 0.f && c1 == 1.f ? go(Mx4Gated<false>{}) : go(Mx4Gated<true>{});
 }
 
 }  // namespace ffn24

@@ -62,14 +62,16 @@ struct Mx4Gemm {
   int first, steps;         // the part of the reduction
 };
 
-// The block tile: 2 x 2 waves of 16 AM x 16 BN.  The ring holds four stages of one step; a stage's scales come with the four steps before them.
+// The block tile: 2 x 2 waves of 16 AM x 16 BN.  The ring holds RING stages of one step; the scales of four steps come beside them.  256 x 128 tiles have a ring of three, so that
+// two share a CU: one's results go out while the other's matrix ops run.
 template <int AM, int BN>
 struct Mx4Geo {
-  static constexpr int BM = 32 * AM, BNT = 32 * BN, RING = 4;
+  static constexpr int BM = 32 * AM, BNT = 32 * BN, RING = AM * BN == 32 ? 3 : 4;
   static constexpr int STAGE = (2 * AM + 2 * BN) * 1024, SCALES = (AM + BN) / 2;   // scales: KiB (instructions) for four steps
-  static constexpr int LDS = RING * STAGE + 2 * SCALES * 1024;
-  static constexpr int NDMA = AM / 2 + BN / 2 + 1;                                  // instructions a wave and stage
+  static constexpr int LDS = RING * STAGE + SCALES * 1024;
+  static constexpr int NDMA = AM / 2 + BN / 2, NSC = (SCALES + 3) / 4;              // instructions a wave: a stage's, four steps' scales
   static constexpr int PER_CU = LDS <= 80 * 1024 ? 2 : 1;
+  static constexpr int UNROLL = RING == 4 ? 4 : 12;                                 // steps until ring and scales' bytes come round together
 };
 
 // The accumulator tied in place: through the builtin the compiler moves accumulators round the scaled op and runs at half its rate (4.9 against 7.1 PFLOP/s in a loop of nothing
@@ -105,10 +107,10 @@ __device__ __forceinline__ void mx4_ride(F&& f) {
 template <class Epi, int AM, int BN>
 __device__ __forceinline__ void mx4_tile(const Mx4Gemm& g, const typename Epi::Args& ea, char* smem, int tm, int tn) {
   using G = Mx4Geo<AM, BN>;
-  constexpr int D = G::NDMA, H1 = (D + 1) / 2, HB = BN / 2, HO = AM * HB;
+  constexpr int D = G::NDMA, H1 = (D + 1) / 2, HB = BN / 2, HO = AM * HB, R = G::RING;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wy = wave >> 1, wx = wave & 1;
   const int a_blocks = (g.M + 63) >> 6, b_blocks = (g.N + 63) >> 6, am = tm * (AM / 2), bm = tn * (BN / 2);   // in blocks of 64 rows
-  const int all = (g.A.steps + 3) >> 2;
+  const int all = (g.A.steps + 3) >> 2, n = g.steps, last = (n - 1) >> 2;   // steps; the last four steps' number
   const auto rsrc = [](const char* p) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), 0, -1, 0x00020000); };
   // (a block beyond the last one is read as the last: its results are not stored)
   const __amdgpu_buffer_rsrc_t ra = rsrc(g.A.codes + ((size_t)am * g.A.steps + g.first) * MX4_PANEL), rb = rsrc(g.B.codes + ((size_t)bm * g.B.steps + g.first) * MX4_PANEL);
@@ -124,36 +126,35 @@ __device__ __forceinline__ void mx4_tile(const Mx4Gemm& g, const typename Epi::A
     const int i = wave * (BN / 2) + j;
     ob[j] = (uint32_t)(min(bm + (i >> 2), b_blocks - 1) - bm) * (uint32_t)g.B.steps * MX4_PANEL + (i & 3) * 1024;
   }
-  const int n = g.steps, last = (n - 1) >> 2;                  // steps; the last four steps' number
-  char* const sc = smem + G::RING * G::STAGE;
-  // the KiB i of the scales of four steps
-  auto issue_scales = [&](int i, int S) {
-    const bool isb = i >= AM / 2;
-    const int blk = isb ? min(bm + i - AM / 2, b_blocks - 1) - bm : min(am + i, a_blocks - 1) - am;
-    const uint32_t off = ((uint32_t)blk * (uint32_t)all + (uint32_t)S) * 1024;
-    lds_char* const to = (lds_char*)(sc + ((S & 1) * G::SCALES + i) * 1024);
-    if (isb) __builtin_amdgcn_raw_ptr_buffer_load_lds(sb_r, to, 16, lane * 16, (int)off, 0, 0);
-    else __builtin_amdgcn_raw_ptr_buffer_load_lds(sa_r, to, 16, lane * 16, (int)off, 0, 0);
+  char* const sc = smem + R * G::STAGE;
+  // the wave's part of the scales of the four steps from 4 S on, a KiB an instruction (where there are fewer of them than waves, some are fetched twice)
+  auto issue_scales = [&](int S) {
+#pragma unroll
+    for (int j = 0; j < G::NSC; j++) {
+      const int i = (wave + 4 * j) % G::SCALES;
+      const bool isb = i >= AM / 2;
+      const int blk = isb ? min(bm + i - AM / 2, b_blocks - 1) - bm : min(am + i, a_blocks - 1) - am;
+      const uint32_t off = ((uint32_t)blk * (uint32_t)all + (uint32_t)min(S, last)) * 1024;
+      if (isb) __builtin_amdgcn_raw_ptr_buffer_load_lds(sb_r, (lds_char*)(sc + i * 1024), 16, lane * 16, (int)off, 0, 0);
+      else __builtin_amdgcn_raw_ptr_buffer_load_lds(sa_r, (lds_char*)(sc + i * 1024), 16, lane * 16, (int)off, 0, 0);
+    }
   };
-  // instruction J of stage kt
-  auto issue = [&](auto J, int kt, int slot) {                 // slot: kt & 3
+  // instruction J of stage kt into place `slot` of the ring
+  auto issue = [&](auto J, int kt, int slot) {
     constexpr int j = decltype(J)::value;
     char* const buf = smem + slot * G::STAGE;
     if constexpr (j < AM / 2) {
       __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_char*)(buf + (wave * (AM / 2) + j) * 1024), 16, lane * 16, (int)(oa[j < AM / 2 ? j : 0] + (uint32_t)kt * MX4_PANEL), 0, 0);
-    } else if constexpr (j < AM / 2 + BN / 2) {
+    } else {
       constexpr int i = j - AM / 2;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_char*)(buf + (2 * AM + wave * (BN / 2) + i) * 1024), 16, lane * 16, (int)(ob[i] + (uint32_t)kt * MX4_PANEL), 0, 0);
-    } else {
-      // a part of the next four steps' scales; the parts come round more often than there are any
-      issue_scales((4 * slot + wave) % G::SCALES, min((kt >> 2) + 1, last));
     }
   };
 
-  const bool full = n >= 4;
-  for (int i = wave; i < (G::SCALES + 3) / 4 * 4; i += 4) issue_scales(i % G::SCALES, 0);
-  for (int s = 0; s < min(n, 3); s++) static_for<D>([&](auto J) { issue(J, s, s); });
-  if (full) static_for<H1>([&](auto J) { issue(J, 3, 3); });
+  const bool full = n >= R;
+  issue_scales(0);
+  for (int s = 0; s < min(n, R - 1); s++) static_for<D>([&](auto J) { issue(J, s, s); });
+  if (full) static_for<H1>([&](auto J) { issue(J, R - 1, R - 1); });
 
   f32x4 acc[AM][BN];
 #pragma unroll
@@ -167,53 +168,56 @@ __device__ __forceinline__ void mx4_tile(const Mx4Gemm& g, const typename Epi::A
   uint32_t sa[AM], sb[BN];
   const char *la = smem + wy * AM * 1024 + lane * 16, *lb = smem + (2 * AM + wx * BN) * 1024 + lane * 16;
   const char *lsa = sc + wy * AM * 256 + lane * 4, *lsb = sc + (AM / 2) * 1024 + wx * BN * 256 + lane * 4;
-  auto read_scales = [&](int S, uint32_t (&xa)[AM], uint32_t (&xb)[BN]) {
-    const int at = (S & 1) * G::SCALES * 1024;
+  auto read_scales = [&](uint32_t (&xa)[AM], uint32_t (&xb)[BN]) {
 #pragma unroll
-    for (int t = 0; t < AM; t++) xa[t] = *reinterpret_cast<const uint32_t*>(lsa + at + t * 256);
+    for (int t = 0; t < AM; t++) xa[t] = *reinterpret_cast<const uint32_t*>(lsa + t * 256);
 #pragma unroll
-    for (int t = 0; t < BN; t++) xb[t] = *reinterpret_cast<const uint32_t*>(lsb + at + t * 256);
+    for (int t = 0; t < BN; t++) xb[t] = *reinterpret_cast<const uint32_t*>(lsb + t * 256);
   };
-  if (full) wait_vmcnt<2 * D + H1>(); else wait_vmcnt<0>();
+  if (full) wait_vmcnt<(R - 2) * D + H1>(); else wait_vmcnt<0>();
   __builtin_amdgcn_s_barrier();
   FFN24_FENCE();
   static_for<AM>([&](auto T) { a[T] = *reinterpret_cast<const u32x4*>(la + T * 1024); });
   static_for<HB>([&](auto T) { b[0][T] = *reinterpret_cast<const u32x4*>(lb + T * 1024); });
-  read_scales(0, sa, sb);
+  read_scales(sa, sb);
   FFN24_FENCE();
   asm volatile("s_nop 4" ::: "memory");
 
-  // The step of stage kt, the J-th of its four, in two halves as the 256 x 256 tile of gemm_core.hpp: the other half's B fragments are read during the first; then one
-  // barrier, behind which this stage's buffer is free; during the second the next step's fragments are read and the stage that reuses the buffer is asked for.
-  // TAIL: there may be no stage left to ask for, or to read (what is read then is not used).
+  // The step of stage kt (kt % UNROLL = J), in two halves as the 256 x 256 tile of gemm_core.hpp: the other half's B fragments are read during the first; then one barrier,
+  // behind which this stage's buffer is free; during the second the next step's fragments are read and the stage that reuses the buffer is asked for (the rest of
+  // it during the next step's first half).  The scales of four steps are read into registers during the last step before them; behind the next barrier their place is
+  // free, and the next four's are asked for.  TAIL: there may be no stage left to ask for, or to read (what is read then is not used).
   auto step = [&](int kt, auto j, auto tail) {
-    constexpr int J = decltype(j)::value, cur = J * G::STAGE, nxt = (J + 1) % 4 * G::STAGE;
+    constexpr int J = decltype(j)::value, S = J % 4, cur = J % R * G::STAGE, nxt = (J + 1) % R * G::STAGE;
     constexpr bool TAIL = decltype(tail)::value != 0;
-    const bool rest = !TAIL || kt + 3 < n, ask = !TAIL || kt + 4 < n;
+    // instructions behind the next stage's that may be in flight at the barrier: the scales went out with the stages 4 i + R
+    constexpr int LEFT = (R - 2) * D + ((S + 2) % 4 == R % 4 || (R == 4 && (S + 3) % 4 == 0) ? G::NSC : 0);
+    const bool rest = !TAIL || kt + R - 1 < n, ask = !TAIL || kt + R < n;
     FFN24_FENCE();
     static_for<HO>([&](auto M) {
       constexpr int mi = M / HB, ni = M % HB;
-      op16_mx4<J>(a[mi], b[0][ni], sa[mi], sb[ni], acc[mi][ni]);
+      op16_mx4<S>(a[mi], b[0][ni], sa[mi], sb[ni], acc[mi][ni]);
       mx4_early<HB, HO, M>([&](auto I) { b[1][I] = *reinterpret_cast<const u32x4*>(lb + cur + (HB + I) * 1024); });
-      mx4_ride<D - H1, HO, M>([&](auto I) { if (rest) issue(std::integral_constant<int, H1 + decltype(I)::value>{}, kt + 3, (J + 3) % 4); });
+      mx4_ride<D - H1, HO, M>([&](auto I) { if (rest) issue(std::integral_constant<int, H1 + decltype(I)::value>{}, kt + R - 1, (J + R - 1) % R); });
       FFN24_FENCE();
     });
-    if (rest && ask) wait_vmcnt<2 * D>(); else wait_vmcnt<0>();
+    if (rest && ask) wait_vmcnt<LEFT>(); else wait_vmcnt<0>();
     wait_lgkmcnt0();
     __builtin_amdgcn_s_barrier();
     FFN24_FENCE();
     uint32_t na[AM], nb[BN];
-    if constexpr (J == 3) read_scales((kt >> 2) + 1, na, nb);
+    if constexpr (S == 3) read_scales(na, nb);
+    if constexpr (S == 0) { if (ask) issue_scales((kt >> 2) + 1); }
     FFN24_FENCE();
     static_for<HO>([&](auto M) {
       constexpr int mi = M / HB, ni = M % HB;
-      op16_mx4<J>(a[mi], b[1][ni], sa[mi], sb[HB + ni], acc[mi][HB + ni]);
+      op16_mx4<S>(a[mi], b[1][ni], sa[mi], sb[HB + ni], acc[mi][HB + ni]);
       mx4_early<HB, HO, M>([&](auto I) { b[0][I] = *reinterpret_cast<const u32x4*>(lb + nxt + I * 1024); });
       if constexpr (ni == HB - 1) a[mi] = *reinterpret_cast<const u32x4*>(la + nxt + mi * 1024);
-      mx4_ride<H1, HO, M>([&](auto I) { if (ask) issue(I, kt + 4, J); });
+      mx4_ride<H1, HO, M>([&](auto I) { if (ask) issue(I, kt + R, J % R); });
       FFN24_FENCE();
     });
-    if constexpr (J == 3) {
+    if constexpr (S == 3) {
       // (a vector instruction may write an operand two states before its op at the latest)
 #pragma unroll
       for (int t = 0; t < AM; t++) sa[t] = na[t];
@@ -225,8 +229,8 @@ __device__ __forceinline__ void mx4_tile(const Mx4Gemm& g, const typename Epi::A
   };
   using I0 = std::integral_constant<int, 0>; using I1 = std::integral_constant<int, 1>;
   int kt = 0;
-  for (; kt + 8 <= n; kt += 4) static_for<4>([&](auto J) { step(kt + J, J, I0{}); });
-  while (kt < n) static_for<4>([&](auto J) {
+  for (; kt + G::UNROLL + R <= n; kt += G::UNROLL) static_for<G::UNROLL>([&](auto J) { step(kt + J, J, I0{}); });
+  while (kt < n) static_for<G::UNROLL>([&](auto J) {
     if (kt < n) {
       step(kt, J, I1{});
       kt++;
@@ -302,9 +306,12 @@ struct Mx4Part {   // the sums of a part of the reduction, [part][n][m]
 
 // The gated block: h = a(G) U of 32 features of a token lies in four lanes, 8 each; their largest magnitude gives the scale, and the codes go out as the down product reads
 // them: 16 tokens' 32 features are 256 bytes in a row.
+template <bool CUBIC>
 struct Mx4Gated {
   struct Args { char* codes; uint8_t* scales; int F, N, steps; Gate gate; };
   static __device__ __forceinline__ void part(Args&, int) {}
+  // without the cubic term the argument needs no hold: the exponential ends at 0 and infinity by itself
+  static __device__ __forceinline__ float act(const Gate& g, float x) { return CUBIC ? gate_act(g, x) : x * sigmoid(x); }
   template <int AM, int BN>
   static __device__ __forceinline__ void run(const Args& e, f32x4 (&acc)[AM][BN], int m, int n, int lane) {
     static_assert(AM % 4 == 0, "whole blocks of 64 rows a wave");
@@ -319,7 +326,7 @@ struct Mx4Gated {
         uint32_t top = 0u;
 #pragma unroll
         for (int v = 0; v < 8; v++) {
-          h[v] = gate_act(e.gate, acc[4 * i + v / 4][j][v % 4]) * acc[4 * i + 2 + v / 4][j][v % 4];
+          h[v] = act(e.gate, acc[4 * i + v / 4][j][v % 4]) * acc[4 * i + 2 + v / 4][j][v % 4];
           top = max(top, magnitude(h[v]));
         }
         top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
