@@ -44,7 +44,7 @@ struct moe_ctx {
   GateCoefficients gate;
   int renormalise, device, have_weights;
   MoeWeights w;
-  void *Wr, *up, *down, *parts, *H, *picks, *shares;
+  void *Wr, *up, *down, *X, *parts, *H, *picks, *shares;   // X, H: tokens and activations as mx4 (H: or bf16)
 };
 
 extern "C" {
@@ -159,12 +159,10 @@ int gated_mx4_fwd(gated_mx4_ctx* c, const void* X, int64_t T, void* Y, void* str
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int t = (int)T, D = (int)c->D, F = (int)c->F;
   const Mx4Operand wgu = mx4_operand(c->Wgu, 2 * F, D), wd = mx4_operand(c->Wd, D, F), x = mx4_operand(c->X, (int)c->T, D), h = mx4_operand(c->H, (int)c->T, F);
-  if (mx4_few_gated(t, D, F)) {
-    if (launch_few_mx4_up(wgu, X, t, D, F, c->gate.c1, c->gate.c3, h, s)) return FFN24_ERR_HIP;
-  } else {
-    if (launch_mx4_tokens(X, t, D, x, s)) return FFN24_ERR_HIP;
-    if (launch_mx4_gated_up(wgu, F, x, t, c->gate.c1, c->gate.c3, h, s)) return FFN24_ERR_HIP;
-  }
+  const bool few = mx4_few_gated(t, D, F), fused = few && mx4_few_fused(t);
+  if (!fused && launch_mx4_tokens(X, t, D, x, s)) return FFN24_ERR_HIP;
+  if (few ? launch_few_mx4_up(wgu, X, fused ? nullptr : &x, t, D, F, c->gate.c1, c->gate.c3, h, s)
+          : launch_mx4_gated_up(wgu, F, x, t, c->gate.c1, c->gate.c3, h, s)) return FFN24_ERR_HIP;
   if (mx4_few(t, F, D)) return done(launch_few_mx4_rows(wd, F, D, nullptr, &h, t, Y, s));
   return done(launch_mx4_product(wd, D, h, t, Y, c->scratch, s));
 }
@@ -178,11 +176,11 @@ int moe_ctx_create(moe_ctx** out, int64_t T, int64_t D, int64_t F, int64_t E, in
   c->T = T; c->D = D; c->F = F; c->E = E; c->k = k; c->gate = coefficients(gate); c->renormalise = renormalise != 0;
   const bool mx4 = type == FFN24_EXPERTS_MX4;
   const int64_t up = mx4 ? mx4_operand_size(2 * F, D) : bf16_operand_size(2 * F, D), down = mx4 ? mx4_operand_size(D, F) : bf16_operand_size(D, F);
-  // (of mx4 rows the k beyond F are zero for good: no kernel writes them)
+  // (of mx4 rows the k beyond D and F are zero for good: no kernel writes them)
   const bool ok = hipGetDevice(&c->device) == hipSuccess && hipMalloc(&c->Wr, (size_t)(2 * D * E)) == hipSuccess && hipMalloc(&c->up, (size_t)(E * up)) == hipSuccess &&
                   hipMalloc(&c->down, (size_t)(E * down)) == hipSuccess && hipMalloc(&c->parts, moe_parts_size((int)T, (int)D, (int)E)) == hipSuccess &&
                   hipMalloc(&c->picks, (size_t)(4 * T * k)) == hipSuccess && hipMalloc(&c->shares, (size_t)(4 * T * k)) == hipSuccess &&
-                  cleared(&c->H, mx4 ? mx4_operand_size(T * k, F) : 2 * T * k * F) && hipDeviceSynchronize() == hipSuccess;
+                  (!mx4 || cleared(&c->X, mx4_operand_size(T, D))) && cleared(&c->H, mx4 ? mx4_operand_size(T * k, F) : 2 * T * k * F) && hipDeviceSynchronize() == hipSuccess;
   if (!ok) {
     (void)hipGetLastError();
     moe_ctx_destroy(c);
@@ -197,7 +195,7 @@ int moe_ctx_create(moe_ctx** out, int64_t T, int64_t D, int64_t F, int64_t E, in
 int moe_ctx_destroy(moe_ctx* c) {
   if (!c) return FFN24_OK;
   int bad = 0;
-  for (void* p : {c->Wr, c->up, c->down, c->parts, c->H, c->picks, c->shares}) if (p && hipFree(p) != hipSuccess) bad = 1;
+  for (void* p : {c->Wr, c->up, c->down, c->X, c->parts, c->H, c->picks, c->shares}) if (p && hipFree(p) != hipSuccess) bad = 1;
   delete c;
   return bad ? FFN24_ERR_HIP : FFN24_OK;
 }
@@ -227,8 +225,9 @@ int moe_fwd(moe_ctx* c, const void* X, int64_t T, void* Y, void* experts, void* 
   const int t = (int)T, D = (int)c->D, F = (int)c->F, E = (int)c->E, k = (int)c->k;
   int* picks = static_cast<int*>(experts ? experts : c->picks);
   float* p = static_cast<float*>(experts ? shares : c->shares);
-  if (launch_moe_route(X, c->Wr, t, D, E, k, c->renormalise != 0, c->parts, picks, p, s)) return FFN24_ERR_HIP;
-  return done(launch_moe_experts(c->w, X, t, D, F, E, k, c->gate.c1, c->gate.c3, picks, p, c->H, (int)(c->T * k), Y, s));
+  const Mx4Operand x = mx4_operand(c->X, (int)c->T, D);
+  if (launch_moe_route(X, c->Wr, t, D, E, k, c->renormalise != 0, c->parts, picks, p, c->w.mx4 ? &x : nullptr, s)) return FFN24_ERR_HIP;
+  return done(launch_moe_experts(c->w, X, &x, t, D, F, E, k, c->gate.c1, c->gate.c3, picks, p, c->H, (int)(c->T * k), Y, s));
 }
 
 }  // extern "C"

@@ -22,95 +22,128 @@ __device__ __forceinline__ unsigned run_of(unsigned id, unsigned n) {
   return xcd * per + min(xcd, more) + (id >> 3);
 }
 
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }   // what is the same for the whole wave, in a scalar register
+
 // Where a wave's weights are: the strip's codes and scales, bytes from a step (four steps' scales) to the next
 struct Strip { const char* codes; const char* scales; int steps; };
 
-// U steps of RG groups of 16 channels
-template <bool MX4, int RG, int U>
-struct Weights {
-  static constexpr int SU = (U + 3) / 4;
-  u32x4 w[U][RG];
-  uint32_t s[MX4 ? SU : 1][MX4 ? RG : 1];
+// The scaled op with its accumulator in place, as in mx4_core.hpp (the builtin also keeps 32 bytes of registers for an operand of 16).  The compiler does not see what it needs: two
+// states behind the vector instructions that make its operands, and where the same accumulator comes round at once (RG 1), the op before it; settle() before results are read.
+template <int RG>
+__device__ __forceinline__ void op16_mx4_few(const u32x4& a, const u32x4& b, uint32_t sa, uint32_t sb, f32x4& c) {
+  if constexpr (RG == 1) asm volatile("s_nop 7\n\tv_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[0,0,0] op_sel_hi:[0,0,0] cbsz:4 blgp:4" : "+v"(c) : "v"(a), "v"(b), "v"(sa), "v"(sb));
+  else asm volatile("s_nop 1\n\tv_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[0,0,0] op_sel_hi:[0,0,0] cbsz:4 blgp:4" : "+v"(c) : "v"(a), "v"(b), "v"(sa), "v"(sb));
+}
+template <int RG, int NT>
+__device__ __forceinline__ void settle(f32x4 (&acc)[RG][NT]) {
+  asm volatile("s_nop 15" ::: "memory");
+#pragma unroll
+  for (int g = 0; g < RG; g++)
+#pragma unroll
+    for (int i = 0; i < NT; i++) asm volatile("" : "+v"(acc[g][i]));
+}
+
+// Tokens of a product: rows of bf16 [..][K] as they are, or to mx4 on the way; or the mx4 operand form
+enum { ROWS_BF16 = 0, ROWS_TO_MX4 = 1, OPERAND_MX4 = 2 };
+struct Tokens { const char* p; const char* scales; int K, steps; };
+
+// U steps of RG groups of 16 channels, and of the first NP groups of 16 tokens, on their way.  The tokens are asked for first: loads come back in order, so what is asked
+// for behind the weights would wait for them.
+template <int SRC, int RG, int U, int NP>
+struct Unit {
+  static constexpr bool MX4 = SRC != ROWS_BF16;
+  static constexpr int SU = MX4 ? (U + 3) / 4 : 1, XW = SRC == ROWS_TO_MX4 ? 4 : 1, KQ = MX4 ? 32 : 8, KS = 4 * KQ;
+  u32x4 w[U][RG], x[U][NP][XW];
+  uint32_t sw[SU][RG], sx[SRC == OPERAND_MX4 ? SU : 1][NP];
+
+  // the lane's words of token row `row` in step s
+  static __device__ __forceinline__ void token(const Tokens& t, int row, bool on, int s, int q, u32x4 (&x)[XW]) {
+    const int k = KS * s + KQ * q;
+#pragma unroll
+    for (int i = 0; i < XW; i++) x[i] = u32x4{0u, 0u, 0u, 0u};
+    if (!on) return;
+    if constexpr (SRC == OPERAND_MX4) {
+      x[0] = *reinterpret_cast<const u32x4*>(t.p + mx4_code_at(row, 4 * s + q, t.steps));
+    } else if (k < t.K) {
+#pragma unroll
+      for (int i = 0; i < XW; i++) x[i] = *reinterpret_cast<const u32x4*>(t.p + ((size_t)row * t.K + k + 8 * i) * 2);
+    }
+  }
+  static __device__ __forceinline__ uint32_t token_scales(const Tokens& t, int row, bool on, int s, int q) {   // of the four steps of s
+    return on ? *reinterpret_cast<const uint32_t*>(t.scales + (mx4_scale_at(row, 4 * s + q, t.steps) & ~(size_t)3)) : 0u;
+  }
   // from step s0 (a multiple of U) on; steps beyond the last read the last one and are not used
-  __device__ __forceinline__ void load(const Strip& p, int s0, int lane) {
+  __device__ __forceinline__ void load(const Strip& p, const Tokens& t, const int (&row)[NP], const bool (&on)[NP], int s0, int lane) {
+    const int q = lane >> 4;
 #pragma unroll
-    for (int j = 0; j < U; j++) {
-      const char* at = p.codes + (size_t)min(s0 + j, p.steps - 1) * MX4_PANEL + lane * 16;
+    for (int j = 0; j < U; j++)
 #pragma unroll
-      for (int g = 0; g < RG; g++) w[j][g] = ld_stream(reinterpret_cast<const u32x4*>(at + g * 1024));
+      for (int i = 0; i < NP; i++) token(t, row[i], on[i], min(s0 + j, p.steps - 1), q, x[j][i]);
+    if constexpr (SRC == OPERAND_MX4) {
+#pragma unroll
+      for (int j = 0; j < SU; j++)
+#pragma unroll
+        for (int i = 0; i < NP; i++) sx[j][i] = token_scales(t, row[i], on[i], min(s0 + 4 * j, p.steps - 1), q);
     }
     if constexpr (MX4) {
 #pragma unroll
       for (int j = 0; j < SU; j++) {
         const char* at = p.scales + (size_t)(min(s0 + 4 * j, p.steps - 1) >> 2) * 1024 + lane * 4;
 #pragma unroll
-        for (int g = 0; g < RG; g++) s[j][g] = *reinterpret_cast<const uint32_t*>(at + g * 256);
+        for (int g = 0; g < RG; g++) sw[j][g] = *reinterpret_cast<const uint32_t*>(at + g * 256);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < U; j++) {
+      const char* at = p.codes + (size_t)min(s0 + j, p.steps - 1) * MX4_PANEL + lane * 16;
+#pragma unroll
+      for (int g = 0; g < RG; g++) w[j][g] = ld_stream(reinterpret_cast<const u32x4*>(at + g * 1024));
+    }
+  }
+  template <int NT>
+  __device__ __forceinline__ void op(int j, int i, int s0, const u32x4 (&v)[XW], uint32_t scales, f32x4 (&acc)[RG][NT]) const {
+    if constexpr (!MX4) {
+#pragma unroll
+      for (int g = 0; g < RG; g++) acc[g][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w[j][g]), __builtin_bit_cast(bf16x8, v[0]), acc[g][i], 0, 0, 0);
+    } else {
+      const int byte = 8 * ((s0 + j) & 3);
+      i32x4 b;
+      uint32_t sb;
+      if constexpr (SRC == ROWS_TO_MX4) {
+        uint32_t top = 0u;
+#pragma unroll
+        for (int d = 0; d < 4; d++) top = i8_top8(v[d], top);
+        sb = mx4_scale_code(top);
+#pragma unroll
+        for (int d = 0; d < 4; d++) b[d] = (int)mx4_codes8(v[d], mx4_scale(sb));
+      } else {
+        b = __builtin_bit_cast(i32x4, v[0]);
+        sb = scales >> byte;
+      }
+#pragma unroll
+      for (int g = 0; g < RG; g++) op16_mx4_few<RG>(w[j][g], __builtin_bit_cast(u32x4, b), sw[j / 4][g] >> byte, sb, acc[g][i]);
+    }
+  }
+  // the ops of the unit for `groups` groups of tokens; those from NP on are asked for here
+  template <int NT>
+  __device__ __forceinline__ void ops(const Tokens& t, const int (&row)[NT], const bool (&on)[NT], int groups, int s0, int steps, int q, f32x4 (&acc)[RG][NT]) const {
+#pragma unroll
+    for (int j = 0; j < U; j++) {
+      if (s0 + j >= steps) break;
+#pragma unroll
+      for (int i = 0; i < NT; i++) {
+        if (i > 0 && i >= groups) break;
+        if (i < NP) {
+          op(j, i, s0, x[j][i < NP ? i : 0], sx[SRC == OPERAND_MX4 ? j / 4 : 0][i < NP ? i : 0], acc);
+        } else {
+          u32x4 v[XW];
+          token(t, row[i], on[i], s0 + j, q, v);
+          op(j, i, s0, v, SRC == OPERAND_MX4 ? token_scales(t, row[i], on[i], s0 + j, q) : 0u, acc);
+        }
       }
     }
   }
 };
-
-// Tokens of one step: an operand (and its scale) of 16 of them
-struct TokenOp { u32x4 x; uint32_t s; };
-// SRC 0: rows of bf16 as they are; 1: rows of bf16 to mx4; 2: the mx4 operand form
-enum { ROWS_BF16 = 0, ROWS_TO_MX4 = 1, OPERAND_MX4 = 2 };
-struct Tokens { const char* p; const char* scales; int K, steps; };   // rows [..][K], or codes and scales
-template <int SRC>
-__device__ __forceinline__ TokenOp token_op(const Tokens& t, int row, bool on, int step, int q) {
-  TokenOp o{{0u, 0u, 0u, 0u}, 0u};
-  if constexpr (SRC == ROWS_BF16) {
-    const int k = 32 * step + 8 * q;
-    if (on && k < t.K) o.x = *reinterpret_cast<const u32x4*>(t.p + ((size_t)row * t.K + k) * 2);
-  } else if constexpr (SRC == ROWS_TO_MX4) {
-    const int k = MX4_STEP * step + 32 * q;
-    if (on && k < t.K) {
-      const u32x4* p = reinterpret_cast<const u32x4*>(t.p + ((size_t)row * t.K + k) * 2);
-      u32x4 v[4];
-#pragma unroll
-      for (int i = 0; i < 4; i++) v[i] = p[i];
-      uint32_t top = 0u;
-#pragma unroll
-      for (int i = 0; i < 4; i++) top = i8_top8(v[i], top);
-      o.s = mx4_scale_code(top);
-      const float s = mx4_scale(o.s);
-#pragma unroll
-      for (int i = 0; i < 4; i++) o.x[i] = mx4_codes8(v[i], s);
-    }
-  } else {
-    if (on) {
-      o.x = *reinterpret_cast<const u32x4*>(t.p + mx4_code_at(row, 4 * step + q, t.steps));
-      o.s = static_cast<uint8_t>(t.scales[mx4_scale_at(row, 4 * step + q, t.steps)]);
-    }
-  }
-  return o;
-}
-
-template <bool MX4>
-__device__ __forceinline__ void few_op(const u32x4& w, uint32_t sw, const TokenOp& x, f32x4& acc) {
-  if constexpr (MX4) {
-    const i32x4 a = __builtin_bit_cast(i32x4, w), b = __builtin_bit_cast(i32x4, x.x);
-    acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(__builtin_shufflevector(a, a, 0, 1, 2, 3, -1, -1, -1, -1), __builtin_shufflevector(b, b, 0, 1, 2, 3, -1, -1, -1, -1), acc, 4, 4,
-                                                           0, (int)sw, 0, (int)x.s);
-  } else {
-    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, x.x), acc, 0, 0, 0);
-  }
-}
-// the ops of U steps for up to NT groups of 16 tokens; row[i]: the lane's row of group i, on[i]: whether there is one; groups: how many there are
-template <bool MX4, int SRC, int RG, int U, int NT>
-__device__ __forceinline__ void few_steps(const Weights<MX4, RG, U>& w, const Tokens& t, const int (&row)[NT], const bool (&on)[NT], int groups, int s0, int steps, int q,
-                                          f32x4 (&acc)[RG][NT]) {
-#pragma unroll
-  for (int j = 0; j < U; j++) {
-    if (s0 + j >= steps) break;
-#pragma unroll
-    for (int i = 0; i < NT; i++) {
-      if (NT > 1 && i >= groups) break;
-      const TokenOp x = token_op<SRC>(t, row[i], on[i], s0 + j, q);
-#pragma unroll
-      for (int g = 0; g < RG; g++) few_op<MX4>(w.w[j][g], MX4 ? w.s[MX4 ? j / 4 : 0][MX4 ? g : 0] >> (8 * ((s0 + j) & 3)) : 0u, x, acc[g][i]);
-    }
-  }
-}
 
 // The channel of a strip's row r (0 .. 16 RG - 1) from the strip's block of 64 on; g0: the strip's first group in its block
 __device__ __forceinline__ int channel_of(int g, int r) { return 32 * (g >> 1) + 8 * (r >> 2) + 4 * (g & 1) + (r & 3); }
@@ -119,6 +152,7 @@ __device__ __forceinline__ int channel_of(int g, int r) { return 32 * (g >> 1) +
 constexpr int MOE_E = 256, MOE_PAIRS = 1024;   // most experts; most (token, choice) pairs
 struct MoeLists {
   int count[MOE_E], at[MOE_E + 1], cursor[MOE_E], active[MOE_E], list[MOE_PAIRS], n_active;
+  float share[MOE_PAIRS];
 };
 // From the picks of all pairs: the chosen experts in ascending order, and each one's pairs.  (The order of an expert's pairs is as it comes: it says which column of
 // an op a token is, which no result depends on.)
@@ -165,15 +199,16 @@ struct UpArgs {
   size_t scales_at;                    // where an expert's scales start
   int steps, K, F, T;                  // steps of K; features
   Gate gate;
-  const char* x;                       // bf16 [T][K]
+  const char* x; const char* x_scales; // bf16 [T][K], or the operand form
   char* h; char* h_scales; int h_steps;   // bf16 rows [..][F], or the mx4 operand form
   const int* picks; int k;             // MOE: [T][k]
 };
 
 // grid (F / 32, slots).  A slot is a chosen expert; without MOE there is one, and it has all tokens.
-template <bool MX4, int NT, bool MOE>
-__global__ void __launch_bounds__(THREADS) few_up_kernel(UpArgs e) {
-  constexpr int RG = 4, U = 2, SRC = MX4 ? ROWS_TO_MX4 : ROWS_BF16;
+template <int SRC, int NT, bool MOE>
+__global__ void __launch_bounds__(THREADS, NT == 1 ? 4 : 2) few_up_kernel(UpArgs e) {
+  constexpr bool MX4 = SRC != ROWS_BF16;
+  constexpr int RG = 4, U = SRC == ROWS_TO_MX4 ? 1 : 2, NP = NT <= 2 ? NT : 1;
   __shared__ __attribute__((aligned(16))) float red[WAVES * 64 * RED];
   __shared__ MoeLists lists[MOE ? 1 : 1];
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, q = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -183,73 +218,80 @@ __global__ void __launch_bounds__(THREADS) few_up_kernel(UpArgs e) {
   if constexpr (MOE) {
     moe_lists(e.picks, e.T * e.k, lists[0]);
     if ((int)slot >= lists[0].n_active) return;
-    expert = lists[0].active[slot];
-    first = lists[0].at[expert];
-    n = lists[0].count[expert];
+    expert = uniform(lists[0].active[slot]);
+    first = uniform(lists[0].at[expert]);
+    n = uniform(lists[0].count[expert]);
   }
   const char* codes = e.w + (size_t)expert * e.w_stride;
   const Strip w{codes + (size_t)strip * e.steps * MX4_PANEL, codes + e.scales_at + (size_t)strip * ((e.steps + 3) >> 2) * 1024, e.steps};
-  const Tokens x{e.x, nullptr, e.K, 0};
+  const Tokens x{e.x, e.x_scales, e.K, e.steps};
 
-  for (int t0 = 0; t0 < n; t0 += 16 * NT) {
-    int row[NT];
-    bool on[NT];
+  // (no expert has more tokens than there are: T <= 16 NT)
+  int row[NT];
+  bool on[NT];
 #pragma unroll
-    for (int i = 0; i < NT; i++) {
-      const int at = t0 + 16 * i + c;
-      on[i] = at < n;
-      const int p = on[i] ? (MOE ? lists[0].list[first + at] : at) : 0;
-      row[i] = MOE ? p / e.k : p;
-    }
-    const int groups = min((n - t0 + 15) >> 4, NT);
-    f32x4 acc[RG][NT];
+  for (int i = 0; i < NT; i++) {
+    const int at = 16 * i + c;
+    on[i] = at < n;
+    const int p = on[i] ? (MOE ? lists[0].list[first + at] : at) : 0;
+    row[i] = MOE ? p / e.k : p;
+  }
+  const int groups = (n + 15) >> 4;
+  f32x4 acc[RG][NT];
 #pragma unroll
-    for (int g = 0; g < RG; g++)
+  for (int g = 0; g < RG; g++)
 #pragma unroll
-      for (int i = 0; i < NT; i++) acc[g][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    Weights<MX4, RG, U> now, next;
-    int s = wave * U;
-    if (s < e.steps) now.load(w, s, lane);
-    for (; s < e.steps; s += WAVES * U) {
-      const bool more = s + WAVES * U < e.steps;
-      if (more) next.load(w, s + WAVES * U, lane);
-      few_steps<MX4, SRC, RG, U, NT>(now, x, row, on, groups, s, e.steps, q, acc);
-      if (more) now = next;
-    }
-    for (int i = 0; i < groups; i++) {
-      __syncthreads();
+    for (int i = 0; i < NT; i++) acc[g][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  int row_p[NP];
+  bool on_p[NP];
 #pragma unroll
-      for (int j = 0; j < NT; j++)
-        if (j == i) {
+  for (int i = 0; i < NP; i++) {
+    row_p[i] = row[i];
+    on_p[i] = on[i];
+  }
+  Unit<SRC, RG, U, NP> now, next;
+  int s = wave * U;
+  if (s < e.steps) now.load(w, x, row_p, on_p, s, lane);
+  for (; s < e.steps; s += WAVES * U) {
+    const bool more = s + WAVES * U < e.steps;
+    if (more) next.load(w, x, row_p, on_p, s + WAVES * U, lane);
+    now.ops(x, row, on, groups, s, e.steps, q, acc);
+    if (more) now = next;
+  }
+  settle(acc);
+  for (int i = 0; i < groups; i++) {
+    __syncthreads();
 #pragma unroll
-          for (int g = 0; g < RG; g++)
+    for (int j = 0; j < NT; j++)
+      if (j == i) {
 #pragma unroll
-            for (int v = 0; v < 4; v++) red[(wave * 64 + 16 * g + 4 * q + v) * RED + c] = acc[g][j][v];
-        }
-      __syncthreads();
-      // 32 neighbouring lanes have the features of a token
-      const int f = tid & 31, tok = tid >> 5, r = ((f >> 2) & 1) * 16 + 4 * (f >> 3) + (f & 3), at = t0 + 16 * i + tok;
-      float gate = 0.f, up = 0.f;
+        for (int g = 0; g < RG; g++)
 #pragma unroll
-      for (int k = 0; k < WAVES; k++) {
-        gate += red[(k * 64 + r) * RED + tok];
-        up += red[(k * 64 + 32 + r) * RED + tok];
+          for (int v = 0; v < 4; v++) red[(wave * 64 + 16 * g + 4 * q + v) * RED + c] = acc[g][j][v];
       }
-      const float h = gate_act(e.gate, gate) * up;
-      const int dest = at < n ? (MOE ? lists[0].list[first + at] : at) : 0;
-      if constexpr (MX4) {
-        uint32_t top = magnitude(h);
+    __syncthreads();
+    // 32 neighbouring lanes have the features of a token
+    const int f = tid & 31, tok = tid >> 5, r = ((f >> 2) & 1) * 16 + 4 * (f >> 3) + (f & 3), at = 16 * i + tok;
+    float gate = 0.f, up = 0.f;
 #pragma unroll
-        for (int d = 1; d < 32; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
-        const uint32_t code = mx4_scale_code(top);
-        uint32_t word = (__builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, h, 0.f, mx4_scale(code), 0) & 15u) << (4 * (f & 7));
+    for (int k = 0; k < WAVES; k++) {
+      gate += red[(k * 64 + r) * RED + tok];
+      up += red[(k * 64 + 32 + r) * RED + tok];
+    }
+    const float h = gate_act(e.gate, gate) * up;
+    const int dest = at < n ? (MOE ? lists[0].list[first + at] : at) : 0;
+    if constexpr (MX4) {
+      uint32_t top = magnitude(h);
 #pragma unroll
-        for (int d = 1; d < 8; d <<= 1) word |= (uint32_t)__shfl_xor((int)word, d, 64);
-        if (at < n && (f & 7) == 0) *reinterpret_cast<uint32_t*>(e.h + mx4_code_at(dest, strip, e.h_steps) + (f >> 1)) = word;
-        if (at < n && f == 0) e.h_scales[mx4_scale_at(dest, strip, e.h_steps)] = (char)code;
-      } else {
-        if (at < n) reinterpret_cast<uint16_t*>(e.h)[(size_t)dest * e.F + 32 * strip + f] = (uint16_t)pack_bf16x2(h, 0.f);
-      }
+      for (int d = 1; d < 32; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
+      const uint32_t code = mx4_scale_code(top);
+      uint32_t word = (__builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, h, 0.f, mx4_scale(code), 0) & 15u) << (4 * (f & 7));
+#pragma unroll
+      for (int d = 1; d < 8; d <<= 1) word |= (uint32_t)__shfl_xor((int)word, d, 64);
+      if (at < n && (f & 7) == 0) *reinterpret_cast<uint32_t*>(e.h + mx4_code_at(dest, strip, e.h_steps) + (f >> 1)) = word;
+      if (at < n && f == 0) e.h_scales[mx4_scale_at(dest, strip, e.h_steps)] = (char)code;
+    } else {
+      if (at < n) reinterpret_cast<uint16_t*>(e.h)[(size_t)dest * e.F + 32 * strip + f] = (uint16_t)pack_bf16x2(h, 0.f);
     }
   }
 }
@@ -260,9 +302,9 @@ struct RowsArgs {
   const char* x; const char* x_scales; int x_steps;
   uint16_t* out;
 };
-template <bool MX4, int RG, int NT, int SRC>
-__global__ void __launch_bounds__(THREADS) few_rows_kernel(RowsArgs e) {
-  constexpr int U = SRC == ROWS_TO_MX4 && RG == 1 ? 4 : 8 / RG;
+template <int RG, int NT, int SRC>
+__global__ void __launch_bounds__(THREADS, NT == 1 && (RG > 1 || SRC == ROWS_TO_MX4) ? 4 : 2) few_rows_kernel(RowsArgs e) {
+  constexpr int U = SRC == ROWS_TO_MX4 ? (RG == 4 ? 1 : 2) : RG == 1 ? 8 : RG == 2 ? 4 : 2;
   __shared__ __attribute__((aligned(16))) float red[WAVES * 16 * RG * RED];
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, q = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int strip = (int)run_of(blockIdx.x, gridDim.x), block = strip / (4 / RG), g0 = strip % (4 / RG) * RG;
@@ -280,15 +322,16 @@ __global__ void __launch_bounds__(THREADS) few_rows_kernel(RowsArgs e) {
   for (int g = 0; g < RG; g++)
 #pragma unroll
     for (int i = 0; i < NT; i++) acc[g][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  Weights<MX4, RG, U> now, next;
+  Unit<SRC, RG, U, NT> now, next;
   int s = wave * U;
-  if (s < e.steps) now.load(w, s, lane);
+  if (s < e.steps) now.load(w, x, row, on, s, lane);
   for (; s < e.steps; s += WAVES * U) {
     const bool more = s + WAVES * U < e.steps;
-    if (more) next.load(w, s + WAVES * U, lane);
-    few_steps<MX4, SRC, RG, U, NT>(now, x, row, on, NT, s, e.steps, q, acc);
+    if (more) next.load(w, x, row, on, s + WAVES * U, lane);
+    now.ops(x, row, on, NT, s, e.steps, q, acc);
     if (more) now = next;
   }
+  settle(acc);
 #pragma unroll
   for (int i = 0; i < NT; i++) {
     if (i > 0) __syncthreads();
@@ -320,56 +363,74 @@ constexpr int down_lds(int T) { return WAVES * T * SUM * 4; }
 
 // grid (D / 16)
 template <bool MX4, int NT>
-__global__ void __launch_bounds__(THREADS) moe_down_kernel(DownArgs e) {
+__global__ void __launch_bounds__(THREADS, 2) moe_down_kernel(DownArgs e) {
   constexpr int U = 8, SRC = MX4 ? OPERAND_MX4 : ROWS_BF16;
   extern __shared__ __attribute__((aligned(16))) float sums[];   // [wave][token][SUM]
   __shared__ MoeLists lists;
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, q = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int strip = (int)run_of(blockIdx.x, gridDim.x), block = strip >> 2, g0 = strip & 3;
   for (int i = tid; i < WAVES * e.T * SUM; i += THREADS) sums[i] = 0.f;
+  for (int i = tid; i < e.T * e.k; i += THREADS) lists.share[i] = e.shares[i];
   moe_lists(e.picks, e.T * e.k, lists);
   float* mine = sums + wave * e.T * SUM;
   const Tokens x{e.h, e.h_scales, e.F, e.h_steps};
-  const int units = (e.steps + U - 1) / U, total = lists.n_active * units;   // units of U steps, the experts' one after the other, dealt out to the waves
+  const int units = (e.steps + U - 1) / U, total = uniform(lists.n_active) * units;   // units of U steps, the experts' one after the other, dealt out to the waves
   auto strip_of = [&](int i, int& expert) {
-    expert = lists.active[i / units];
+    expert = uniform(lists.active[i / units]);
     const char* codes = e.w + (size_t)expert * e.w_stride;
     return Strip{codes + (size_t)block * e.steps * MX4_PANEL + g0 * 1024, codes + e.scales_at + (size_t)block * ((e.steps + 3) >> 2) * 1024 + g0 * 256, e.steps};
   };
-  Weights<MX4, 1, U> now, next;
-  int i = wave, expert = 0;
-  if (i < total) now.load(strip_of(i, expert), i % units * U, lane);
+  // the lane's rows of the first 16 of an expert's tokens
+  auto first_rows = [&](int expert, int (&row)[1], bool (&on)[1]) {
+    on[0] = c < lists.count[expert];
+    row[0] = on[0] ? lists.list[lists.at[expert] + c] : 0;
+  };
+  Unit<SRC, 1, U, 1> now, next;
+  int i = wave, expert = 0, row_n[1], row_f[1];
+  bool on_n[1], on_f[1];
+  if (i < total) {
+    const Strip w = strip_of(i, expert);
+    first_rows(expert, row_f, on_f);
+    now.load(w, x, row_f, on_f, i % units * U, lane);
+  }
   for (; i < total; i += WAVES) {
     const bool more = i + WAVES < total;
     int then = 0;
-    if (more) next.load(strip_of(i + WAVES, then), (i + WAVES) % units * U, lane);
-    const int n = lists.count[expert], first = lists.at[expert];
-    for (int t0 = 0; t0 < n; t0 += 16 * NT) {
-      int row[NT];
-      bool on[NT];
-#pragma unroll
-      for (int g = 0; g < NT; g++) {
-        const int at = t0 + 16 * g + c;
-        on[g] = at < n;
-        row[g] = on[g] ? lists.list[first + at] : 0;
-      }
-      f32x4 acc[1][NT];
-#pragma unroll
-      for (int g = 0; g < NT; g++) acc[0][g] = f32x4{0.f, 0.f, 0.f, 0.f};
-      few_steps<MX4, SRC, 1, U, NT>(now, x, row, on, min((n - t0 + 15) >> 4, NT), i % units * U, e.steps, q, acc);
-#pragma unroll
-      for (int g = 0; g < NT; g++)
-        if (on[g]) {                                       // (a token chooses an expert once: no two lanes of a quarter have the same one)
-          const float p = e.shares[row[g]];
-          f32x4* to = reinterpret_cast<f32x4*>(mine + row[g] / e.k * SUM + 4 * q);
-          f32x4 y = *to;
-#pragma unroll
-          for (int v = 0; v < 4; v++) y[v] += p * acc[0][g][v];
-          *to = y;
-        }
+    if (more) {
+      const Strip w = strip_of(i + WAVES, then);
+      first_rows(then, row_n, on_n);
+      next.load(w, x, row_n, on_n, (i + WAVES) % units * U, lane);
     }
+    const int n = uniform(lists.count[expert]), first = uniform(lists.at[expert]), groups = (n + 15) >> 4;
+    int row[NT];
+    bool on[NT];
+    row[0] = row_f[0];
+    on[0] = on_f[0];
+#pragma unroll
+    for (int g = 1; g < NT; g++) {
+      const int at = 16 * g + c;
+      on[g] = at < n;
+      row[g] = on[g] ? lists.list[first + at] : 0;
+    }
+    f32x4 acc[1][NT];
+#pragma unroll
+    for (int g = 0; g < NT; g++) acc[0][g] = f32x4{0.f, 0.f, 0.f, 0.f};
+    now.ops(x, row, on, groups, i % units * U, e.steps, q, acc);
+    settle(acc);
+#pragma unroll
+    for (int g = 0; g < NT; g++)
+      if (on[g]) {                                         // (a token chooses an expert once: no two lanes of a quarter have the same one)
+        const float p = lists.share[row[g]];
+        f32x4* to = reinterpret_cast<f32x4*>(mine + row[g] / e.k * SUM + 4 * q);
+        f32x4 y = *to;
+#pragma unroll
+        for (int v = 0; v < 4; v++) y[v] += p * acc[0][g][v];
+        *to = y;
+      }
     if (more) now = next;
     expert = then;
+    row_f[0] = row_n[0];
+    on_f[0] = on_n[0];
   }
   __syncthreads();
   for (int o = tid; o < 16 * e.T; o += THREADS) {
@@ -384,10 +445,19 @@ __global__ void __launch_bounds__(THREADS) moe_down_kernel(DownArgs e) {
 // ------------------------------------------------------------------------------------------------ router
 constexpr int ROUTE_D = 64, ROUTE_T = 8;   // of D and of the tokens a workgroup
 // grid (D / 64, T / 8); parts [D / 64][T][E]
-__global__ void __launch_bounds__(256) moe_router_kernel(const uint16_t* __restrict__ X, const uint16_t* __restrict__ Wr, int T, int D, int E, double* __restrict__ parts) {
+// steps > 0: the tokens go out as mx4 too, in the operand form
+__global__ void __launch_bounds__(256) moe_router_kernel(const uint16_t* __restrict__ X, const uint16_t* __restrict__ Wr, int T, int D, int E, double* __restrict__ parts, int steps,
+                                                         char* __restrict__ codes, char* __restrict__ scales) {
   __shared__ float x[ROUTE_T][ROUTE_D];
   __shared__ double sums[256 * ROUTE_T];
   const int tid = threadIdx.x, d0 = blockIdx.x * ROUTE_D, t0 = blockIdx.y * ROUTE_T, tokens = min(T - t0, ROUTE_T);
+  if (steps > 0 && tid < 8 * tokens) {                         // four lanes have a block of 32
+    const int t = t0 + tid / 8, d = d0 + 8 * (tid & 7), p = tid & 3;
+    const u32x4 w = *reinterpret_cast<const u32x4*>(X + (size_t)t * D + d);
+    const uint32_t code = mx4_scale_code(quad_max(i8_top8(w, 0u)));
+    *reinterpret_cast<uint32_t*>(codes + mx4_code_at(t, d >> 5, steps) + 4 * p) = mx4_codes8(w, mx4_scale(code));
+    if (p == 0) scales[mx4_scale_at(t, d >> 5, steps)] = (char)code;
+  }
   for (int i = tid; i < tokens * ROUTE_D; i += 256) x[i / ROUTE_D][i % ROUTE_D] = bf16_lo_to_f32(X[(size_t)(t0 + i / ROUTE_D) * D + d0 + i % ROUTE_D]);
   __syncthreads();
   const int ways = 256 / E, way = tid / E, ex = tid - way * E;   // the rows of Wr are dealt out to `ways` groups of E work items
@@ -454,11 +524,12 @@ __global__ void __launch_bounds__(256) moe_pick_kernel(const double* __restrict_
   if (rank < k) shares[t * k + rank] = x / (part[0] + part[1] + part[2] + part[3]);
 }
 
-template <int NT, bool MOE>
-int launch_up(const UpArgs& a, bool mx4, int slots, hipStream_t s) {
+template <int SRC, bool MOE>
+int launch_up(const UpArgs& a, int slots, hipStream_t s) {
   const dim3 grid((unsigned)(a.F / 32), (unsigned)slots);
-  if (mx4) hipLaunchKernelGGL((few_up_kernel<true, NT, MOE>), grid, dim3(THREADS), 0, s, a);
-  else hipLaunchKernelGGL((few_up_kernel<false, NT, MOE>), grid, dim3(THREADS), 0, s, a);
+  if (a.T <= 16) hipLaunchKernelGGL((few_up_kernel<SRC, 1, MOE>), grid, dim3(THREADS), 0, s, a);
+  else if (a.T <= 32 || !MOE) hipLaunchKernelGGL((few_up_kernel<SRC, 2, MOE>), grid, dim3(THREADS), 0, s, a);
+  else hipLaunchKernelGGL((few_up_kernel<SRC, MOE ? 4 : 2, MOE>), grid, dim3(THREADS), 0, s, a);
   return (int)hipGetLastError();
 }
 template <bool MX4, int NT>
@@ -472,36 +543,36 @@ int launch_down(const DownArgs& a, hipStream_t s) {
 template <int RG, int SRC>
 int launch_rows(const RowsArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)(RG == 1 ? (a.N + 31) / 32 * 2 : (a.N + 16 * RG - 1) / (16 * RG)));   // (two groups of 16 share 32 channels)
-  if (a.T <= 16) hipLaunchKernelGGL((few_rows_kernel<true, RG, 1, SRC>), grid, dim3(THREADS), 0, s, a);
-  else hipLaunchKernelGGL((few_rows_kernel<true, RG, 2, SRC>), grid, dim3(THREADS), 0, s, a);
+  if (a.T <= 16) hipLaunchKernelGGL((few_rows_kernel<RG, 1, SRC>), grid, dim3(THREADS), 0, s, a);
+  else hipLaunchKernelGGL((few_rows_kernel<RG, 2, SRC>), grid, dim3(THREADS), 0, s, a);
   return (int)hipGetLastError();
 }
 }  // namespace
 
 size_t moe_parts_size(int T, int D, int E) { return (size_t)(D / ROUTE_D) * T * E * sizeof(double); }
 
-int launch_moe_route(const void* X, const void* Wr, int T, int D, int E, int k, bool renormalise, void* parts, int* picks, float* shares, hipStream_t s) {
+int launch_moe_route(const void* X, const void* Wr, int T, int D, int E, int k, bool renormalise, void* parts, int* picks, float* shares, const Mx4Operand* x, hipStream_t s) {
   const int n = D / ROUTE_D;
   hipLaunchKernelGGL(moe_router_kernel, dim3((unsigned)n, (unsigned)((T + ROUTE_T - 1) / ROUTE_T)), dim3(256), 0, s, static_cast<const uint16_t*>(X),
-                     static_cast<const uint16_t*>(Wr), T, D, E, static_cast<double*>(parts));
+                     static_cast<const uint16_t*>(Wr), T, D, E, static_cast<double*>(parts), x ? x->steps : 0, x ? const_cast<char*>(x->codes) : nullptr,
+                     x ? const_cast<char*>(x->scales) : nullptr);
   hipLaunchKernelGGL(moe_pick_kernel, dim3((unsigned)T), dim3(256), 0, s, static_cast<const double*>(parts), n, T, E, k, (int)renormalise, picks, shares);
   return (int)hipGetLastError();
 }
 
-int launch_moe_experts(const MoeWeights& w, const void* X, int T, int D, int F, int E, int k, float c1, float c3, const int* picks, const float* shares, void* H, int h_rows,
-                       void* Y, hipStream_t s) {
+int launch_moe_experts(const MoeWeights& w, const void* X, const Mx4Operand* x, int T, int D, int F, int E, int k, float c1, float c3, const int* picks, const float* shares,
+                       void* H, int h_rows, void* Y, hipStream_t s) {
   UpArgs up{};
   up.w = static_cast<const char*>(w.up); up.w_stride = w.up_stride; up.scales_at = w.up_scales;
   up.K = D; up.F = F; up.T = T; up.steps = w.mx4 ? mx4_steps(D) : D / 32; up.gate = Gate{c1, c3};
-  up.x = static_cast<const char*>(X);
+  up.x = w.mx4 ? x->codes : static_cast<const char*>(X); up.x_scales = w.mx4 ? x->scales : nullptr;
   const Mx4Operand h = mx4_operand(H, h_rows, F);
   up.h = const_cast<char*>(w.mx4 ? h.codes : static_cast<const char*>(H));
   up.h_scales = const_cast<char*>(h.scales);
   up.h_steps = h.steps;
   up.picks = picks; up.k = k;
   const int slots = T * k < E ? T * k : E;
-  const int rc = T <= 16 ? launch_up<1, true>(up, w.mx4, slots, s) : T <= 32 ? launch_up<2, true>(up, w.mx4, slots, s) : launch_up<4, true>(up, w.mx4, slots, s);
-  if (rc) return rc;
+  if (const int rc = w.mx4 ? launch_up<OPERAND_MX4, true>(up, slots, s) : launch_up<ROWS_BF16, true>(up, slots, s)) return rc;
   DownArgs d{};
   d.w = static_cast<const char*>(w.down); d.w_stride = w.down_stride; d.scales_at = w.down_scales;
   d.steps = w.mx4 ? mx4_steps(F) : F / 32; d.F = F; d.D = D; d.T = T; d.k = k;
@@ -511,13 +582,14 @@ int launch_moe_experts(const MoeWeights& w, const void* X, int T, int D, int F, 
   return w.mx4 ? launch_down<true, 4>(d, s) : launch_down<false, 4>(d, s);
 }
 
-int launch_few_mx4_up(const Mx4Operand& w, const void* X, int T, int D, int F, float c1, float c3, const Mx4Operand& h, hipStream_t s) {
+// X: bf16 rows; x: instead of them
+int launch_few_mx4_up(const Mx4Operand& w, const void* X, const Mx4Operand* x, int T, int D, int F, float c1, float c3, const Mx4Operand& h, hipStream_t s) {
   UpArgs up{};
   up.w = w.codes; up.scales_at = (size_t)(w.scales - w.codes);
   up.K = D; up.F = F; up.T = T; up.steps = w.steps; up.gate = Gate{c1, c3};
-  up.x = static_cast<const char*>(X);
+  up.x = x ? x->codes : static_cast<const char*>(X); up.x_scales = x ? x->scales : nullptr;
   up.h = const_cast<char*>(h.codes); up.h_scales = const_cast<char*>(h.scales); up.h_steps = h.steps;
-  return T <= 16 ? launch_up<1, false>(up, true, 1, s) : launch_up<2, false>(up, true, 1, s);
+  return x ? launch_up<OPERAND_MX4, false>(up, 1, s) : launch_up<ROWS_TO_MX4, false>(up, 1, s);
 }
 // Strips of 64, 32 or 16 channels: at least 512 workgroups if there are that many
 int launch_few_mx4_rows(const Mx4Operand& w, int K, int N, const void* X, const Mx4Operand* x, int T, void* Y, hipStream_t s) {

@@ -8,9 +8,6 @@
 namespace ffn24 {
 namespace {
 
-template <int P> __device__ __forceinline__ uint32_t quad_max(uint32_t x) { return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, P, 0xF, 0xF, true)); }
-__device__ __forceinline__ uint32_t quad_max(uint32_t x) { return quad_max<quad_perm(2, 3, 0, 1)>(quad_max<quad_perm(1, 0, 3, 2)>(x)); }
-
 // Eight values of a row: as bf16 or fp32 in memory
 template <bool F32> struct Eight;
 template <> struct Eight<false> {

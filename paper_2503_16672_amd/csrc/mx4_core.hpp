@@ -47,6 +47,9 @@ __device__ __forceinline__ uint32_t mx4_codes8(const float (&x)[8], float s) {
 }
 __device__ __forceinline__ uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7FFFFFFFu; }
 
+template <int P> __device__ __forceinline__ uint32_t quad_max(uint32_t x) { return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, P, 0xF, 0xF, true)); }
+__device__ __forceinline__ uint32_t quad_max(uint32_t x) { return quad_max<quad_perm(2, 3, 0, 1)>(quad_max<quad_perm(1, 0, 3, 2)>(x)); }   // over the lanes of a quad
+
 // Where row r's codes of the 32 k [32 kb, ...) start, and the byte of their scale
 __device__ __forceinline__ size_t mx4_code_at(int r, int kb, int steps) {
   return ((size_t)(r >> 6) * steps + (kb >> 2)) * MX4_PANEL + ((r >> 4) & 3) * 1024 + (((kb & 3) << 4) + (r & 15)) * 16;
