@@ -44,7 +44,7 @@ struct moe_ctx {
   GateCoefficients gate;
   int renormalise, device, have_weights;
   MoeWeights w;
-  void *Wr, *up, *down, *X, *parts, *H, *picks, *shares;   // X, H: tokens and activations as mx4 (H: or bf16)
+  void *Wr, *up, *down, *X, *parts, *plan, *H, *picks, *shares;   // X, H: tokens and activations as mx4 (H: or bf16)
 };
 
 extern "C" {
@@ -180,7 +180,7 @@ int moe_ctx_create(moe_ctx** out, int64_t T, int64_t D, int64_t F, int64_t E, in
   const bool ok = hipGetDevice(&c->device) == hipSuccess && hipMalloc(&c->Wr, (size_t)(2 * D * E)) == hipSuccess && hipMalloc(&c->up, (size_t)(E * up)) == hipSuccess &&
                   hipMalloc(&c->down, (size_t)(E * down)) == hipSuccess && hipMalloc(&c->parts, moe_parts_size((int)T, (int)D, (int)E)) == hipSuccess &&
                   hipMalloc(&c->picks, (size_t)(4 * T * k)) == hipSuccess && hipMalloc(&c->shares, (size_t)(4 * T * k)) == hipSuccess &&
-                  (!mx4 || cleared(&c->X, mx4_operand_size(T, D))) && cleared(&c->H, mx4 ? mx4_operand_size(T * k, F) : 2 * T * k * F) && hipDeviceSynchronize() == hipSuccess;
+                  cleared(&c->plan, (int64_t)moe_plan_size()) && (!mx4 || cleared(&c->X, mx4_operand_size(T, D))) && cleared(&c->H, mx4 ? mx4_operand_size(T * k, F) : 2 * T * k * F) && hipDeviceSynchronize() == hipSuccess;
   if (!ok) {
     (void)hipGetLastError();
     moe_ctx_destroy(c);
@@ -195,7 +195,7 @@ int moe_ctx_create(moe_ctx** out, int64_t T, int64_t D, int64_t F, int64_t E, in
 int moe_ctx_destroy(moe_ctx* c) {
   if (!c) return FFN24_OK;
   int bad = 0;
-  for (void* p : {c->Wr, c->up, c->down, c->X, c->parts, c->H, c->picks, c->shares}) if (p && hipFree(p) != hipSuccess) bad = 1;
+  for (void* p : {c->Wr, c->up, c->down, c->X, c->parts, c->plan, c->H, c->picks, c->shares}) if (p && hipFree(p) != hipSuccess) bad = 1;
   delete c;
   return bad ? FFN24_ERR_HIP : FFN24_OK;
 }
@@ -226,8 +226,8 @@ int moe_fwd(moe_ctx* c, const void* X, int64_t T, void* Y, void* experts, void* 
   int* picks = static_cast<int*>(experts ? experts : c->picks);
   float* p = static_cast<float*>(experts ? shares : c->shares);
   const Mx4Operand x = mx4_operand(c->X, (int)c->T, D);
-  if (launch_moe_route(X, c->Wr, t, D, E, k, c->renormalise != 0, c->parts, picks, p, c->w.mx4 ? &x : nullptr, s)) return FFN24_ERR_HIP;
-  return done(launch_moe_experts(c->w, X, &x, t, D, F, E, k, c->gate.c1, c->gate.c3, picks, p, c->H, (int)(c->T * k), Y, s));
+  if (launch_moe_route(X, c->Wr, t, D, E, k, c->renormalise != 0, c->parts, picks, p, c->plan, c->w.mx4 ? &x : nullptr, s)) return FFN24_ERR_HIP;
+  return done(launch_moe_experts(c->w, X, &x, t, D, F, E, k, c->gate.c1, c->gate.c3, c->plan, c->H, (int)(c->T * k), Y, s));
 }
 
 }  // extern "C"

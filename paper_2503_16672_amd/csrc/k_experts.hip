@@ -149,49 +149,18 @@ struct Unit {
 __device__ __forceinline__ int channel_of(int g, int r) { return 32 * (g >> 1) + 8 * (r >> 2) + 4 * (g & 1) + (r & 3); }
 
 // ------------------------------------------------------------------------------------------------ experts' lists
-constexpr int MOE_E = 256, MOE_PAIRS = 1024;   // most experts; most (token, choice) pairs
-struct MoeLists {
-  int count[MOE_E], at[MOE_E + 1], cursor[MOE_E], active[MOE_E], list[MOE_PAIRS], n_active;
+constexpr int MOE_E = MOE_MAX_E, MOE_PAIRS = MOE_TOKENS * MOE_MAX_K;   // most experts; most (token, choice) pairs
+// The chosen experts in ascending order; the pairs of the i-th are list[start[i]] .. list[start[i + 1] - 1], with their shares beside them.  (The order of an expert's pairs
+// is as it comes: it says which column of an op a token is, which no result depends on.)
+struct MoePlan {
+  int ticket, n_active, expert[MOE_E], start[MOE_E + 2], list[MOE_PAIRS];
   float share[MOE_PAIRS];
+  int picks[MOE_PAIRS];                // on their way to the plan
+  float shares[MOE_PAIRS];
 };
-// From the picks of all pairs: the chosen experts in ascending order, and each one's pairs.  (The order of an expert's pairs is as it comes: it says which column of
-// an op a token is, which no result depends on.)
-__device__ __forceinline__ void moe_lists(const int* __restrict__ picks, int pairs, MoeLists& l) {
-  const int tid = threadIdx.x;
-  if (tid < MOE_E) l.count[tid] = 0;
-  __syncthreads();
-  for (int p = tid; p < pairs; p += THREADS) atomicAdd(&l.count[picks[p]], 1);
-  __syncthreads();
-  if (tid < 64) {                                              // four experts a lane
-    int n[4], sum = 0;
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-      n[i] = l.count[4 * tid + i];
-      sum += n[i] | (n[i] > 0 ? 1 << 16 : 0);                  // pairs below, chosen experts above
-    }
-    int upto = sum;
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) {
-      const int x = __shfl_up(upto, s, 64);
-      if (tid >= s) upto += x;
-    }
-    int run = upto - sum;
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-      const int e = 4 * tid + i;
-      l.at[e] = l.cursor[e] = run & 0xFFFF;
-      if (n[i] > 0) l.active[run >> 16] = e;
-      run += n[i] | (n[i] > 0 ? 1 << 16 : 0);
-    }
-    if (tid == 63) {
-      l.at[MOE_E] = run & 0xFFFF;
-      l.n_active = run >> 16;
-    }
-  }
-  __syncthreads();
-  for (int p = tid; p < pairs; p += THREADS) l.list[atomicAdd(&l.cursor[picks[p]], 1)] = p;
-  __syncthreads();
-}
+// Words that workgroups of a launch hand to each other go past the XCDs' own L2s (agent scope); what was stored so is there once the storing wave has waited for it.
+template <class T> __device__ __forceinline__ void put(T* p, T x) { __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+template <class T> __device__ __forceinline__ T get(const T* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
 // ------------------------------------------------------------------------------------------------ up
 struct UpArgs {
@@ -201,7 +170,7 @@ struct UpArgs {
   Gate gate;
   const char* x; const char* x_scales; // bf16 [T][K], or the operand form
   char* h; char* h_scales; int h_steps;   // bf16 rows [..][F], or the mx4 operand form
-  const int* picks; int k;             // MOE: [T][k]
+  const MoePlan* plan; int k;          // MOE
 };
 
 // grid (F / 32, slots).  A slot is a chosen expert; without MOE there is one, and it has all tokens.
@@ -210,17 +179,15 @@ __global__ void __launch_bounds__(THREADS, NT == 1 ? 4 : 2) few_up_kernel(UpArgs
   constexpr bool MX4 = SRC != ROWS_BF16;
   constexpr int RG = 4, U = SRC == ROWS_TO_MX4 ? 1 : 2, NP = NT <= 2 ? NT : 1;
   __shared__ __attribute__((aligned(16))) float red[WAVES * 64 * RED];
-  __shared__ MoeLists lists[MOE ? 1 : 1];
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, q = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const unsigned id = run_of(blockIdx.y * gridDim.x + blockIdx.x, gridDim.x * gridDim.y), slot = id / gridDim.x;
   const int strip = (int)(id - slot * gridDim.x);
   int expert = 0, n = e.T, first = 0;
   if constexpr (MOE) {
-    moe_lists(e.picks, e.T * e.k, lists[0]);
-    if ((int)slot >= lists[0].n_active) return;
-    expert = uniform(lists[0].active[slot]);
-    first = uniform(lists[0].at[expert]);
-    n = uniform(lists[0].count[expert]);
+    if ((int)slot >= e.plan->n_active) return;
+    expert = e.plan->expert[slot];
+    first = e.plan->start[slot];
+    n = e.plan->start[slot + 1] - first;
   }
   const char* codes = e.w + (size_t)expert * e.w_stride;
   const Strip w{codes + (size_t)strip * e.steps * MX4_PANEL, codes + e.scales_at + (size_t)strip * ((e.steps + 3) >> 2) * 1024, e.steps};
@@ -233,7 +200,7 @@ __global__ void __launch_bounds__(THREADS, NT == 1 ? 4 : 2) few_up_kernel(UpArgs
   for (int i = 0; i < NT; i++) {
     const int at = 16 * i + c;
     on[i] = at < n;
-    const int p = on[i] ? (MOE ? lists[0].list[first + at] : at) : 0;
+    const int p = on[i] ? (MOE ? e.plan->list[first + at] : at) : 0;
     row[i] = MOE ? p / e.k : p;
   }
   const int groups = (n + 15) >> 4;
@@ -279,7 +246,7 @@ __global__ void __launch_bounds__(THREADS, NT == 1 ? 4 : 2) few_up_kernel(UpArgs
       up += red[(k * 64 + 32 + r) * RED + tok];
     }
     const float h = gate_act(e.gate, gate) * up;
-    const int dest = at < n ? (MOE ? lists[0].list[first + at] : at) : 0;
+    const int dest = at < n ? (MOE ? e.plan->list[first + at] : at) : 0;
     if constexpr (MX4) {
       uint32_t top = magnitude(h);
 #pragma unroll
@@ -355,7 +322,7 @@ struct DownArgs {
   const char* w; size_t w_stride, scales_at;
   int steps, F, D, T, k;
   const char* h; const char* h_scales; int h_steps;   // rows by pair
-  const int* picks; const float* shares;
+  const MoePlan* plan;
   uint16_t* out;
 };
 constexpr int SUM = 20;                                    // pitch of a token's 16 channels
@@ -366,42 +333,46 @@ template <bool MX4, int NT>
 __global__ void __launch_bounds__(THREADS, 2) moe_down_kernel(DownArgs e) {
   constexpr int U = 8, SRC = MX4 ? OPERAND_MX4 : ROWS_BF16;
   extern __shared__ __attribute__((aligned(16))) float sums[];   // [wave][token][SUM]
-  __shared__ MoeLists lists;
+  __shared__ int active[MOE_E], start[MOE_E + 1], list[MOE_PAIRS];
+  __shared__ float share[MOE_PAIRS];
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, q = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int strip = (int)run_of(blockIdx.x, gridDim.x), block = strip >> 2, g0 = strip & 3;
   for (int i = tid; i < WAVES * e.T * SUM; i += THREADS) sums[i] = 0.f;
-  for (int i = tid; i < e.T * e.k; i += THREADS) lists.share[i] = e.shares[i];
-  moe_lists(e.picks, e.T * e.k, lists);
+  const int n_active = e.plan->n_active;
+  for (int i = tid; i < e.T * e.k; i += THREADS) {
+    list[i] = e.plan->list[i];
+    share[i] = e.plan->share[i];
+  }
+  if (tid < n_active) active[tid] = e.plan->expert[tid];
+  if (tid <= n_active) start[tid] = e.plan->start[tid];
+  __syncthreads();
   float* mine = sums + wave * e.T * SUM;
   const Tokens x{e.h, e.h_scales, e.F, e.h_steps};
-  const int units = (e.steps + U - 1) / U, total = uniform(lists.n_active) * units;   // units of U steps, the experts' one after the other, dealt out to the waves
-  auto strip_of = [&](int i, int& expert) {
-    expert = uniform(lists.active[i / units]);
-    const char* codes = e.w + (size_t)expert * e.w_stride;
+  const int units = (e.steps + U - 1) / U, total = n_active * units;   // units of U steps, the experts' one after the other, dealt out to the waves
+  // of unit i: the strip, and the lane's row of the first 16 of the expert's tokens
+  auto strip_of = [&](int i) {
+    const char* codes = e.w + (size_t)uniform(active[i / units]) * e.w_stride;
     return Strip{codes + (size_t)block * e.steps * MX4_PANEL + g0 * 1024, codes + e.scales_at + (size_t)block * ((e.steps + 3) >> 2) * 1024 + g0 * 256, e.steps};
   };
-  // the lane's rows of the first 16 of an expert's tokens
-  auto first_rows = [&](int expert, int (&row)[1], bool (&on)[1]) {
-    on[0] = c < lists.count[expert];
-    row[0] = on[0] ? lists.list[lists.at[expert] + c] : 0;
+  auto first_rows = [&](int i, int (&row)[1], bool (&on)[1]) {
+    const int at = start[i / units] + c;
+    on[0] = at < start[i / units + 1];
+    row[0] = on[0] ? list[at] : 0;
   };
   Unit<SRC, 1, U, 1> now, next;
-  int i = wave, expert = 0, row_n[1], row_f[1];
+  int i = wave, row_n[1], row_f[1];
   bool on_n[1], on_f[1];
   if (i < total) {
-    const Strip w = strip_of(i, expert);
-    first_rows(expert, row_f, on_f);
-    now.load(w, x, row_f, on_f, i % units * U, lane);
+    first_rows(i, row_f, on_f);
+    now.load(strip_of(i), x, row_f, on_f, i % units * U, lane);
   }
   for (; i < total; i += WAVES) {
     const bool more = i + WAVES < total;
-    int then = 0;
     if (more) {
-      const Strip w = strip_of(i + WAVES, then);
-      first_rows(then, row_n, on_n);
-      next.load(w, x, row_n, on_n, (i + WAVES) % units * U, lane);
+      first_rows(i + WAVES, row_n, on_n);
+      next.load(strip_of(i + WAVES), x, row_n, on_n, (i + WAVES) % units * U, lane);
     }
-    const int n = uniform(lists.count[expert]), first = uniform(lists.at[expert]), groups = (n + 15) >> 4;
+    const int first = uniform(start[i / units]), n = uniform(start[i / units + 1]) - first, groups = (n + 15) >> 4;
     int row[NT];
     bool on[NT];
     row[0] = row_f[0];
@@ -410,7 +381,7 @@ __global__ void __launch_bounds__(THREADS, 2) moe_down_kernel(DownArgs e) {
     for (int g = 1; g < NT; g++) {
       const int at = 16 * g + c;
       on[g] = at < n;
-      row[g] = on[g] ? lists.list[first + at] : 0;
+      row[g] = on[g] ? list[first + at] : 0;
     }
     f32x4 acc[1][NT];
 #pragma unroll
@@ -420,7 +391,7 @@ __global__ void __launch_bounds__(THREADS, 2) moe_down_kernel(DownArgs e) {
 #pragma unroll
     for (int g = 0; g < NT; g++)
       if (on[g]) {                                         // (a token chooses an expert once: no two lanes of a quarter have the same one)
-        const float p = lists.share[row[g]];
+        const float p = share[first + 16 * g + c];
         f32x4* to = reinterpret_cast<f32x4*>(mine + row[g] / e.k * SUM + 4 * q);
         f32x4 y = *to;
 #pragma unroll
@@ -428,7 +399,6 @@ __global__ void __launch_bounds__(THREADS, 2) moe_down_kernel(DownArgs e) {
         *to = y;
       }
     if (more) now = next;
-    expert = then;
     row_f[0] = row_n[0];
     on_f[0] = on_n[0];
   }
@@ -463,11 +433,18 @@ __global__ void __launch_bounds__(256) moe_router_kernel(const uint16_t* __restr
   const int ways = 256 / E, way = tid / E, ex = tid - way * E;   // the rows of Wr are dealt out to `ways` groups of E work items
   double acc[ROUTE_T] = {};
   if (way < ways) {
-    for (int d = way; d < ROUTE_D; d += ways) {
-      const float w = bf16_lo_to_f32(Wr[(size_t)(d0 + d) * E + ex]);
+    for (int d = way; d < ROUTE_D; d += 16 * ways) {         // 16 rows on their way at once
+      uint16_t w[16];
 #pragma unroll
-      for (int t = 0; t < ROUTE_T; t++)
-        if (t < tokens) acc[t] += (double)(x[t][d] * w);
+      for (int j = 0; j < 16; j++) w[j] = d + j * ways < ROUTE_D ? Wr[(size_t)(d0 + d + j * ways) * E + ex] : (uint16_t)0;
+#pragma unroll
+      for (int j = 0; j < 16; j++) {
+        if (d + j * ways >= ROUTE_D) break;
+        const float y = bf16_lo_to_f32(w[j]);
+#pragma unroll
+        for (int t = 0; t < ROUTE_T; t++)
+          if (t < tokens) acc[t] += (double)(x[t][d + j * ways] * y);
+      }
     }
 #pragma unroll
     for (int t = 0; t < ROUTE_T; t++)
@@ -487,31 +464,43 @@ __device__ __forceinline__ unsigned long long order_of(double x) {
   const unsigned long long b = __builtin_bit_cast(unsigned long long, x + 0.0);   // (-0 is 0)
   return x != x ? 0ull : b >> 63 ? ~b : b | 1ull << 63;
 }
-// a workgroup a token
+// A workgroup a token; the one that comes last makes the plan.
 __global__ void __launch_bounds__(256) moe_pick_kernel(const double* __restrict__ parts, int n_parts, int T, int E, int k, int renormalise, int* __restrict__ picks,
-                                                       float* __restrict__ shares) {
+                                                       float* __restrict__ shares, MoePlan* __restrict__ plan) {
+  __shared__ double sums[256], chosen[MOE_MAX_K];
   __shared__ unsigned long long order[MOE_E];
-  __shared__ double logit[MOE_E], chosen[16];
   __shared__ float part[4];
-  const int t = blockIdx.x, e = threadIdx.x;
+  __shared__ int count[MOE_E], cursor[MOE_E], come;
+  const int t = blockIdx.x, tid = threadIdx.x, ways = 256 / E, way = tid / E, ex = tid - way * E;
+  {
+    double s = 0.0;
+    if (way < ways) {
+      const double* p = parts + (size_t)t * E + ex;
+      for (int i = way; i < n_parts; i += 8 * ways) {          // eight on their way at once
+        double v[8];
+#pragma unroll
+        for (int j = 0; j < 8; j++) v[j] = i + j * ways < n_parts ? p[(size_t)(i + j * ways) * T * E] : 0.0;
+#pragma unroll
+        for (int j = 0; j < 8; j++) s += v[j];
+      }
+    }
+    sums[tid] = s;
+  }
+  __syncthreads();
+  const int e = tid;
   double s = 0.0;
   if (e < E) {
-    const double* p = parts + (size_t)t * E + e;
-#pragma unroll 8
-    for (int i = 0; i < n_parts; i++) s += p[(size_t)i * T * E];
+    for (int i = 0; i < ways; i++) s += sums[i * E + e];
     order[e] = order_of(s);
-    logit[e] = s;
   }
   __syncthreads();
   int rank = MOE_E;
   if (e < E) {
     const unsigned long long mine = order[e];
     rank = 0;
+#pragma unroll 4
     for (int i = 0; i < E; i++) rank += order[i] > mine || (order[i] == mine && i < e);
-    if (rank < k) {
-      picks[t * k + rank] = e;
-      chosen[rank] = s;
-    }
+    if (rank < k) chosen[rank] = s;
   }
   __syncthreads();
   // shares: exp(l - largest) over its sum, of the chosen or of all
@@ -521,7 +510,72 @@ __global__ void __launch_bounds__(256) moe_pick_kernel(const double* __restrict_
   for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d, 64);
   if ((e & 63) == 0) part[e >> 6] = sum;
   __syncthreads();
-  if (rank < k) shares[t * k + rank] = x / (part[0] + part[1] + part[2] + part[3]);
+  if (rank < k) {
+    const float p = x / (part[0] + part[1] + part[2] + part[3]);
+    picks[t * k + rank] = e;
+    shares[t * k + rank] = p;
+    put(&plan->picks[t * k + rank], e);
+    put(&plan->shares[t * k + rank], p);
+  }
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+  if (tid == 0) come = __hip_atomic_fetch_add(&plan->ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  count[tid] = 0;
+  __syncthreads();
+  if (come != T - 1) return;
+
+  const int pairs = T * k;
+  int mine[MOE_PAIRS / 256];
+  float p[MOE_PAIRS / 256];
+#pragma unroll
+  for (int j = 0; j < MOE_PAIRS / 256; j++) {
+    const int i = 256 * j + tid;
+    if (i < pairs) {
+      mine[j] = get(&plan->picks[i]);
+      p[j] = get(&plan->shares[i]);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < MOE_PAIRS / 256; j++)
+    if (256 * j + tid < pairs) atomicAdd(&count[mine[j]], 1);
+  __syncthreads();
+  if (tid < 64) {                                              // four experts a lane: pairs before them below, chosen ones above
+    int n[4], all = 0;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      n[i] = count[4 * tid + i];
+      all += n[i] | (n[i] > 0 ? 1 << 16 : 0);
+    }
+    int upto = all;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int y = __shfl_up(upto, d, 64);
+      if (tid >= d) upto += y;
+    }
+    int run = upto - all;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      cursor[4 * tid + i] = run & 0xFFFF;
+      if (n[i] > 0) {
+        plan->expert[run >> 16] = 4 * tid + i;
+        plan->start[run >> 16] = run & 0xFFFF;
+      }
+      run += n[i] | (n[i] > 0 ? 1 << 16 : 0);
+    }
+    if (tid == 63) {
+      plan->start[run >> 16] = run & 0xFFFF;
+      plan->n_active = run >> 16;
+      put(&plan->ticket, 0);
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < MOE_PAIRS / 256; j++)
+    if (256 * j + tid < pairs) {
+      const int at = atomicAdd(&cursor[mine[j]], 1);
+      plan->list[at] = 256 * j + tid;
+      plan->share[at] = p[j];
+    }
 }
 
 template <int SRC, bool MOE>
@@ -549,19 +603,22 @@ int launch_rows(const RowsArgs& a, hipStream_t s) {
 }
 }  // namespace
 
+size_t moe_plan_size() { return sizeof(MoePlan); }
 size_t moe_parts_size(int T, int D, int E) { return (size_t)(D / ROUTE_D) * T * E * sizeof(double); }
 
-int launch_moe_route(const void* X, const void* Wr, int T, int D, int E, int k, bool renormalise, void* parts, int* picks, float* shares, const Mx4Operand* x, hipStream_t s) {
+int launch_moe_route(const void* X, const void* Wr, int T, int D, int E, int k, bool renormalise, void* parts, int* picks, float* shares, void* plan,
+                     const Mx4Operand* x, hipStream_t s) {
   const int n = D / ROUTE_D;
   hipLaunchKernelGGL(moe_router_kernel, dim3((unsigned)n, (unsigned)((T + ROUTE_T - 1) / ROUTE_T)), dim3(256), 0, s, static_cast<const uint16_t*>(X),
                      static_cast<const uint16_t*>(Wr), T, D, E, static_cast<double*>(parts), x ? x->steps : 0, x ? const_cast<char*>(x->codes) : nullptr,
                      x ? const_cast<char*>(x->scales) : nullptr);
-  hipLaunchKernelGGL(moe_pick_kernel, dim3((unsigned)T), dim3(256), 0, s, static_cast<const double*>(parts), n, T, E, k, (int)renormalise, picks, shares);
+  hipLaunchKernelGGL(moe_pick_kernel, dim3((unsigned)T), dim3(256), 0, s, static_cast<const double*>(parts), n, T, E, k, (int)renormalise, picks, shares,
+                     static_cast<MoePlan*>(plan));
   return (int)hipGetLastError();
 }
 
-int launch_moe_experts(const MoeWeights& w, const void* X, const Mx4Operand* x, int T, int D, int F, int E, int k, float c1, float c3, const int* picks, const float* shares,
-                       void* H, int h_rows, void* Y, hipStream_t s) {
+int launch_moe_experts(const MoeWeights& w, const void* X, const Mx4Operand* x, int T, int D, int F, int E, int k, float c1, float c3, const void* plan, void* H,
+                       int h_rows, void* Y, hipStream_t s) {
   UpArgs up{};
   up.w = static_cast<const char*>(w.up); up.w_stride = w.up_stride; up.scales_at = w.up_scales;
   up.K = D; up.F = F; up.T = T; up.steps = w.mx4 ? mx4_steps(D) : D / 32; up.gate = Gate{c1, c3};
@@ -570,14 +627,14 @@ int launch_moe_experts(const MoeWeights& w, const void* X, const Mx4Operand* x, 
   up.h = const_cast<char*>(w.mx4 ? h.codes : static_cast<const char*>(H));
   up.h_scales = const_cast<char*>(h.scales);
   up.h_steps = h.steps;
-  up.picks = picks; up.k = k;
+  up.plan = static_cast<const MoePlan*>(plan); up.k = k;
   const int slots = T * k < E ? T * k : E;
   if (const int rc = w.mx4 ? launch_up<OPERAND_MX4, true>(up, slots, s) : launch_up<ROWS_BF16, true>(up, slots, s)) return rc;
   DownArgs d{};
   d.w = static_cast<const char*>(w.down); d.w_stride = w.down_stride; d.scales_at = w.down_scales;
   d.steps = w.mx4 ? mx4_steps(F) : F / 32; d.F = F; d.D = D; d.T = T; d.k = k;
   d.h = up.h; d.h_scales = h.scales; d.h_steps = h.steps;
-  d.picks = picks; d.shares = shares; d.out = static_cast<uint16_t*>(Y);
+  d.plan = up.plan; d.out = static_cast<uint16_t*>(Y);
   if (T <= 16) return w.mx4 ? launch_down<true, 1>(d, s) : launch_down<false, 1>(d, s);
   return w.mx4 ? launch_down<true, 4>(d, s) : launch_down<false, 4>(d, s);
 }

@@ -78,9 +78,10 @@ int launch_few_mx4_rows(const Mx4Operand& w, int K, int N, const void* X, const 
 constexpr int MOE_TOKENS = 64, MOE_MAX_E = 256, MOE_MAX_K = 16;
 struct MoeWeights { bool mx4; const void *up, *down; size_t up_stride, down_stride, up_scales, down_scales; };
 size_t moe_parts_size(int T, int D, int E);
-int launch_moe_route(const void* X, const void* Wr, int T, int D, int E, int k, bool renormalise, void* parts, int* picks, float* shares, const Mx4Operand* x,
-                     hipStream_t s);   // x: the tokens as mx4 go there
-int launch_moe_experts(const MoeWeights& w, const void* X, const Mx4Operand* x, int T, int D, int F, int E, int k, float c1, float c3, const int* picks, const float* shares,
-                       void* H, int h_rows, void* Y, hipStream_t s);
+size_t moe_plan_size();                          // zero before its first use
+int launch_moe_route(const void* X, const void* Wr, int T, int D, int E, int k, bool renormalise, void* parts, int* picks, float* shares, void* plan,
+                     const Mx4Operand* x, hipStream_t s);   // x: the tokens as mx4 go there
+int launch_moe_experts(const MoeWeights& w, const void* X, const Mx4Operand* x, int T, int D, int F, int E, int k, float c1, float c3, const void* plan, void* H,
+                       int h_rows, void* Y, hipStream_t s);
 
 }  // namespace ffn24
