@@ -44,7 +44,7 @@ struct moe_ctx {
   GateCoefficients gate;
   int renormalise, device, have_weights;
   MoeWeights w;
-  void *Wr, *up, *down, *X, *parts, *plan, *H, *picks, *shares;   // X, H: tokens and activations as mx4 (H: or bf16)
+  void *Wr, *up, *down, *X, *parts, *plan, *sums, *H, *picks, *shares;   // X, H: tokens and activations as mx4 (H: or bf16)
 };
 
 extern "C" {
@@ -177,10 +177,10 @@ int moe_ctx_create(moe_ctx** out, int64_t T, int64_t D, int64_t F, int64_t E, in
   const bool mx4 = type == FFN24_EXPERTS_MX4;
   const int64_t up = mx4 ? mx4_operand_size(2 * F, D) : bf16_operand_size(2 * F, D), down = mx4 ? mx4_operand_size(D, F) : bf16_operand_size(D, F);
   // (of mx4 rows the k beyond D and F are zero for good: no kernel writes them)
-  const bool ok = hipGetDevice(&c->device) == hipSuccess && hipMalloc(&c->Wr, (size_t)(2 * D * E)) == hipSuccess && hipMalloc(&c->up, (size_t)(E * up)) == hipSuccess &&
+  const bool ok = hipGetDevice(&c->device) == hipSuccess && hipMalloc(&c->Wr, (size_t)bf16_operand_size(E, D)) == hipSuccess && hipMalloc(&c->up, (size_t)(E * up)) == hipSuccess &&
                   hipMalloc(&c->down, (size_t)(E * down)) == hipSuccess && hipMalloc(&c->parts, moe_parts_size((int)T, (int)D, (int)E)) == hipSuccess &&
                   hipMalloc(&c->picks, (size_t)(4 * T * k)) == hipSuccess && hipMalloc(&c->shares, (size_t)(4 * T * k)) == hipSuccess &&
-                  cleared(&c->plan, (int64_t)moe_plan_size()) && (!mx4 || cleared(&c->X, mx4_operand_size(T, D))) && cleared(&c->H, mx4 ? mx4_operand_size(T * k, F) : 2 * T * k * F) && hipDeviceSynchronize() == hipSuccess;
+                  hipMalloc(&c->sums, (size_t)(4 * MOE_SPLITS * T * D)) == hipSuccess && cleared(&c->plan, (int64_t)moe_plan_size()) && (!mx4 || cleared(&c->X, mx4_operand_size(T, D))) && cleared(&c->H, mx4 ? mx4_operand_size(T * k, F) : 2 * T * k * F) && hipDeviceSynchronize() == hipSuccess;
   if (!ok) {
     (void)hipGetLastError();
     moe_ctx_destroy(c);
@@ -195,7 +195,7 @@ int moe_ctx_create(moe_ctx** out, int64_t T, int64_t D, int64_t F, int64_t E, in
 int moe_ctx_destroy(moe_ctx* c) {
   if (!c) return FFN24_OK;
   int bad = 0;
-  for (void* p : {c->Wr, c->up, c->down, c->X, c->parts, c->plan, c->H, c->picks, c->shares}) if (p && hipFree(p) != hipSuccess) bad = 1;
+  for (void* p : {c->Wr, c->up, c->down, c->X, c->parts, c->plan, c->sums, c->H, c->picks, c->shares}) if (p && hipFree(p) != hipSuccess) bad = 1;
   delete c;
   return bad ? FFN24_ERR_HIP : FFN24_OK;
 }
@@ -208,7 +208,7 @@ int moe_set_weights(moe_ctx* c, const void* Wr, const void* Wgu, const void* Wd,
   const int D = (int)c->D, F = (int)c->F, E = (int)c->E;
   c->have_weights = 0;
   const auto lay_out = c->w.mx4 ? launch_mx4_weight : launch_bf16_weight;
-  if (launch_copy16(Wr, c->Wr, (size_t)2 * D * E, s) || lay_out(Wgu, D, 2 * F, true, E, c->up, s) || lay_out(Wd, F, D, false, E, c->down, s)) return FFN24_ERR_HIP;
+  if (launch_bf16_weight(Wr, D, E, false, 1, c->Wr, s) || lay_out(Wgu, D, 2 * F, true, E, c->up, s) || lay_out(Wd, F, D, false, E, c->down, s)) return FFN24_ERR_HIP;
   c->have_weights = 1;
   return FFN24_OK;
 }
@@ -227,7 +227,7 @@ int moe_fwd(moe_ctx* c, const void* X, int64_t T, void* Y, void* experts, void* 
   float* p = static_cast<float*>(experts ? shares : c->shares);
   const Mx4Operand x = mx4_operand(c->X, (int)c->T, D);
   if (launch_moe_route(X, c->Wr, t, D, E, k, c->renormalise != 0, c->parts, picks, p, c->plan, c->w.mx4 ? &x : nullptr, s)) return FFN24_ERR_HIP;
-  return done(launch_moe_experts(c->w, X, &x, t, D, F, E, k, c->gate.c1, c->gate.c3, c->plan, c->H, (int)(c->T * k), Y, s));
+  return done(launch_moe_experts(c->w, X, &x, t, D, F, E, k, c->gate.c1, c->gate.c3, c->plan, c->H, (int)(c->T * k), c->sums, Y, s));
 }
 
 }  // extern "C"

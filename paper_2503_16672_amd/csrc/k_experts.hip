@@ -9,6 +9,7 @@
 //   up       a workgroup a strip of 32 features of a chosen expert: h = a(G) U for the tokens that chose it; a row of H for each (token, choice)
 //   down     a workgroup a strip of 16 channels and all chosen experts one after the other: the shares' sum stays in LDS, in the order of the experts
 #include "mx4_core.hpp"
+#include "mx4_rule.hpp"
 #include "stream_core.hpp"
 
 namespace ffn24 {
@@ -49,7 +50,7 @@ struct Tokens { const char* p; const char* scales; int K, steps; };
 
 // U steps of RG groups of 16 channels, and of the first NP groups of 16 tokens, on their way.  The tokens are asked for first: loads come back in order, so what is asked
 // for behind the weights would wait for them.
-template <int SRC, int RG, int U, int NP>
+template <int SRC, int RG, int U, int NP, int GS = 1>   // GS: from a group to the next of the strip's
 struct Unit {
   static constexpr bool MX4 = SRC != ROWS_BF16;
   static constexpr int SU = MX4 ? (U + 3) / 4 : 1, XW = SRC == ROWS_TO_MX4 ? 4 : 1, KQ = MX4 ? 32 : 8, KS = 4 * KQ;
@@ -90,14 +91,14 @@ struct Unit {
       for (int j = 0; j < SU; j++) {
         const char* at = p.scales + (size_t)(min(s0 + 4 * j, p.steps - 1) >> 2) * 1024 + lane * 4;
 #pragma unroll
-        for (int g = 0; g < RG; g++) sw[j][g] = *reinterpret_cast<const uint32_t*>(at + g * 256);
+        for (int g = 0; g < RG; g++) sw[j][g] = *reinterpret_cast<const uint32_t*>(at + g * GS * 256);
       }
     }
 #pragma unroll
     for (int j = 0; j < U; j++) {
       const char* at = p.codes + (size_t)min(s0 + j, p.steps - 1) * MX4_PANEL + lane * 16;
 #pragma unroll
-      for (int g = 0; g < RG; g++) w[j][g] = ld_stream(reinterpret_cast<const u32x4*>(at + g * 1024));
+      for (int g = 0; g < RG; g++) w[j][g] = ld_stream(reinterpret_cast<const u32x4*>(at + g * GS * 1024));
     }
   }
   template <int NT>
@@ -173,15 +174,18 @@ struct UpArgs {
   const MoePlan* plan; int k;          // MOE
 };
 
-// grid (F / 32, slots).  A slot is a chosen expert; without MOE there is one, and it has all tokens.
-template <int SRC, int NT, bool MOE>
-__global__ void __launch_bounds__(THREADS, NT == 1 ? 4 : 2) few_up_kernel(UpArgs e) {
+// grid (strips, slots).  A slot is a chosen expert; without MOE there is one, and it has all tokens.  A strip is 8 RG features: a block of 64 rows, or (RG 2, bf16, whose result needs no
+// 32 features together) every other group of one.
+template <int SRC, int NT, bool MOE, int RG, int W>
+__global__ void __launch_bounds__(64 * W, NT == 1 ? 4 : 2) few_up_kernel(UpArgs e) {
   constexpr bool MX4 = SRC != ROWS_BF16;
-  constexpr int RG = 4, U = SRC == ROWS_TO_MX4 ? 1 : 2, NP = NT <= 2 ? NT : 1;
-  __shared__ __attribute__((aligned(16))) float red[WAVES * 64 * RED];
+  constexpr int U = SRC == ROWS_TO_MX4 ? 1 : 8 / RG, NP = NT <= 2 ? NT : 1, FEATS = 8 * RG;
+  static_assert(RG == 4 || (RG == 2 && !MX4), "whole blocks of 32 features");
+  __shared__ __attribute__((aligned(16))) float red[W * 16 * RG * RED];
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, q = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const unsigned id = run_of(blockIdx.y * gridDim.x + blockIdx.x, gridDim.x * gridDim.y), slot = id / gridDim.x;
-  const int strip = (int)(id - slot * gridDim.x);
+  // whole blocks are 4 KiB a step and cover an L2's channels by themselves: they go round the XCDs, which then share the experts that were chosen (the last slots may have none)
+  const unsigned at = blockIdx.y * gridDim.x + blockIdx.x, id = RG == 4 ? at : run_of(at, gridDim.x * gridDim.y), slot = id / gridDim.x;
+  const int strip = (int)(id - slot * gridDim.x), block = RG == 4 ? strip : strip >> 1, half = RG == 4 ? 0 : strip & 1;
   int expert = 0, n = e.T, first = 0;
   if constexpr (MOE) {
     if ((int)slot >= e.plan->n_active) return;
@@ -190,18 +194,22 @@ __global__ void __launch_bounds__(THREADS, NT == 1 ? 4 : 2) few_up_kernel(UpArgs
     n = e.plan->start[slot + 1] - first;
   }
   const char* codes = e.w + (size_t)expert * e.w_stride;
-  const Strip w{codes + (size_t)strip * e.steps * MX4_PANEL, codes + e.scales_at + (size_t)strip * ((e.steps + 3) >> 2) * 1024, e.steps};
+  const Strip w{codes + (size_t)block * e.steps * MX4_PANEL + half * 1024, codes + e.scales_at + (size_t)block * ((e.steps + 3) >> 2) * 1024, e.steps};
   const Tokens x{e.x, e.x_scales, e.K, e.steps};
 
   // (no expert has more tokens than there are: T <= 16 NT)
-  int row[NT];
-  bool on[NT];
+  int row[NT], row_p[NP];
+  bool on[NT], on_p[NP];
 #pragma unroll
   for (int i = 0; i < NT; i++) {
     const int at = 16 * i + c;
     on[i] = at < n;
     const int p = on[i] ? (MOE ? e.plan->list[first + at] : at) : 0;
     row[i] = MOE ? p / e.k : p;
+    if (i < NP) {
+      row_p[i < NP ? i : 0] = row[i];
+      on_p[i < NP ? i : 0] = on[i];
+    }
   }
   const int groups = (n + 15) >> 4;
   f32x4 acc[RG][NT];
@@ -209,19 +217,12 @@ __global__ void __launch_bounds__(THREADS, NT == 1 ? 4 : 2) few_up_kernel(UpArgs
   for (int g = 0; g < RG; g++)
 #pragma unroll
     for (int i = 0; i < NT; i++) acc[g][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  int row_p[NP];
-  bool on_p[NP];
-#pragma unroll
-  for (int i = 0; i < NP; i++) {
-    row_p[i] = row[i];
-    on_p[i] = on[i];
-  }
-  Unit<SRC, RG, U, NP> now, next;
+  Unit<SRC, RG, U, NP, RG == 4 ? 1 : 2> now, next;
   int s = wave * U;
   if (s < e.steps) now.load(w, x, row_p, on_p, s, lane);
-  for (; s < e.steps; s += WAVES * U) {
-    const bool more = s + WAVES * U < e.steps;
-    if (more) next.load(w, x, row_p, on_p, s + WAVES * U, lane);
+  for (; s < e.steps; s += W * U) {
+    const bool more = s + W * U < e.steps;
+    if (more) next.load(w, x, row_p, on_p, s + W * U, lane);
     now.ops(x, row, on, groups, s, e.steps, q, acc);
     if (more) now = next;
   }
@@ -234,31 +235,35 @@ __global__ void __launch_bounds__(THREADS, NT == 1 ? 4 : 2) few_up_kernel(UpArgs
 #pragma unroll
         for (int g = 0; g < RG; g++)
 #pragma unroll
-          for (int v = 0; v < 4; v++) red[(wave * 64 + 16 * g + 4 * q + v) * RED + c] = acc[g][j][v];
+          for (int v = 0; v < 4; v++) red[(wave * 16 * RG + 16 * g + 4 * q + v) * RED + c] = acc[g][j][v];
       }
     __syncthreads();
-    // 32 neighbouring lanes have the features of a token
-    const int f = tid & 31, tok = tid >> 5, r = ((f >> 2) & 1) * 16 + 4 * (f >> 3) + (f & 3), at = 16 * i + tok;
-    float gate = 0.f, up = 0.f;
+    // neighbouring lanes have the features of a token
+    for (int o = tid; o < FEATS * 16; o += 64 * W) {
+      const int f = o % FEATS, tok = o / FEATS, at = 16 * i + tok;
+      const int r = RG == 4 ? ((f >> 2) & 1) * 16 + 4 * (f >> 3) + (f & 3) : f;
+      float gate = 0.f, up = 0.f;
 #pragma unroll
-    for (int k = 0; k < WAVES; k++) {
-      gate += red[(k * 64 + r) * RED + tok];
-      up += red[(k * 64 + 32 + r) * RED + tok];
-    }
-    const float h = gate_act(e.gate, gate) * up;
-    const int dest = at < n ? (MOE ? e.plan->list[first + at] : at) : 0;
-    if constexpr (MX4) {
-      uint32_t top = magnitude(h);
+      for (int k = 0; k < W; k++) {
+        gate += red[(k * 16 * RG + r) * RED + tok];
+        up += red[(k * 16 * RG + 8 * RG + r) * RED + tok];
+      }
+      const float h = gate_act(e.gate, gate) * up;
+      const int dest = at < n ? (MOE ? e.plan->list[first + at] : at) : 0;
+      if constexpr (MX4) {
+        uint32_t top = magnitude(h);
 #pragma unroll
-      for (int d = 1; d < 32; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
-      const uint32_t code = mx4_scale_code(top);
-      uint32_t word = (__builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, h, 0.f, mx4_scale(code), 0) & 15u) << (4 * (f & 7));
+        for (int d = 1; d < 32; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
+        const uint32_t code = mx4_scale_code(top);
+        uint32_t word = (__builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, h, 0.f, mx4_scale(code), 0) & 15u) << (4 * (f & 7));
 #pragma unroll
-      for (int d = 1; d < 8; d <<= 1) word |= (uint32_t)__shfl_xor((int)word, d, 64);
-      if (at < n && (f & 7) == 0) *reinterpret_cast<uint32_t*>(e.h + mx4_code_at(dest, strip, e.h_steps) + (f >> 1)) = word;
-      if (at < n && f == 0) e.h_scales[mx4_scale_at(dest, strip, e.h_steps)] = (char)code;
-    } else {
-      if (at < n) reinterpret_cast<uint16_t*>(e.h)[(size_t)dest * e.F + 32 * strip + f] = (uint16_t)pack_bf16x2(h, 0.f);
+        for (int d = 1; d < 8; d <<= 1) word |= (uint32_t)__shfl_xor((int)word, d, 64);
+        if (at < n && (f & 7) == 0) *reinterpret_cast<uint32_t*>(e.h + mx4_code_at(dest, block, e.h_steps) + (f >> 1)) = word;
+        if (at < n && f == 0) e.h_scales[mx4_scale_at(dest, block, e.h_steps)] = (char)code;
+      } else {
+        const int feat = 32 * block + (RG == 4 ? f : 8 * (f >> 2) + 4 * half + (f & 3));
+        if (at < n) reinterpret_cast<uint16_t*>(e.h)[(size_t)dest * e.F + feat] = (uint16_t)pack_bf16x2(h, 0.f);
+      }
     }
   }
 }
@@ -323,12 +328,13 @@ struct DownArgs {
   int steps, F, D, T, k;
   const char* h; const char* h_scales; int h_steps;   // rows by pair
   const MoePlan* plan;
+  float* parts;                        // [splits][T][D]
   uint16_t* out;
 };
 constexpr int SUM = 20;                                    // pitch of a token's 16 channels
 constexpr int down_lds(int T) { return WAVES * T * SUM * 4; }
 
-// grid (D / 16)
+// grid (D / 16, splits).  Where the strips are few, several workgroups share one's experts, and a second kernel adds up.
 template <bool MX4, int NT>
 __global__ void __launch_bounds__(THREADS, 2) moe_down_kernel(DownArgs e) {
   constexpr int U = 8, SRC = MX4 ? OPERAND_MX4 : ROWS_BF16;
@@ -336,7 +342,8 @@ __global__ void __launch_bounds__(THREADS, 2) moe_down_kernel(DownArgs e) {
   __shared__ int active[MOE_E], start[MOE_E + 1], list[MOE_PAIRS];
   __shared__ float share[MOE_PAIRS];
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, q = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int strip = (int)run_of(blockIdx.x, gridDim.x), block = strip >> 2, g0 = strip & 3;
+  const unsigned id = run_of(blockIdx.y * gridDim.x + blockIdx.x, gridDim.x * gridDim.y), splits = gridDim.y;
+  const int strip = (int)(id / splits), split = (int)(id - strip * splits), block = strip >> 2, g0 = strip & 3, stride = WAVES * (int)splits;
   for (int i = tid; i < WAVES * e.T * SUM; i += THREADS) sums[i] = 0.f;
   const int n_active = e.plan->n_active;
   for (int i = tid; i < e.T * e.k; i += THREADS) {
@@ -360,17 +367,17 @@ __global__ void __launch_bounds__(THREADS, 2) moe_down_kernel(DownArgs e) {
     row[0] = on[0] ? list[at] : 0;
   };
   Unit<SRC, 1, U, 1> now, next;
-  int i = wave, row_n[1], row_f[1];
+  int i = split * WAVES + wave, row_n[1], row_f[1];
   bool on_n[1], on_f[1];
   if (i < total) {
     first_rows(i, row_f, on_f);
     now.load(strip_of(i), x, row_f, on_f, i % units * U, lane);
   }
-  for (; i < total; i += WAVES) {
-    const bool more = i + WAVES < total;
+  for (; i < total; i += stride) {
+    const bool more = i + stride < total;
     if (more) {
-      first_rows(i + WAVES, row_n, on_n);
-      next.load(strip_of(i + WAVES), x, row_n, on_n, (i + WAVES) % units * U, lane);
+      first_rows(i + stride, row_n, on_n);
+      next.load(strip_of(i + stride), x, row_n, on_n, (i + stride) % units * U, lane);
     }
     const int first = uniform(start[i / units]), n = uniform(start[i / units + 1]) - first, groups = (n + 15) >> 4;
     int row[NT];
@@ -404,58 +411,54 @@ __global__ void __launch_bounds__(THREADS, 2) moe_down_kernel(DownArgs e) {
   }
   __syncthreads();
   for (int o = tid; o < 16 * e.T; o += THREADS) {
-    const int r = o & 15, t = o >> 4, ch = 64 * block + channel_of(g0, r);
+    const int r = o & 15, t = o >> 4;
     float y = 0.f;
 #pragma unroll
     for (int k = 0; k < WAVES; k++) y += sums[(k * e.T + t) * SUM + r];
-    if (ch < e.D) e.out[(size_t)t * e.D + ch] = (uint16_t)pack_bf16x2(y, 0.f);
+    const size_t at = (size_t)t * e.D + 64 * block + channel_of(g0, r);
+    if (splits == 1) e.out[at] = (uint16_t)pack_bf16x2(y, 0.f);
+    else e.parts[(size_t)split * e.T * e.D + at] = y;
   }
 }
 
 // ------------------------------------------------------------------------------------------------ router
-constexpr int ROUTE_D = 64, ROUTE_T = 8;   // of D and of the tokens a workgroup
-// grid (D / 64, T / 8); parts [D / 64][T][E]
-// steps > 0: the tokens go out as mx4 too, in the operand form
-__global__ void __launch_bounds__(256) moe_router_kernel(const uint16_t* __restrict__ X, const uint16_t* __restrict__ Wr, int T, int D, int E, double* __restrict__ parts, int steps,
+// In 64 bits on the matrix ops too: op j of a step of 32 d takes d 8 q + j from lane quarter q.  A: 16 tokens, B: 16 experts (Wr in the order of the bf16 operands).
+// grid (parts of 128 d, groups of 16 tokens); parts [part][T][E].  steps > 0: the tokens go out as mx4 too, in the operand form.
+typedef double f64x4 __attribute__((ext_vector_type(4)));
+constexpr int ROUTE_D = 128, ROUTE_STEPS = ROUTE_D / 32;
+__device__ __forceinline__ double bf16_of(const u32x4& w, int j) { return (double)(j % 2 ? bf16_hi_to_f32(w[j / 2]) : bf16_lo_to_f32(w[j / 2])); }
+__global__ void __launch_bounds__(256) moe_router_kernel(const uint16_t* __restrict__ X, const char* __restrict__ Wr, int T, int D, int E, double* __restrict__ parts, int steps,
                                                          char* __restrict__ codes, char* __restrict__ scales) {
-  __shared__ float x[ROUTE_T][ROUTE_D];
-  __shared__ double sums[256 * ROUTE_T];
-  const int tid = threadIdx.x, d0 = blockIdx.x * ROUTE_D, t0 = blockIdx.y * ROUTE_T, tokens = min(T - t0, ROUTE_T);
-  if (steps > 0 && tid < 8 * tokens) {                         // four lanes have a block of 32
-    const int t = t0 + tid / 8, d = d0 + 8 * (tid & 7), p = tid & 3;
+  const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, q = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int s0 = blockIdx.x * ROUTE_STEPS, all = D / 32, n = min(all - s0, ROUTE_STEPS), t0 = 16 * blockIdx.y;
+  const int groups = 4 * (E / 64) + (E % 64 > 32 ? 4 : E % 64 ? 2 : 0);    // of 16 rows that have an expert
+  u32x4 x[ROUTE_STEPS];
+#pragma unroll
+  for (int s = 0; s < ROUTE_STEPS; s++)
+    x[s] = t0 + c < T && s < n ? *reinterpret_cast<const u32x4*>(X + (size_t)(t0 + c) * D + 32 * (s0 + s) + 8 * q) : u32x4{0u, 0u, 0u, 0u};
+  for (int g = wave; g < groups; g += 4) {
+    const char* w = Wr + ((size_t)(g >> 2) * all + s0) * MX4_PANEL + (g & 3) * 1024 + lane * 16;
+    u32x4 y[ROUTE_STEPS];
+#pragma unroll
+    for (int s = 0; s < ROUTE_STEPS; s++) y[s] = s < n ? *reinterpret_cast<const u32x4*>(w + (size_t)s * MX4_PANEL) : u32x4{0u, 0u, 0u, 0u};
+    f64x4 acc = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+    for (int s = 0; s < ROUTE_STEPS; s++)
+#pragma unroll
+      for (int j = 0; j < 8; j++) acc = __builtin_amdgcn_mfma_f64_16x16x4f64(bf16_of(x[s], j), bf16_of(y[s], j), acc, 0, 0, 0);
+    const int e = 64 * (g >> 2) + channel_of(g & 3, c);                    // result v of a lane: token 4 v + q, column c
+#pragma unroll
+    for (int v = 0; v < 4; v++) {
+      const int t = t0 + 4 * v + q;
+      if (t < T && e < E) parts[((size_t)blockIdx.x * T + t) * E + e] = acc[v];
+    }
+  }
+  const int t = t0 + (tid >> 4), d = 32 * s0 + 8 * (tid & 15), p = tid & 3;    // four lanes have a block of 32
+  if (steps > 0 && t < T && d < D) {
     const u32x4 w = *reinterpret_cast<const u32x4*>(X + (size_t)t * D + d);
     const uint32_t code = mx4_scale_code(quad_max(i8_top8(w, 0u)));
     *reinterpret_cast<uint32_t*>(codes + mx4_code_at(t, d >> 5, steps) + 4 * p) = mx4_codes8(w, mx4_scale(code));
     if (p == 0) scales[mx4_scale_at(t, d >> 5, steps)] = (char)code;
-  }
-  for (int i = tid; i < tokens * ROUTE_D; i += 256) x[i / ROUTE_D][i % ROUTE_D] = bf16_lo_to_f32(X[(size_t)(t0 + i / ROUTE_D) * D + d0 + i % ROUTE_D]);
-  __syncthreads();
-  const int ways = 256 / E, way = tid / E, ex = tid - way * E;   // the rows of Wr are dealt out to `ways` groups of E work items
-  double acc[ROUTE_T] = {};
-  if (way < ways) {
-    for (int d = way; d < ROUTE_D; d += 16 * ways) {         // 16 rows on their way at once
-      uint16_t w[16];
-#pragma unroll
-      for (int j = 0; j < 16; j++) w[j] = d + j * ways < ROUTE_D ? Wr[(size_t)(d0 + d + j * ways) * E + ex] : (uint16_t)0;
-#pragma unroll
-      for (int j = 0; j < 16; j++) {
-        if (d + j * ways >= ROUTE_D) break;
-        const float y = bf16_lo_to_f32(w[j]);
-#pragma unroll
-        for (int t = 0; t < ROUTE_T; t++)
-          if (t < tokens) acc[t] += (double)(x[t][d + j * ways] * y);
-      }
-    }
-#pragma unroll
-    for (int t = 0; t < ROUTE_T; t++)
-      if (t < tokens) sums[(t * ways + way) * E + ex] = acc[t];
-  }
-  __syncthreads();
-  for (int i = tid; i < tokens * E; i += 256) {
-    const int t = i / E, n = i - t * E;
-    double s = 0.0;
-    for (int k = 0; k < ways; k++) s += sums[(t * ways + k) * E + n];
-    parts[((size_t)blockIdx.x * T + t0 + t) * E + n] = s;
   }
 }
 
@@ -470,7 +473,7 @@ __global__ void __launch_bounds__(256) moe_pick_kernel(const double* __restrict_
   __shared__ double sums[256], chosen[MOE_MAX_K];
   __shared__ unsigned long long order[MOE_E];
   __shared__ float part[4];
-  __shared__ int count[MOE_E], cursor[MOE_E], come;
+  __shared__ int count[MOE_E], cursor[MOE_E], which[MOE_MAX_K], come;
   const int t = blockIdx.x, tid = threadIdx.x, ways = 256 / E, way = tid / E, ex = tid - way * E;
   {
     double s = 0.0;
@@ -500,7 +503,10 @@ __global__ void __launch_bounds__(256) moe_pick_kernel(const double* __restrict_
     rank = 0;
 #pragma unroll 4
     for (int i = 0; i < E; i++) rank += order[i] > mine || (order[i] == mine && i < e);
-    if (rank < k) chosen[rank] = s;
+    if (rank < k) {
+      chosen[rank] = s;
+      which[rank] = e;
+    }
   }
   __syncthreads();
   // shares: exp(l - largest) over its sum, of the chosen or of all
@@ -514,9 +520,23 @@ __global__ void __launch_bounds__(256) moe_pick_kernel(const double* __restrict_
     const float p = x / (part[0] + part[1] + part[2] + part[3]);
     picks[t * k + rank] = e;
     shares[t * k + rank] = p;
-    put(&plan->picks[t * k + rank], e);
-    put(&plan->shares[t * k + rank], p);
+    if (T == 1) {                                              // the plan by itself: the chosen experts in their order
+      int at = 0;
+      for (int i = 0; i < k; i++) at += which[i] < e;
+      plan->expert[at] = e;
+      plan->start[at] = at;
+      plan->list[at] = rank;
+      plan->share[at] = p;
+      if (rank == 0) {
+        plan->n_active = k;
+        plan->start[k] = k;
+      }
+    } else {
+      put(&plan->picks[t * k + rank], e);
+      put(&plan->shares[t * k + rank], p);
+    }
   }
+  if (T == 1) return;
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
   if (tid == 0) come = __hip_atomic_fetch_add(&plan->ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -578,20 +598,32 @@ __global__ void __launch_bounds__(256) moe_pick_kernel(const double* __restrict_
     }
 }
 
-template <int SRC, bool MOE>
-int launch_up(const UpArgs& a, int slots, hipStream_t s) {
-  const dim3 grid((unsigned)(a.F / 32), (unsigned)slots);
-  if (a.T <= 16) hipLaunchKernelGGL((few_up_kernel<SRC, 1, MOE>), grid, dim3(THREADS), 0, s, a);
-  else if (a.T <= 32 || !MOE) hipLaunchKernelGGL((few_up_kernel<SRC, 2, MOE>), grid, dim3(THREADS), 0, s, a);
-  else hipLaunchKernelGGL((few_up_kernel<SRC, MOE ? 4 : 2, MOE>), grid, dim3(THREADS), 0, s, a);
+// Waves a workgroup and features a strip: eight waves, which ask for more at once, until there are enough workgroups to have four of four waves on a CU; half strips where there
+// are fewer than the CUs.
+template <int SRC, int NT, bool MOE, int RG, int W>
+int launch_up_one(const UpArgs& a, int slots, hipStream_t s) {
+  hipLaunchKernelGGL((few_up_kernel<SRC, NT, MOE, RG, W>), dim3((unsigned)(a.F / (8 * RG)), (unsigned)slots), dim3(64 * W), 0, s, a);
   return (int)hipGetLastError();
 }
+template <int SRC, int NT, bool MOE>
+int launch_up_tokens(const UpArgs& a, int slots, hipStream_t s) {
+  if (few_up_waves(a.F / 32 * slots, NT) == 4) return launch_up_one<SRC, NT, MOE, 4, 4>(a, slots, s);
+  if constexpr (SRC == ROWS_BF16 && NT == 1)
+    if (few_up_halves(a.F / 32 * slots)) return launch_up_one<SRC, NT, MOE, 2, 8>(a, slots, s);
+  return launch_up_one<SRC, NT, MOE, 4, 8>(a, slots, s);
+}
+template <int SRC, bool MOE>
+int launch_up(const UpArgs& a, int slots, hipStream_t s) {
+  if (a.T <= 16) return launch_up_tokens<SRC, 1, MOE>(a, slots, s);
+  if (a.T <= 32 || !MOE) return launch_up_tokens<SRC, 2, MOE>(a, slots, s);
+  return launch_up_tokens<SRC, MOE ? 4 : 2, MOE>(a, slots, s);
+}
 template <bool MX4, int NT>
-int launch_down(const DownArgs& a, hipStream_t s) {
+int launch_down(const DownArgs& a, int splits, hipStream_t s) {
   auto kern = moe_down_kernel<MX4, NT>;
   static std::atomic<bool> configured[MAX_DEVICES] = {};
   if (int rc = ensure_dynamic_lds(reinterpret_cast<const void*>(kern), down_lds(MOE_TOKENS), configured)) return rc;
-  hipLaunchKernelGGL(kern, dim3((unsigned)(a.D / 16)), dim3(THREADS), down_lds(a.T), s, a);
+  hipLaunchKernelGGL(kern, dim3((unsigned)(a.D / 16), (unsigned)splits), dim3(THREADS), down_lds(a.T), s, a);
   return (int)hipGetLastError();
 }
 template <int RG, int SRC>
@@ -604,13 +636,12 @@ int launch_rows(const RowsArgs& a, hipStream_t s) {
 }  // namespace
 
 size_t moe_plan_size() { return sizeof(MoePlan); }
-size_t moe_parts_size(int T, int D, int E) { return (size_t)(D / ROUTE_D) * T * E * sizeof(double); }
+size_t moe_parts_size(int T, int D, int E) { return (size_t)((D + ROUTE_D - 1) / ROUTE_D) * T * E * sizeof(double); }
 
 int launch_moe_route(const void* X, const void* Wr, int T, int D, int E, int k, bool renormalise, void* parts, int* picks, float* shares, void* plan,
                      const Mx4Operand* x, hipStream_t s) {
-  const int n = D / ROUTE_D;
-  hipLaunchKernelGGL(moe_router_kernel, dim3((unsigned)n, (unsigned)((T + ROUTE_T - 1) / ROUTE_T)), dim3(256), 0, s, static_cast<const uint16_t*>(X),
-                     static_cast<const uint16_t*>(Wr), T, D, E, static_cast<double*>(parts), x ? x->steps : 0, x ? const_cast<char*>(x->codes) : nullptr,
+  const int n = (D + ROUTE_D - 1) / ROUTE_D;
+  hipLaunchKernelGGL(moe_router_kernel, dim3((unsigned)n, (unsigned)((T + 15) / 16)), dim3(256), 0, s, static_cast<const uint16_t*>(X), static_cast<const char*>(Wr), T, D, E, static_cast<double*>(parts), x ? x->steps : 0, x ? const_cast<char*>(x->codes) : nullptr,
                      x ? const_cast<char*>(x->scales) : nullptr);
   hipLaunchKernelGGL(moe_pick_kernel, dim3((unsigned)T), dim3(256), 0, s, static_cast<const double*>(parts), n, T, E, k, (int)renormalise, picks, shares,
                      static_cast<MoePlan*>(plan));
@@ -618,7 +649,7 @@ int launch_moe_route(const void* X, const void* Wr, int T, int D, int E, int k, 
 }
 
 int launch_moe_experts(const MoeWeights& w, const void* X, const Mx4Operand* x, int T, int D, int F, int E, int k, float c1, float c3, const void* plan, void* H,
-                       int h_rows, void* Y, hipStream_t s) {
+                       int h_rows, void* parts, void* Y, hipStream_t s) {
   UpArgs up{};
   up.w = static_cast<const char*>(w.up); up.w_stride = w.up_stride; up.scales_at = w.up_scales;
   up.K = D; up.F = F; up.T = T; up.steps = w.mx4 ? mx4_steps(D) : D / 32; up.gate = Gate{c1, c3};
@@ -635,8 +666,14 @@ int launch_moe_experts(const MoeWeights& w, const void* X, const Mx4Operand* x, 
   d.steps = w.mx4 ? mx4_steps(F) : F / 32; d.F = F; d.D = D; d.T = T; d.k = k;
   d.h = up.h; d.h_scales = h.scales; d.h_steps = h.steps;
   d.plan = up.plan; d.out = static_cast<uint16_t*>(Y);
-  if (T <= 16) return w.mx4 ? launch_down<true, 1>(d, s) : launch_down<false, 1>(d, s);
-  return w.mx4 ? launch_down<true, 4>(d, s) : launch_down<false, 4>(d, s);
+  d.parts = static_cast<float*>(parts);
+  const int splits = moe_down_splits(D / 16, (T * k < E ? T * k : E) * ((d.steps + 7) / 8));
+  const int rc = T <= 16 ? (w.mx4 ? launch_down<true, 1>(d, splits, s) : launch_down<false, 1>(d, splits, s))
+                         : (w.mx4 ? launch_down<true, 4>(d, splits, s) : launch_down<false, 4>(d, splits, s));
+  if (rc || splits == 1) return rc;
+  hipLaunchKernelGGL((edge_sum_kernel<false>), dim3((unsigned)((D / 4 * T + 255) / 256)), dim3(256), 0, s, static_cast<const uint32_t*>(parts), splits, D, T, I8Scales{},
+                     static_cast<uint16_t*>(Y));
+  return (int)hipGetLastError();
 }
 
 // X: bf16 rows; x: instead of them

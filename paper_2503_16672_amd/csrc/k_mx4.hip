@@ -162,11 +162,6 @@ __global__ void __launch_bounds__(256) operand_weight_kernel(const void* __restr
   }
 }
 
-__global__ void __launch_bounds__(256) copy16_kernel(const u32x4* __restrict__ from, u32x4* __restrict__ to, size_t n) {
-  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-  if (i < n) to[i] = from[i];
-}
-
 template <class Epi, int AM, int BN>
 int launch_mx4_tile(Mx4Gemm g, const typename Epi::Args& ea, int splits, int part, hipStream_t s) {
   using G = Mx4Geo<AM, BN>;
@@ -233,12 +228,6 @@ int launch_bf16_weight(const void* W, int K, int N, bool halves, int count, void
                      halves ? N / 2 : 0, K / 32, static_cast<char*>(out), nullptr, (size_t)K * N, (size_t)bf16_operand_size(N, K), (size_t)0);
   return (int)hipGetLastError();
 }
-int launch_copy16(const void* from, void* to, size_t bytes, hipStream_t s) {
-  const size_t n = bytes / 16;
-  hipLaunchKernelGGL(copy16_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, static_cast<const u32x4*>(from), static_cast<u32x4*>(to), n);
-  return (int)hipGetLastError();
-}
-
 int launch_mx4_tokens(const void* X, int T, int K, const Mx4Operand& o, hipStream_t s) {
   const long long waves = (long long)((T + 15) / 16) * ((o.steps + 3) / 4);
   hipLaunchKernelGGL(mx4_tokens_kernel, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, static_cast<const uint16_t*>(X), T, K, o.steps, const_cast<char*>(o.codes),

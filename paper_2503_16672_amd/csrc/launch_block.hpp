@@ -65,7 +65,6 @@ Mx4Operand mx4_operand(const void* p, int rows, int K);
 int launch_mx4_weight(const void* W, int K, int N, bool halves, int count, void* out, hipStream_t s);
 int launch_bf16_weight(const void* W, int K, int N, bool halves, int count, void* out, hipStream_t s);
 int launch_mx4_weight_codes(const void* codes, const void* scales, int K, int N, bool halves, void* out, hipStream_t s);
-int launch_copy16(const void* from, void* to, size_t bytes, hipStream_t s);   // 16-byte aligned, a multiple of 16 bytes
 int launch_mx4_tokens(const void* X, int T, int K, const Mx4Operand& out, hipStream_t s);
 size_t mx4_split_scratch(int M, int N, int K);
 int launch_mx4_product(const Mx4Operand& w, int M, const Mx4Operand& x, int T, void* Y, const Scratch& scratch, hipStream_t s);
@@ -82,6 +81,6 @@ size_t moe_plan_size();                          // zero before its first use
 int launch_moe_route(const void* X, const void* Wr, int T, int D, int E, int k, bool renormalise, void* parts, int* picks, float* shares, void* plan,
                      const Mx4Operand* x, hipStream_t s);   // x: the tokens as mx4 go there
 int launch_moe_experts(const MoeWeights& w, const void* X, const Mx4Operand* x, int T, int D, int F, int E, int k, float c1, float c3, const void* plan, void* H,
-                       int h_rows, void* Y, hipStream_t s);
+                       int h_rows, void* parts, void* Y, hipStream_t s);
 
 }  // namespace ffn24

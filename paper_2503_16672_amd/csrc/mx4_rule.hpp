@@ -39,4 +39,16 @@ inline bool mx4_few_fused(int T) { return T <= 16; }
 inline bool mx4_few(int T, int, int) { return T <= FEW_MX4_TOKENS; }
 inline bool mx4_few_gated(int T, int, int) { return T <= FEW_MX4_TOKENS; }
 
+// Experts: waves a workgroup of the up projection of `strips` strips, half strips, and over how many workgroups a strip's experts of the down projection are dealt out
+// (`units`: of eight steps, at most, that a strip has)
+inline int few_up_waves(int strips, int nt) { return strips >= 1024 && nt == 1 ? 4 : 8; }
+inline bool few_up_halves(int strips) { return strips < 256; }
+constexpr int MOE_SPLITS = 8;
+inline int moe_down_splits(int strips, int units) {
+  const int fill = 256 / strips, most = units / 16;              // (two units a wave at least)
+  int s = fill < most ? fill : most;
+  s = s < MOE_SPLITS ? s : MOE_SPLITS;
+  return s > 2 ? s : 1;
+}
+
 }  // namespace ffn24
