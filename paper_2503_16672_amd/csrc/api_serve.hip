@@ -85,14 +85,14 @@ int mx4_weight_codes(const void* codes, const void* scales, int64_t K, int64_t N
 
 int64_t linear_mx4_scratch(int64_t T, int64_t K, int64_t N) {
   if (!tokens(T) || !sizes(K, N)) return -1;
-  if (T == 0 || mx4_few_fused((int)T)) return 0;
+  if (T == 0 || mx4_few_fused((int)T, (int)K)) return 0;
   return up16(mx4_operand_size(T, K)) + (mx4_few((int)T, (int)K, (int)N) ? 0 : (int64_t)mx4_split_scratch((int)N, (int)T, (int)K));
 }
 
 int linear_mx4(const void* X, int64_t T, const void* weight, int64_t K, int64_t N, void* Y, void* scratch, void* stream) {
   if (!tokens(T) || !sizes(K, N)) return FFN24_ERR_SHAPE;
   if (T == 0) return FFN24_OK;
-  const bool fused = mx4_few_fused((int)T);
+  const bool fused = mx4_few_fused((int)T, (int)K);
   if (!X || !weight || !Y || (!scratch && !fused)) return FFN24_ERR_NULL;
   if (misaligned(X, weight, Y, scratch)) return FFN24_ERR_ALIGN;
   hipStream_t s = static_cast<hipStream_t>(stream);
@@ -159,7 +159,7 @@ int gated_mx4_fwd(gated_mx4_ctx* c, const void* X, int64_t T, void* Y, void* str
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int t = (int)T, D = (int)c->D, F = (int)c->F;
   const Mx4Operand wgu = mx4_operand(c->Wgu, 2 * F, D), wd = mx4_operand(c->Wd, D, F), x = mx4_operand(c->X, (int)c->T, D), h = mx4_operand(c->H, (int)c->T, F);
-  const bool few = mx4_few_gated(t, D, F), fused = few && mx4_few_fused(t);
+  const bool few = mx4_few_gated(t, D, F), fused = few && mx4_few_fused(t, D);
   if (!fused && launch_mx4_tokens(X, t, D, x, s)) return FFN24_ERR_HIP;
   if (few ? launch_few_mx4_up(wgu, X, fused ? nullptr : &x, t, D, F, c->gate.c1, c->gate.c3, h, s)
           : launch_mx4_gated_up(wgu, F, x, t, c->gate.c1, c->gate.c3, h, s)) return FFN24_ERR_HIP;

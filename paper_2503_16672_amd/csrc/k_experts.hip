@@ -44,42 +44,65 @@ __device__ __forceinline__ void settle(f32x4 (&acc)[RG][NT]) {
     for (int i = 0; i < NT; i++) asm volatile("" : "+v"(acc[g][i]));
 }
 
-// Tokens of a product: rows of bf16 [..][K] as they are, or to mx4 on the way; or the mx4 operand form
-enum { ROWS_BF16 = 0, ROWS_TO_MX4 = 1, OPERAND_MX4 = 2 };
-struct Tokens { const char* p; const char* scales; int K, steps; };
+// Tokens of a product: rows of bf16 [..][K]; the mx4 operand form; or (a small T K) rows of bf16 that the workgroup brings to mx4 in its LDS, codes [K / 32][T][16 bytes] and scales
+// [K / 32][T], while its first weights are on their way
+enum { ROWS_BF16 = 0, OPERAND_MX4 = 1, LDS_MX4 = 2 };
+struct Tokens { const char* p; const char* scales; int K, steps, T; };
+constexpr int LDS_PIECES = MX4_FUSED_VALUES / 8 / THREADS;     // of 8 values a work item
+
+struct StagedTokens {
+  u32x4 w[LDS_PIECES];
+  __device__ __forceinline__ void load(const char* X, int pieces) {
+#pragma unroll
+    for (int j = 0; j < LDS_PIECES; j++) {
+      const int i = j * THREADS + (int)threadIdx.x;
+      if (j * THREADS < pieces) w[j] = i < pieces ? reinterpret_cast<const u32x4*>(X)[i] : u32x4{0u, 0u, 0u, 0u};
+    }
+  }
+  // (a row is a whole number of blocks, so the four lanes of a block are all there or none)
+  __device__ __forceinline__ void store(char* codes, char* scales, int pieces, int K, int T) const {
+    const int per = K / 8, p = threadIdx.x & 3;
+#pragma unroll
+    for (int j = 0; j < LDS_PIECES; j++) {
+      const int i = j * THREADS + (int)threadIdx.x;
+      if (j * THREADS >= pieces) break;
+      const uint32_t code = mx4_scale_code(quad_max(mx4_top8(w[j])));
+      const int t = i / per, at = ((i - t * per) >> 2) * T + t;
+      if (i < pieces) {
+        *reinterpret_cast<uint32_t*>(codes + at * 16 + 4 * p) = mx4_codes8(w[j], mx4_scale(code));
+        if (p == 0) scales[at] = (char)code;
+      }
+    }
+  }
+};
 
 // U steps of RG groups of 16 channels, and of the first NP groups of 16 tokens, on their way.  The tokens are asked for first: loads come back in order, so what is asked
 // for behind the weights would wait for them.
 template <int SRC, int RG, int U, int NP, int GS = 1>   // GS: from a group to the next of the strip's
 struct Unit {
   static constexpr bool MX4 = SRC != ROWS_BF16;
-  static constexpr int SU = MX4 ? (U + 3) / 4 : 1, XW = SRC == ROWS_TO_MX4 ? 4 : 1, KQ = MX4 ? 32 : 8, KS = 4 * KQ;
-  u32x4 w[U][RG], x[U][NP][XW];
+  static constexpr int SU = MX4 ? (U + 3) / 4 : 1, XU = SRC == LDS_MX4 ? 1 : U;
+  u32x4 w[U][RG], x[XU][NP];
   uint32_t sw[SU][RG], sx[SRC == OPERAND_MX4 ? SU : 1][NP];
 
-  // the lane's words of token row `row` in step s
-  static __device__ __forceinline__ void token(const Tokens& t, int row, bool on, int s, int q, u32x4 (&x)[XW]) {
-    const int k = KS * s + KQ * q;
-#pragma unroll
-    for (int i = 0; i < XW; i++) x[i] = u32x4{0u, 0u, 0u, 0u};
-    if (!on) return;
-    if constexpr (SRC == OPERAND_MX4) {
-      x[0] = *reinterpret_cast<const u32x4*>(t.p + mx4_code_at(row, 4 * s + q, t.steps));
-    } else if (k < t.K) {
-#pragma unroll
-      for (int i = 0; i < XW; i++) x[i] = *reinterpret_cast<const u32x4*>(t.p + ((size_t)row * t.K + k + 8 * i) * 2);
-    }
+  // the lane's 16 bytes of token row `row` in step s, and its scales of the four steps of s
+  static __device__ __forceinline__ u32x4 token(const Tokens& t, int row, bool on, int s, int q) {
+    if (!on) return u32x4{0u, 0u, 0u, 0u};
+    if constexpr (SRC == OPERAND_MX4) return *reinterpret_cast<const u32x4*>(t.p + mx4_code_at(row, 4 * s + q, t.steps));
+    return *reinterpret_cast<const u32x4*>(t.p + ((size_t)row * t.K + 32 * s + 8 * q) * 2);
   }
-  static __device__ __forceinline__ uint32_t token_scales(const Tokens& t, int row, bool on, int s, int q) {   // of the four steps of s
+  static __device__ __forceinline__ uint32_t token_scales(const Tokens& t, int row, bool on, int s, int q) {
     return on ? *reinterpret_cast<const uint32_t*>(t.scales + (mx4_scale_at(row, 4 * s + q, t.steps) & ~(size_t)3)) : 0u;
   }
   // from step s0 (a multiple of U) on; steps beyond the last read the last one and are not used
   __device__ __forceinline__ void load(const Strip& p, const Tokens& t, const int (&row)[NP], const bool (&on)[NP], int s0, int lane) {
     const int q = lane >> 4;
+    if constexpr (SRC != LDS_MX4) {
 #pragma unroll
-    for (int j = 0; j < U; j++)
+      for (int j = 0; j < U; j++)
 #pragma unroll
-      for (int i = 0; i < NP; i++) token(t, row[i], on[i], min(s0 + j, p.steps - 1), q, x[j][i]);
+        for (int i = 0; i < NP; i++) x[j][i] = token(t, row[i], on[i], min(s0 + j, p.steps - 1), q);
+    }
     if constexpr (SRC == OPERAND_MX4) {
 #pragma unroll
       for (int j = 0; j < SU; j++)
@@ -101,28 +124,13 @@ struct Unit {
       for (int g = 0; g < RG; g++) w[j][g] = ld_stream(reinterpret_cast<const u32x4*>(at + g * GS * 1024));
     }
   }
+  // sx: the scale in the low byte
   template <int NT>
-  __device__ __forceinline__ void op(int j, int i, int s0, const u32x4 (&v)[XW], uint32_t scales, f32x4 (&acc)[RG][NT]) const {
-    if constexpr (!MX4) {
+  __device__ __forceinline__ void op(int j, int i, int s0, const u32x4& v, uint32_t sx, f32x4 (&acc)[RG][NT]) const {
 #pragma unroll
-      for (int g = 0; g < RG; g++) acc[g][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w[j][g]), __builtin_bit_cast(bf16x8, v[0]), acc[g][i], 0, 0, 0);
-    } else {
-      const int byte = 8 * ((s0 + j) & 3);
-      i32x4 b;
-      uint32_t sb;
-      if constexpr (SRC == ROWS_TO_MX4) {
-        uint32_t top = 0u;
-#pragma unroll
-        for (int d = 0; d < 4; d++) top = i8_top8(v[d], top);
-        sb = mx4_scale_code(top);
-#pragma unroll
-        for (int d = 0; d < 4; d++) b[d] = (int)mx4_codes8(v[d], mx4_scale(sb));
-      } else {
-        b = __builtin_bit_cast(i32x4, v[0]);
-        sb = scales >> byte;
-      }
-#pragma unroll
-      for (int g = 0; g < RG; g++) op16_mx4_few<RG>(w[j][g], __builtin_bit_cast(u32x4, b), sw[j / 4][g] >> byte, sb, acc[g][i]);
+    for (int g = 0; g < RG; g++) {
+      if constexpr (MX4) op16_mx4_few<RG>(w[j][g], v, sw[j / 4][g] >> (8 * ((s0 + j) & 3)), sx, acc[g][i]);
+      else acc[g][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w[j][g]), __builtin_bit_cast(bf16x8, v), acc[g][i], 0, 0, 0);
     }
   }
   // the ops of the unit for `groups` groups of tokens; those from NP on are asked for here
@@ -131,15 +139,18 @@ struct Unit {
 #pragma unroll
     for (int j = 0; j < U; j++) {
       if (s0 + j >= steps) break;
+      const int byte = 8 * ((s0 + j) & 3);
 #pragma unroll
       for (int i = 0; i < NT; i++) {
         if (i > 0 && i >= groups) break;
-        if (i < NP) {
-          op(j, i, s0, x[j][i < NP ? i : 0], sx[SRC == OPERAND_MX4 ? j / 4 : 0][i < NP ? i : 0], acc);
+        if constexpr (SRC == LDS_MX4) {
+          const int kb = 4 * (s0 + j) + q, at = kb * t.T + row[i];
+          const bool there = on[i] && 32 * kb < t.K;
+          op(j, i, s0, there ? *reinterpret_cast<const u32x4*>(t.p + at * 16) : u32x4{0u, 0u, 0u, 0u}, there ? (uint32_t)(uint8_t)t.scales[at] : 0u, acc);
+        } else if (i < NP) {
+          op(j, i, s0, x[j][i < NP ? i : 0], SRC == OPERAND_MX4 ? sx[SRC == OPERAND_MX4 ? j / 4 : 0][i < NP ? i : 0] >> byte : 0u, acc);
         } else {
-          u32x4 v[XW];
-          token(t, row[i], on[i], s0 + j, q, v);
-          op(j, i, s0, v, SRC == OPERAND_MX4 ? token_scales(t, row[i], on[i], s0 + j, q) : 0u, acc);
+          op(j, i, s0, token(t, row[i], on[i], s0 + j, q), SRC == OPERAND_MX4 ? token_scales(t, row[i], on[i], s0 + j, q) >> byte : 0u, acc);
         }
       }
     }
@@ -179,9 +190,10 @@ struct UpArgs {
 template <int SRC, int NT, bool MOE, int RG, int W>
 __global__ void __launch_bounds__(64 * W, NT == 1 ? 4 : 2) few_up_kernel(UpArgs e) {
   constexpr bool MX4 = SRC != ROWS_BF16;
-  constexpr int U = SRC == ROWS_TO_MX4 ? 1 : 8 / RG, NP = NT <= 2 ? NT : 1, FEATS = 8 * RG;
+  constexpr int U = 8 / RG, NP = NT <= 2 ? NT : 1, FEATS = 8 * RG;
   static_assert(RG == 4 || (RG == 2 && !MX4), "whole blocks of 32 features");
   __shared__ __attribute__((aligned(16))) float red[W * 16 * RG * RED];
+  extern __shared__ __attribute__((aligned(16))) char staged_lds[];   // LDS_MX4: T K 17 / 32 bytes
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, q = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // whole blocks are 4 KiB a step and cover an L2's channels by themselves: they go round the XCDs, which then share the experts that were chosen (the last slots may have none)
   const unsigned at = blockIdx.y * gridDim.x + blockIdx.x, id = RG == 4 ? at : run_of(at, gridDim.x * gridDim.y), slot = id / gridDim.x;
@@ -195,7 +207,10 @@ __global__ void __launch_bounds__(64 * W, NT == 1 ? 4 : 2) few_up_kernel(UpArgs 
   }
   const char* codes = e.w + (size_t)expert * e.w_stride;
   const Strip w{codes + (size_t)block * e.steps * MX4_PANEL + half * 1024, codes + e.scales_at + (size_t)block * ((e.steps + 3) >> 2) * 1024, e.steps};
-  const Tokens x{e.x, e.x_scales, e.K, e.steps};
+  Tokens x{e.x, e.x_scales, e.K, e.steps, e.T};
+  const int pieces = e.T * e.K / 8;
+  StagedTokens staged;
+  if constexpr (SRC == LDS_MX4) staged.load(e.x, pieces);
 
   // (no expert has more tokens than there are: T <= 16 NT)
   int row[NT], row_p[NP];
@@ -220,6 +235,13 @@ __global__ void __launch_bounds__(64 * W, NT == 1 ? 4 : 2) few_up_kernel(UpArgs 
   Unit<SRC, RG, U, NP, RG == 4 ? 1 : 2> now, next;
   int s = wave * U;
   if (s < e.steps) now.load(w, x, row_p, on_p, s, lane);
+  if constexpr (SRC == LDS_MX4) {
+    static_assert(W == WAVES, "staged by all work items");
+    x.p = staged_lds;
+    x.scales = staged_lds + e.T * e.K / 2;
+    staged.store(staged_lds, staged_lds + e.T * e.K / 2, pieces, e.K, e.T);
+    __syncthreads();
+  }
   for (; s < e.steps; s += W * U) {
     const bool more = s + W * U < e.steps;
     if (more) next.load(w, x, row_p, on_p, s + W * U, lane);
@@ -275,13 +297,17 @@ struct RowsArgs {
   uint16_t* out;
 };
 template <int RG, int NT, int SRC>
-__global__ void __launch_bounds__(THREADS, NT == 1 && (RG > 1 || SRC == ROWS_TO_MX4) ? 4 : 2) few_rows_kernel(RowsArgs e) {
-  constexpr int U = SRC == ROWS_TO_MX4 ? (RG == 4 ? 1 : 2) : RG == 1 ? 8 : RG == 2 ? 4 : 2;
+__global__ void __launch_bounds__(THREADS, NT == 1 && (RG > 1 || SRC == LDS_MX4) ? 4 : 2) few_rows_kernel(RowsArgs e) {
+  constexpr int U = 8 / RG;
   __shared__ __attribute__((aligned(16))) float red[WAVES * 16 * RG * RED];
+  extern __shared__ __attribute__((aligned(16))) char staged_lds[];
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, q = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int strip = (int)run_of(blockIdx.x, gridDim.x), block = strip / (4 / RG), g0 = strip % (4 / RG) * RG;
   const Strip w{e.w + (size_t)block * e.steps * MX4_PANEL + g0 * 1024, e.w_scales + (size_t)block * ((e.steps + 3) >> 2) * 1024 + g0 * 256, e.steps};
-  const Tokens x{e.x, e.x_scales, e.K, e.x_steps};
+  Tokens x{e.x, e.x_scales, e.K, e.x_steps, e.T};
+  const int pieces = e.T * e.K / 8;
+  StagedTokens staged;
+  if constexpr (SRC == LDS_MX4) staged.load(e.x, pieces);
   int row[NT];
   bool on[NT];
 #pragma unroll
@@ -297,6 +323,12 @@ __global__ void __launch_bounds__(THREADS, NT == 1 && (RG > 1 || SRC == ROWS_TO_
   Unit<SRC, RG, U, NT> now, next;
   int s = wave * U;
   if (s < e.steps) now.load(w, x, row, on, s, lane);
+  if constexpr (SRC == LDS_MX4) {
+    x.p = staged_lds;
+    x.scales = staged_lds + e.T * e.K / 2;
+    staged.store(staged_lds, staged_lds + e.T * e.K / 2, pieces, e.K, e.T);
+    __syncthreads();
+  }
   for (; s < e.steps; s += WAVES * U) {
     const bool more = s + WAVES * U < e.steps;
     if (more) next.load(w, x, row, on, s + WAVES * U, lane);
@@ -354,7 +386,7 @@ __global__ void __launch_bounds__(THREADS, 2) moe_down_kernel(DownArgs e) {
   if (tid <= n_active) start[tid] = e.plan->start[tid];
   __syncthreads();
   float* mine = sums + wave * e.T * SUM;
-  const Tokens x{e.h, e.h_scales, e.F, e.h_steps};
+  const Tokens x{e.h, e.h_scales, e.F, e.h_steps, 0};
   const int units = (e.steps + U - 1) / U, total = n_active * units;   // units of U steps, the experts' one after the other, dealt out to the waves
   // of unit i: the strip, and the lane's row of the first 16 of the expert's tokens
   auto strip_of = [&](int i) {
@@ -456,7 +488,7 @@ __global__ void __launch_bounds__(256) moe_router_kernel(const uint16_t* __restr
   const int t = t0 + (tid >> 4), d = 32 * s0 + 8 * (tid & 15), p = tid & 3;    // four lanes have a block of 32
   if (steps > 0 && t < T && d < D) {
     const u32x4 w = *reinterpret_cast<const u32x4*>(X + (size_t)t * D + d);
-    const uint32_t code = mx4_scale_code(quad_max(i8_top8(w, 0u)));
+    const uint32_t code = mx4_scale_code(quad_max(mx4_top8(w)));
     *reinterpret_cast<uint32_t*>(codes + mx4_code_at(t, d >> 5, steps) + 4 * p) = mx4_codes8(w, mx4_scale(code));
     if (p == 0) scales[mx4_scale_at(t, d >> 5, steps)] = (char)code;
   }
@@ -598,25 +630,35 @@ __global__ void __launch_bounds__(256) moe_pick_kernel(const double* __restrict_
     }
 }
 
+int staged_bytes(int T, int K) { return T * K / 2 + T * K / 32; }
+
 // Waves a workgroup and features a strip: eight waves, which ask for more at once, until there are enough workgroups to have four of four waves on a CU; half strips where there
 // are fewer than the CUs.
 template <int SRC, int NT, bool MOE, int RG, int W>
 int launch_up_one(const UpArgs& a, int slots, hipStream_t s) {
-  hipLaunchKernelGGL((few_up_kernel<SRC, NT, MOE, RG, W>), dim3((unsigned)(a.F / (8 * RG)), (unsigned)slots), dim3(64 * W), 0, s, a);
+  auto kern = few_up_kernel<SRC, NT, MOE, RG, W>;
+  int lds = 0;
+  if constexpr (SRC == LDS_MX4) {
+    static std::atomic<bool> configured[MAX_DEVICES] = {};
+    if (int rc = ensure_dynamic_lds(reinterpret_cast<const void*>(kern), staged_bytes(1, MX4_FUSED_VALUES), configured)) return rc;
+    lds = staged_bytes(a.T, a.K);
+  }
+  hipLaunchKernelGGL(kern, dim3((unsigned)(a.F / (8 * RG)), (unsigned)slots), dim3(64 * W), lds, s, a);
   return (int)hipGetLastError();
 }
 template <int SRC, int NT, bool MOE>
 int launch_up_tokens(const UpArgs& a, int slots, hipStream_t s) {
-  if (few_up_waves(a.F / 32 * slots, NT) == 4) return launch_up_one<SRC, NT, MOE, 4, 4>(a, slots, s);
+  if constexpr (SRC != LDS_MX4 && NT == 1)
+    if (few_up_waves(a.F / 32 * slots) == 4) return launch_up_one<SRC, NT, MOE, 4, 4>(a, slots, s);
   if constexpr (SRC == ROWS_BF16 && NT == 1)
     if (few_up_halves(a.F / 32 * slots)) return launch_up_one<SRC, NT, MOE, 2, 8>(a, slots, s);
   return launch_up_one<SRC, NT, MOE, 4, 8>(a, slots, s);
 }
-template <int SRC, bool MOE>
-int launch_up(const UpArgs& a, int slots, hipStream_t s) {
-  if (a.T <= 16) return launch_up_tokens<SRC, 1, MOE>(a, slots, s);
-  if (a.T <= 32 || !MOE) return launch_up_tokens<SRC, 2, MOE>(a, slots, s);
-  return launch_up_tokens<SRC, MOE ? 4 : 2, MOE>(a, slots, s);
+template <int SRC>
+int launch_moe_up(const UpArgs& a, int slots, hipStream_t s) {
+  if (a.T <= 16) return launch_up_tokens<SRC, 1, true>(a, slots, s);
+  if (a.T <= 32) return launch_up_tokens<SRC, 2, true>(a, slots, s);
+  return launch_up_tokens<SRC, 4, true>(a, slots, s);
 }
 template <bool MX4, int NT>
 int launch_down(const DownArgs& a, int splits, hipStream_t s) {
@@ -626,12 +668,23 @@ int launch_down(const DownArgs& a, int splits, hipStream_t s) {
   hipLaunchKernelGGL(kern, dim3((unsigned)(a.D / 16), (unsigned)splits), dim3(THREADS), down_lds(a.T), s, a);
   return (int)hipGetLastError();
 }
-template <int RG, int SRC>
-int launch_rows(const RowsArgs& a, hipStream_t s) {
+template <int RG, int SRC, int NT>
+int launch_rows_tokens(const RowsArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)(RG == 1 ? (a.N + 31) / 32 * 2 : (a.N + 16 * RG - 1) / (16 * RG)));   // (two groups of 16 share 32 channels)
-  if (a.T <= 16) hipLaunchKernelGGL((few_rows_kernel<RG, 1, SRC>), grid, dim3(THREADS), 0, s, a);
-  else hipLaunchKernelGGL((few_rows_kernel<RG, 2, SRC>), grid, dim3(THREADS), 0, s, a);
+  auto kern = few_rows_kernel<RG, NT, SRC>;
+  int lds = 0;
+  if constexpr (SRC == LDS_MX4) {
+    static std::atomic<bool> configured[MAX_DEVICES] = {};
+    if (int rc = ensure_dynamic_lds(reinterpret_cast<const void*>(kern), staged_bytes(1, MX4_FUSED_VALUES), configured)) return rc;
+    lds = staged_bytes(a.T, a.K);
+  }
+  hipLaunchKernelGGL(kern, grid, dim3(THREADS), lds, s, a);
   return (int)hipGetLastError();
+}
+template <int RG>
+int launch_rows(const RowsArgs& a, bool staged, hipStream_t s) {
+  if (staged) return launch_rows_tokens<RG, LDS_MX4, 1>(a, s);
+  return a.T <= 16 ? launch_rows_tokens<RG, OPERAND_MX4, 1>(a, s) : launch_rows_tokens<RG, OPERAND_MX4, 2>(a, s);
 }
 }  // namespace
 
@@ -660,7 +713,7 @@ int launch_moe_experts(const MoeWeights& w, const void* X, const Mx4Operand* x, 
   up.h_steps = h.steps;
   up.plan = static_cast<const MoePlan*>(plan); up.k = k;
   const int slots = T * k < E ? T * k : E;
-  if (const int rc = w.mx4 ? launch_up<OPERAND_MX4, true>(up, slots, s) : launch_up<ROWS_BF16, true>(up, slots, s)) return rc;
+  if (const int rc = w.mx4 ? launch_moe_up<OPERAND_MX4>(up, slots, s) : launch_moe_up<ROWS_BF16>(up, slots, s)) return rc;
   DownArgs d{};
   d.w = static_cast<const char*>(w.down); d.w_stride = w.down_stride; d.scales_at = w.down_scales;
   d.steps = w.mx4 ? mx4_steps(F) : F / 32; d.F = F; d.D = D; d.T = T; d.k = k;
@@ -683,15 +736,15 @@ int launch_few_mx4_up(const Mx4Operand& w, const void* X, const Mx4Operand* x, i
   up.K = D; up.F = F; up.T = T; up.steps = w.steps; up.gate = Gate{c1, c3};
   up.x = x ? x->codes : static_cast<const char*>(X); up.x_scales = x ? x->scales : nullptr;
   up.h = const_cast<char*>(h.codes); up.h_scales = const_cast<char*>(h.scales); up.h_steps = h.steps;
-  return x ? launch_up<OPERAND_MX4, false>(up, 1, s) : launch_up<ROWS_TO_MX4, false>(up, 1, s);
+  if (!x) return launch_up_tokens<LDS_MX4, 1, false>(up, 1, s);
+  return T <= 16 ? launch_up_tokens<OPERAND_MX4, 1, false>(up, 1, s) : launch_up_tokens<OPERAND_MX4, 2, false>(up, 1, s);
 }
 // Strips of 64, 32 or 16 channels: at least 512 workgroups if there are that many
 int launch_few_mx4_rows(const Mx4Operand& w, int K, int N, const void* X, const Mx4Operand* x, int T, void* Y, hipStream_t s) {
   RowsArgs a{w.codes, w.scales, w.steps, K, N, T, static_cast<const char*>(X), nullptr, 0, static_cast<uint16_t*>(Y)};
   if (x) { a.x = x->codes; a.x_scales = x->scales; a.x_steps = x->steps; }
-  if (N >= 512 * 64) return x ? launch_rows<4, OPERAND_MX4>(a, s) : launch_rows<4, ROWS_TO_MX4>(a, s);
-  if (N >= 512 * 32) return x ? launch_rows<2, OPERAND_MX4>(a, s) : launch_rows<2, ROWS_TO_MX4>(a, s);
-  return x ? launch_rows<1, OPERAND_MX4>(a, s) : launch_rows<1, ROWS_TO_MX4>(a, s);
+  if (N >= 512 * 64) return launch_rows<4>(a, !x, s);
+  return N >= 512 * 32 ? launch_rows<2>(a, !x, s) : launch_rows<1>(a, !x, s);
 }
 
 }  // namespace ffn24

@@ -13,7 +13,7 @@ template <bool F32> struct Eight;
 template <> struct Eight<false> {
   u32x4 w;
   __device__ __forceinline__ void load(const void* p, size_t i) { w = ld_stream(static_cast<const u32x4*>(p) + i); }
-  __device__ __forceinline__ uint32_t top() const { return i8_top8(w, 0u); }
+  __device__ __forceinline__ uint32_t top() const { return mx4_top8(w); }
   __device__ __forceinline__ uint32_t codes(float s) const { return mx4_codes8(w, s); }
 };
 template <> struct Eight<true> {
@@ -108,7 +108,7 @@ __global__ void __launch_bounds__(256) mx4_tokens_kernel(const uint16_t* __restr
   char* out = codes + mx4_code_at(16 * group, 16 * S, steps) + c * 16 + 4 * p;
 #pragma unroll
   for (int i = 0; i < 16; i++) {
-    const uint32_t code = mx4_scale_code(quad_max(i8_top8(w[i], 0u)));
+    const uint32_t code = mx4_scale_code(quad_max(mx4_top8(w[i])));
     if ((i & 3) == p) mine |= code << (8 * (i >> 2));
     if (4 * S + (i >> 2) < steps) *reinterpret_cast<uint32_t*>(out + (size_t)(i >> 2) * MX4_PANEL + (i & 3) * 256) = mx4_codes8(w[i], mx4_scale(code));
   }
@@ -144,7 +144,7 @@ __global__ void __launch_bounds__(256) operand_weight_kernel(const void* __restr
       } else {
         uint32_t top = 0u;
 #pragma unroll
-        for (int j = 0; j < 4; j++) top = i8_top8(v[j], top);
+        for (int j = 0; j < 4; j++) top = max(top, mx4_top8(v[j]));
         code = mx4_scale_code(top);
 #pragma unroll
         for (int j = 0; j < 4; j++) o[j] = mx4_codes8(v[j], mx4_scale(code));

@@ -45,6 +45,11 @@ __device__ __forceinline__ uint32_t mx4_codes8(const float (&x)[8], float s) {
   o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, x[4], x[5], s, 2);
   return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, x[6], x[7], s, 3);
 }
+// the bits of the largest magnitude of 8 bf16 values, as an fp32's
+__device__ __forceinline__ uint32_t mx4_top8(const u32x4& w) {
+  const uint32_t m = pk_max16(pk_max16(w[0] & 0x7FFF7FFFu, w[1] & 0x7FFF7FFFu), pk_max16(w[2] & 0x7FFF7FFFu, w[3] & 0x7FFF7FFFu));
+  return max(m << 16, m & 0xFFFF0000u);
+}
 __device__ __forceinline__ uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7FFFFFFFu; }
 
 template <int P> __device__ __forceinline__ uint32_t quad_max(uint32_t x) { return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, P, 0xF, 0xF, true)); }
