@@ -159,7 +159,7 @@ int gated_mx4_fwd(gated_mx4_ctx* c, const void* X, int64_t T, void* Y, void* str
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int t = (int)T, D = (int)c->D, F = (int)c->F;
   const Mx4Operand wgu = mx4_operand(c->Wgu, 2 * F, D), wd = mx4_operand(c->Wd, D, F), x = mx4_operand(c->X, (int)c->T, D), h = mx4_operand(c->H, (int)c->T, F);
-  const bool few = mx4_few_gated(t, D, F), fused = few && mx4_few_fused(t, D);
+  const bool few = mx4_few_gated(t), fused = few && mx4_few_fused(t, D);
   if (!fused && launch_mx4_tokens(X, t, D, x, s)) return FFN24_ERR_HIP;
   if (few ? launch_few_mx4_up(wgu, X, fused ? nullptr : &x, t, D, F, c->gate.c1, c->gate.c3, h, s)
           : launch_mx4_gated_up(wgu, F, x, t, c->gate.c1, c->gate.c3, h, s)) return FFN24_ERR_HIP;
@@ -222,12 +222,11 @@ int moe_fwd(moe_ctx* c, const void* X, int64_t T, void* Y, void* experts, void* 
   if (misaligned(X, Y, experts, shares)) return FFN24_ERR_ALIGN;
   if (int rc = check_device(c->device)) return rc;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const int t = (int)T, D = (int)c->D, F = (int)c->F, E = (int)c->E, k = (int)c->k;
-  int* picks = static_cast<int*>(experts ? experts : c->picks);
-  float* p = static_cast<float*>(experts ? shares : c->shares);
-  const Mx4Operand x = mx4_operand(c->X, (int)c->T, D);
-  if (launch_moe_route(X, c->Wr, t, D, E, k, c->renormalise != 0, c->parts, picks, p, c->plan, c->w.mx4 ? &x : nullptr, s)) return FFN24_ERR_HIP;
-  return done(launch_moe_experts(c->w, X, &x, t, D, F, E, k, c->gate.c1, c->gate.c3, c->plan, c->H, (int)(c->T * k), c->sums, Y, s));
+  const MoeCall m{X, c->Wr, (int)T, (int)c->D, (int)c->F, (int)c->E, (int)c->k, c->renormalise != 0, c->parts, c->plan, static_cast<int*>(experts ? experts : c->picks),
+                  static_cast<float*>(experts ? shares : c->shares), c->H, (int)(c->T * c->k), c->sums, Y};
+  const Mx4Operand x = mx4_operand(c->X, (int)c->T, (int)c->D);
+  if (launch_moe_route(m, c->w.mx4 ? &x : nullptr, s)) return FFN24_ERR_HIP;
+  return done(launch_moe_experts(m, c->w, &x, c->gate.c1, c->gate.c3, s));
 }
 
 }  // extern "C"

@@ -5,7 +5,7 @@
 //
 // Mixture of experts, four launches:
 //   router   logits X Wr in 64 bits, a part of D a workgroup (a product of two bf16 is exact in fp32; in 64 bits the choice between near experts is the definition's)
-//   pick     a token's k largest by their rank, ties to the lowest index; shares
+//   pick     a token's k largest by their rank, ties to the lowest index; shares; and the plan, which expert has which tokens (a single token's: in `up`)
 //   up       a workgroup a strip of 32 features of a chosen expert: h = a(G) U for the tokens that chose it; a row of H for each (token, choice)
 //   down     a workgroup a strip of 16 channels and all chosen experts one after the other: the shares' sum stays in LDS, in the order of the experts
 #include "mx4_core.hpp"
@@ -174,6 +174,70 @@ struct MoePlan {
 template <class T> __device__ __forceinline__ void put(T* p, T x) { __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 template <class T> __device__ __forceinline__ T get(const T* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
+// A value as an integer of the same order; NaN below all
+__device__ __forceinline__ unsigned long long order_of(double x) {
+  const unsigned long long b = __builtin_bit_cast(unsigned long long, x + 0.0);   // (-0 is 0)
+  return x != x ? 0ull : b >> 63 ? ~b : b | 1ull << 63;
+}
+
+// The choice of one token by the first 256 work items of a workgroup (all of them come here): its k experts by falling logit, and their shares.  p: the token's parts of the
+// logits, `stride` values from a part to the next.
+struct Choice {
+  double sums[256], logit[MOE_MAX_K];
+  unsigned long long order[MOE_E];
+  int which[MOE_MAX_K];
+  float share[MOE_MAX_K], part[4];
+};
+__device__ __forceinline__ void moe_choose(const double* __restrict__ p, size_t stride, int n_parts, int E, int k, bool renormalise, Choice& c) {
+  const int e = threadIdx.x, ways = 256 / E, way = e / E, ex = e - way * E;
+  if (e < 256) {
+    double s = 0.0;
+    if (way < ways)
+      for (int i = way; i < n_parts; i += 8 * ways) {          // eight on their way at once
+        double v[8];
+#pragma unroll
+        for (int j = 0; j < 8; j++) v[j] = i + j * ways < n_parts ? p[(size_t)(i + j * ways) * stride + ex] : 0.0;
+#pragma unroll
+        for (int j = 0; j < 8; j++) s += v[j];
+      }
+    c.sums[e] = s;
+  }
+  __syncthreads();
+  double s = 0.0;
+  if (e < E) {
+    for (int i = 0; i < ways; i++) s += c.sums[i * E + e];
+    c.order[e] = order_of(s);
+  }
+  __syncthreads();
+  int rank = MOE_E;
+  if (e < E) {
+    const unsigned long long mine = c.order[e];
+    rank = 0;
+#pragma unroll 4
+    for (int i = 0; i < E; i++) rank += c.order[i] > mine || (c.order[i] == mine && i < e);
+    if (rank < k) {
+      c.logit[rank] = s;
+      c.which[rank] = e;
+    }
+  }
+  __syncthreads();
+  // shares: exp(l - largest) over its sum, of the chosen or of all
+  const float x = e < E && (rank < k || !renormalise) ? expf((float)(s - c.logit[0])) : 0.f;
+  float sum = x;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d, 64);
+  if (e < 256 && (e & 63) == 0) c.part[e >> 6] = sum;
+  __syncthreads();
+  if (rank < k) c.share[rank] = x / (c.part[0] + c.part[1] + c.part[2] + c.part[3]);
+  __syncthreads();
+}
+// Work item j < k of a single token: its expert's place among the chosen ones
+__device__ __forceinline__ int place_of(const Choice& c, int j, int k) {
+  int at = 0;
+  for (int i = 0; i < k; i++) at += c.which[i] < c.which[j];
+  return at;
+}
+
 // ------------------------------------------------------------------------------------------------ up
 struct UpArgs {
   const char* w; size_t w_stride;      // weights of an expert (operand form, codes then scales) and bytes to the next expert's
@@ -183,14 +247,18 @@ struct UpArgs {
   const char* x; const char* x_scales; // bf16 [T][K], or the operand form
   char* h; char* h_scales; int h_steps;   // bf16 rows [..][F], or the mx4 operand form
   const MoePlan* plan; int k;          // MOE
+  MoePlan* plan_out; const double* logits; int n_parts, E, renormalise; int* picks; float* shares;   // MOE_ONE: parts of the logits, where the choice goes
 };
 
 // grid (strips, slots).  A slot is a chosen expert; without MOE there is one, and it has all tokens.  A strip is 8 RG features: a block of 64 rows, or (RG 2, bf16, whose result needs no
 // 32 features together) every other group of one.
-template <int SRC, int NT, bool MOE, int RG, int W>
-__global__ void __launch_bounds__(64 * W, NT == 1 ? 4 : 2) few_up_kernel(UpArgs e) {
+// MOE_ONE: a single token of the experts, whose choice every workgroup makes by itself; the first one stores it.  PASSES: over the weights, one for every 16 NT tokens of the expert
+// (otherwise it has no more than those).
+enum { ALL_TOKENS = 0, MOE = 1, MOE_ONE = 2 };
+template <int SRC, int NT, int WHO, int RG, int W, bool PASSES = false>
+__global__ void __launch_bounds__(64 * W, NT == 1 && WHO != MOE_ONE ? 4 : 2) few_up_kernel(UpArgs e) {
   constexpr bool MX4 = SRC != ROWS_BF16;
-  constexpr int U = 8 / RG, NP = NT <= 2 ? NT : 1, FEATS = 8 * RG;
+  constexpr int U = PASSES && MX4 ? 1 : 8 / RG, NP = 1, FEATS = 8 * RG;   // (more would not fit the registers)
   static_assert(RG == 4 || (RG == 2 && !MX4), "whole blocks of 32 features");
   __shared__ __attribute__((aligned(16))) float red[W * 16 * RG * RED];
   extern __shared__ __attribute__((aligned(16))) char staged_lds[];   // LDS_MX4: T K 17 / 32 bytes
@@ -199,7 +267,31 @@ __global__ void __launch_bounds__(64 * W, NT == 1 ? 4 : 2) few_up_kernel(UpArgs 
   const unsigned at = blockIdx.y * gridDim.x + blockIdx.x, id = RG == 4 ? at : run_of(at, gridDim.x * gridDim.y), slot = id / gridDim.x;
   const int strip = (int)(id - slot * gridDim.x), block = RG == 4 ? strip : strip >> 1, half = RG == 4 ? 0 : strip & 1;
   int expert = 0, n = e.T, first = 0;
-  if constexpr (MOE) {
+  if constexpr (WHO == MOE_ONE) {
+    __shared__ Choice one;
+    __shared__ int mine;
+    moe_choose(e.logits, (size_t)e.E, e.n_parts, e.E, e.k, e.renormalise != 0, one);
+    if (tid < e.k) {
+      const int to = place_of(one, tid, e.k);
+      if (to == (int)slot) mine = tid;
+      if (at == 0) {
+        e.picks[tid] = one.which[tid];
+        e.shares[tid] = one.share[tid];
+        e.plan_out->expert[to] = one.which[tid];
+        e.plan_out->start[to] = to;
+        e.plan_out->list[to] = tid;
+        e.plan_out->share[to] = one.share[tid];
+        if (tid == 0) {
+          e.plan_out->n_active = e.k;
+          e.plan_out->start[e.k] = e.k;
+        }
+      }
+    }
+    __syncthreads();
+    first = uniform(mine);                                     // (the pair: the row of H)
+    expert = uniform(one.which[first]);
+  }
+  if constexpr (WHO == MOE) {
     if ((int)slot >= e.plan->n_active) return;
     expert = e.plan->expert[slot];
     first = e.plan->start[slot];
@@ -212,21 +304,21 @@ __global__ void __launch_bounds__(64 * W, NT == 1 ? 4 : 2) few_up_kernel(UpArgs 
   StagedTokens staged;
   if constexpr (SRC == LDS_MX4) staged.load(e.x, pieces);
 
-  // (no expert has more tokens than there are: T <= 16 NT)
+  // the pair (row of H) of token `at` of the expert
+  auto pair = [&](int at) { return WHO == MOE ? e.plan->list[first + at] : WHO == MOE_ONE ? first : at; };
+  for (int t0 = 0; t0 < (PASSES ? n : 1); t0 += 16 * NT) {
   int row[NT], row_p[NP];
   bool on[NT], on_p[NP];
 #pragma unroll
   for (int i = 0; i < NT; i++) {
-    const int at = 16 * i + c;
+    const int at = t0 + 16 * i + c;
     on[i] = at < n;
-    const int p = on[i] ? (MOE ? e.plan->list[first + at] : at) : 0;
-    row[i] = MOE ? p / e.k : p;
-    if (i < NP) {
-      row_p[i < NP ? i : 0] = row[i];
-      on_p[i < NP ? i : 0] = on[i];
-    }
+    const int p = on[i] ? pair(at) : 0;
+    row[i] = WHO == ALL_TOKENS ? p : p / e.k;
   }
-  const int groups = (n + 15) >> 4;
+  row_p[0] = row[0];
+  on_p[0] = on[0];
+  const int groups = min((n - t0 + 15) >> 4, NT);
   f32x4 acc[RG][NT];
 #pragma unroll
   for (int g = 0; g < RG; g++)
@@ -262,7 +354,7 @@ __global__ void __launch_bounds__(64 * W, NT == 1 ? 4 : 2) few_up_kernel(UpArgs 
     __syncthreads();
     // neighbouring lanes have the features of a token
     for (int o = tid; o < FEATS * 16; o += 64 * W) {
-      const int f = o % FEATS, tok = o / FEATS, at = 16 * i + tok;
+      const int f = o % FEATS, tok = o / FEATS, at = t0 + 16 * i + tok;
       const int r = RG == 4 ? ((f >> 2) & 1) * 16 + 4 * (f >> 3) + (f & 3) : f;
       float gate = 0.f, up = 0.f;
 #pragma unroll
@@ -271,7 +363,7 @@ __global__ void __launch_bounds__(64 * W, NT == 1 ? 4 : 2) few_up_kernel(UpArgs 
         up += red[(k * 16 * RG + 8 * RG + r) * RED + tok];
       }
       const float h = gate_act(e.gate, gate) * up;
-      const int dest = at < n ? (MOE ? e.plan->list[first + at] : at) : 0;
+      const int dest = at < n ? pair(at) : 0;
       if constexpr (MX4) {
         uint32_t top = magnitude(h);
 #pragma unroll
@@ -288,6 +380,7 @@ __global__ void __launch_bounds__(64 * W, NT == 1 ? 4 : 2) few_up_kernel(UpArgs 
       }
     }
   }
+  }   // passes
 }
 
 // ------------------------------------------------------------------------------------------------ a product by itself
@@ -494,81 +587,19 @@ __global__ void __launch_bounds__(256) moe_router_kernel(const uint16_t* __restr
   }
 }
 
-// A value as an integer of the same order; NaN below all
-__device__ __forceinline__ unsigned long long order_of(double x) {
-  const unsigned long long b = __builtin_bit_cast(unsigned long long, x + 0.0);   // (-0 is 0)
-  return x != x ? 0ull : b >> 63 ? ~b : b | 1ull << 63;
-}
 // A workgroup a token; the one that comes last makes the plan.
 __global__ void __launch_bounds__(256) moe_pick_kernel(const double* __restrict__ parts, int n_parts, int T, int E, int k, int renormalise, int* __restrict__ picks,
                                                        float* __restrict__ shares, MoePlan* __restrict__ plan) {
-  __shared__ double sums[256], chosen[MOE_MAX_K];
-  __shared__ unsigned long long order[MOE_E];
-  __shared__ float part[4];
-  __shared__ int count[MOE_E], cursor[MOE_E], which[MOE_MAX_K], come;
-  const int t = blockIdx.x, tid = threadIdx.x, ways = 256 / E, way = tid / E, ex = tid - way * E;
-  {
-    double s = 0.0;
-    if (way < ways) {
-      const double* p = parts + (size_t)t * E + ex;
-      for (int i = way; i < n_parts; i += 8 * ways) {          // eight on their way at once
-        double v[8];
-#pragma unroll
-        for (int j = 0; j < 8; j++) v[j] = i + j * ways < n_parts ? p[(size_t)(i + j * ways) * T * E] : 0.0;
-#pragma unroll
-        for (int j = 0; j < 8; j++) s += v[j];
-      }
-    }
-    sums[tid] = s;
+  __shared__ Choice c;
+  __shared__ int count[MOE_E], cursor[MOE_E], come;
+  const int t = blockIdx.x, tid = threadIdx.x;
+  moe_choose(parts + (size_t)t * E, (size_t)T * E, n_parts, E, k, renormalise != 0, c);
+  if (tid < k) {
+    picks[t * k + tid] = c.which[tid];
+    shares[t * k + tid] = c.share[tid];
+    put(&plan->picks[t * k + tid], c.which[tid]);
+    put(&plan->shares[t * k + tid], c.share[tid]);
   }
-  __syncthreads();
-  const int e = tid;
-  double s = 0.0;
-  if (e < E) {
-    for (int i = 0; i < ways; i++) s += sums[i * E + e];
-    order[e] = order_of(s);
-  }
-  __syncthreads();
-  int rank = MOE_E;
-  if (e < E) {
-    const unsigned long long mine = order[e];
-    rank = 0;
-#pragma unroll 4
-    for (int i = 0; i < E; i++) rank += order[i] > mine || (order[i] == mine && i < e);
-    if (rank < k) {
-      chosen[rank] = s;
-      which[rank] = e;
-    }
-  }
-  __syncthreads();
-  // shares: exp(l - largest) over its sum, of the chosen or of all
-  const float x = e < E && (rank < k || !renormalise) ? expf((float)(s - chosen[0])) : 0.f;
-  float sum = x;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d, 64);
-  if ((e & 63) == 0) part[e >> 6] = sum;
-  __syncthreads();
-  if (rank < k) {
-    const float p = x / (part[0] + part[1] + part[2] + part[3]);
-    picks[t * k + rank] = e;
-    shares[t * k + rank] = p;
-    if (T == 1) {                                              // the plan by itself: the chosen experts in their order
-      int at = 0;
-      for (int i = 0; i < k; i++) at += which[i] < e;
-      plan->expert[at] = e;
-      plan->start[at] = at;
-      plan->list[at] = rank;
-      plan->share[at] = p;
-      if (rank == 0) {
-        plan->n_active = k;
-        plan->start[k] = k;
-      }
-    } else {
-      put(&plan->picks[t * k + rank], e);
-      put(&plan->shares[t * k + rank], p);
-    }
-  }
-  if (T == 1) return;
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
   if (tid == 0) come = __hip_atomic_fetch_add(&plan->ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -634,9 +665,9 @@ int staged_bytes(int T, int K) { return T * K / 2 + T * K / 32; }
 
 // Waves a workgroup and features a strip: eight waves, which ask for more at once, until there are enough workgroups to have four of four waves on a CU; half strips where there
 // are fewer than the CUs.
-template <int SRC, int NT, bool MOE, int RG, int W>
+template <int SRC, int NT, int WHO, int RG, int W, bool PASSES = false>
 int launch_up_one(const UpArgs& a, int slots, hipStream_t s) {
-  auto kern = few_up_kernel<SRC, NT, MOE, RG, W>;
+  auto kern = few_up_kernel<SRC, NT, WHO, RG, W, PASSES>;
   int lds = 0;
   if constexpr (SRC == LDS_MX4) {
     static std::atomic<bool> configured[MAX_DEVICES] = {};
@@ -646,19 +677,19 @@ int launch_up_one(const UpArgs& a, int slots, hipStream_t s) {
   hipLaunchKernelGGL(kern, dim3((unsigned)(a.F / (8 * RG)), (unsigned)slots), dim3(64 * W), lds, s, a);
   return (int)hipGetLastError();
 }
-template <int SRC, int NT, bool MOE>
+template <int SRC, int WHO, bool PASSES = false>
 int launch_up_tokens(const UpArgs& a, int slots, hipStream_t s) {
-  if constexpr (SRC != LDS_MX4 && NT == 1)
-    if (few_up_waves(a.F / 32 * slots) == 4) return launch_up_one<SRC, NT, MOE, 4, 4>(a, slots, s);
-  if constexpr (SRC == ROWS_BF16 && NT == 1)
-    if (few_up_halves(a.F / 32 * slots)) return launch_up_one<SRC, NT, MOE, 2, 8>(a, slots, s);
-  return launch_up_one<SRC, NT, MOE, 4, 8>(a, slots, s);
+  if constexpr (SRC != LDS_MX4 && WHO != MOE_ONE)
+    if (few_up_waves(a.F / 32 * slots) == 4) return launch_up_one<SRC, 1, WHO, 4, 4, PASSES>(a, slots, s);
+  if constexpr (SRC == ROWS_BF16 && !PASSES)
+    if (few_up_halves(a.F / 32 * slots)) return launch_up_one<SRC, 1, WHO, 2, 8>(a, slots, s);
+  return launch_up_one<SRC, 1, WHO, 4, 8, PASSES>(a, slots, s);
 }
 template <int SRC>
 int launch_moe_up(const UpArgs& a, int slots, hipStream_t s) {
-  if (a.T <= 16) return launch_up_tokens<SRC, 1, true>(a, slots, s);
-  if (a.T <= 32) return launch_up_tokens<SRC, 2, true>(a, slots, s);
-  return launch_up_tokens<SRC, 4, true>(a, slots, s);
+  if (a.T == 1) return launch_up_tokens<SRC, MOE_ONE>(a, slots, s);
+  if (a.T <= 16) return launch_up_tokens<SRC, MOE>(a, slots, s);
+  return moe_crowded(a.T, a.k, a.E) ? launch_up_one<SRC, 4, MOE, 4, 8>(a, slots, s) : launch_up_tokens<SRC, MOE, true>(a, slots, s);
 }
 template <bool MX4, int NT>
 int launch_down(const DownArgs& a, int splits, hipStream_t s) {
@@ -684,48 +715,52 @@ int launch_rows_tokens(const RowsArgs& a, hipStream_t s) {
 template <int RG>
 int launch_rows(const RowsArgs& a, bool staged, hipStream_t s) {
   if (staged) return launch_rows_tokens<RG, LDS_MX4, 1>(a, s);
-  return a.T <= 16 ? launch_rows_tokens<RG, OPERAND_MX4, 1>(a, s) : launch_rows_tokens<RG, OPERAND_MX4, 2>(a, s);
+  if constexpr (RG == 1)
+    if (a.T > 16) return launch_rows_tokens<RG, OPERAND_MX4, 2>(a, s);
+  return launch_rows_tokens<RG, OPERAND_MX4, 1>(a, s);
 }
 }  // namespace
 
 size_t moe_plan_size() { return sizeof(MoePlan); }
 size_t moe_parts_size(int T, int D, int E) { return (size_t)((D + ROUTE_D - 1) / ROUTE_D) * T * E * sizeof(double); }
 
-int launch_moe_route(const void* X, const void* Wr, int T, int D, int E, int k, bool renormalise, void* parts, int* picks, float* shares, void* plan,
-                     const Mx4Operand* x, hipStream_t s) {
-  const int n = (D + ROUTE_D - 1) / ROUTE_D;
-  hipLaunchKernelGGL(moe_router_kernel, dim3((unsigned)n, (unsigned)((T + 15) / 16)), dim3(256), 0, s, static_cast<const uint16_t*>(X), static_cast<const char*>(Wr), T, D, E, static_cast<double*>(parts), x ? x->steps : 0, x ? const_cast<char*>(x->codes) : nullptr,
-                     x ? const_cast<char*>(x->scales) : nullptr);
-  hipLaunchKernelGGL(moe_pick_kernel, dim3((unsigned)T), dim3(256), 0, s, static_cast<const double*>(parts), n, T, E, k, (int)renormalise, picks, shares,
-                     static_cast<MoePlan*>(plan));
+int launch_moe_route(const MoeCall& m, const Mx4Operand* x, hipStream_t s) {
+  const int n = (m.D + ROUTE_D - 1) / ROUTE_D;
+  hipLaunchKernelGGL(moe_router_kernel, dim3((unsigned)n, (unsigned)((m.T + 15) / 16)), dim3(256), 0, s, static_cast<const uint16_t*>(m.X), static_cast<const char*>(m.Wr), m.T, m.D,
+                     m.E, static_cast<double*>(m.logits), x ? x->steps : 0, x ? const_cast<char*>(x->codes) : nullptr, x ? const_cast<char*>(x->scales) : nullptr);
+  if (m.T > 1)
+    hipLaunchKernelGGL(moe_pick_kernel, dim3((unsigned)m.T), dim3(256), 0, s, static_cast<const double*>(m.logits), n, m.T, m.E, m.k, (int)m.renormalise, m.picks, m.shares,
+                       static_cast<MoePlan*>(m.plan));
   return (int)hipGetLastError();
 }
 
-int launch_moe_experts(const MoeWeights& w, const void* X, const Mx4Operand* x, int T, int D, int F, int E, int k, float c1, float c3, const void* plan, void* H,
-                       int h_rows, void* parts, void* Y, hipStream_t s) {
+int launch_moe_experts(const MoeCall& m, const MoeWeights& w, const Mx4Operand* x, float c1, float c3, hipStream_t s) {
+  const int T = m.T, D = m.D, F = m.F, E = m.E, k = m.k;
   UpArgs up{};
   up.w = static_cast<const char*>(w.up); up.w_stride = w.up_stride; up.scales_at = w.up_scales;
   up.K = D; up.F = F; up.T = T; up.steps = w.mx4 ? mx4_steps(D) : D / 32; up.gate = Gate{c1, c3};
-  up.x = w.mx4 ? x->codes : static_cast<const char*>(X); up.x_scales = w.mx4 ? x->scales : nullptr;
-  const Mx4Operand h = mx4_operand(H, h_rows, F);
-  up.h = const_cast<char*>(w.mx4 ? h.codes : static_cast<const char*>(H));
+  up.x = w.mx4 ? x->codes : static_cast<const char*>(m.X); up.x_scales = w.mx4 ? x->scales : nullptr;
+  const Mx4Operand h = mx4_operand(m.H, m.h_rows, F);
+  up.h = const_cast<char*>(w.mx4 ? h.codes : static_cast<const char*>(m.H));
   up.h_scales = const_cast<char*>(h.scales);
   up.h_steps = h.steps;
-  up.plan = static_cast<const MoePlan*>(plan); up.k = k;
+  up.plan = up.plan_out = static_cast<MoePlan*>(m.plan); up.k = k;
+  up.logits = static_cast<const double*>(m.logits); up.n_parts = (D + ROUTE_D - 1) / ROUTE_D; up.E = E; up.renormalise = m.renormalise;
+  up.picks = m.picks; up.shares = m.shares;
   const int slots = T * k < E ? T * k : E;
   if (const int rc = w.mx4 ? launch_moe_up<OPERAND_MX4>(up, slots, s) : launch_moe_up<ROWS_BF16>(up, slots, s)) return rc;
   DownArgs d{};
   d.w = static_cast<const char*>(w.down); d.w_stride = w.down_stride; d.scales_at = w.down_scales;
   d.steps = w.mx4 ? mx4_steps(F) : F / 32; d.F = F; d.D = D; d.T = T; d.k = k;
   d.h = up.h; d.h_scales = h.scales; d.h_steps = h.steps;
-  d.plan = up.plan; d.out = static_cast<uint16_t*>(Y);
-  d.parts = static_cast<float*>(parts);
-  const int splits = moe_down_splits(D / 16, (T * k < E ? T * k : E) * ((d.steps + 7) / 8));
+  d.plan = up.plan; d.out = static_cast<uint16_t*>(m.Y);
+  d.parts = static_cast<float*>(m.parts);
+  const int splits = moe_down_splits(D / 16, slots * ((d.steps + 7) / 8));
   const int rc = T <= 16 ? (w.mx4 ? launch_down<true, 1>(d, splits, s) : launch_down<false, 1>(d, splits, s))
                          : (w.mx4 ? launch_down<true, 4>(d, splits, s) : launch_down<false, 4>(d, splits, s));
   if (rc || splits == 1) return rc;
-  hipLaunchKernelGGL((edge_sum_kernel<false>), dim3((unsigned)((D / 4 * T + 255) / 256)), dim3(256), 0, s, static_cast<const uint32_t*>(parts), splits, D, T, I8Scales{},
-                     static_cast<uint16_t*>(Y));
+  hipLaunchKernelGGL((edge_sum_kernel<false>), dim3((unsigned)((D / 4 * T + 255) / 256)), dim3(256), 0, s, static_cast<const uint32_t*>(m.parts), splits, D, T, I8Scales{},
+                     static_cast<uint16_t*>(m.Y));
   return (int)hipGetLastError();
 }
 
@@ -736,15 +771,17 @@ int launch_few_mx4_up(const Mx4Operand& w, const void* X, const Mx4Operand* x, i
   up.K = D; up.F = F; up.T = T; up.steps = w.steps; up.gate = Gate{c1, c3};
   up.x = x ? x->codes : static_cast<const char*>(X); up.x_scales = x ? x->scales : nullptr;
   up.h = const_cast<char*>(h.codes); up.h_scales = const_cast<char*>(h.scales); up.h_steps = h.steps;
-  if (!x) return launch_up_tokens<LDS_MX4, 1, false>(up, 1, s);
-  return T <= 16 ? launch_up_tokens<OPERAND_MX4, 1, false>(up, 1, s) : launch_up_tokens<OPERAND_MX4, 2, false>(up, 1, s);
+  if (!x) return launch_up_tokens<LDS_MX4, ALL_TOKENS>(up, 1, s);
+  return launch_up_tokens<OPERAND_MX4, ALL_TOKENS>(up, 1, s);
 }
-// Strips of 64, 32 or 16 channels: at least 512 workgroups if there are that many
 int launch_few_mx4_rows(const Mx4Operand& w, int K, int N, const void* X, const Mx4Operand* x, int T, void* Y, hipStream_t s) {
   RowsArgs a{w.codes, w.scales, w.steps, K, N, T, static_cast<const char*>(X), nullptr, 0, static_cast<uint16_t*>(Y)};
   if (x) { a.x = x->codes; a.x_scales = x->scales; a.x_steps = x->steps; }
-  if (N >= 512 * 64) return launch_rows<4>(a, !x, s);
-  return N >= 512 * 32 ? launch_rows<2>(a, !x, s) : launch_rows<1>(a, !x, s);
+  switch (T > 16 ? 1 : mx4_few_groups(N, w.steps)) {
+    case 4: return launch_rows<4>(a, !x, s);
+    case 2: return launch_rows<2>(a, !x, s);
+    default: return launch_rows<1>(a, !x, s);
+  }
 }
 
 }  // namespace ffn24

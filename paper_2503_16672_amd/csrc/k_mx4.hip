@@ -91,28 +91,32 @@ __global__ void __launch_bounds__(256) dequantise_mx4_kernel(const uint32_t* __r
   }
 }
 
-// Tokens to the operand form: a wave takes 16 rows and four steps.  Lane 4 c + p has 8 values of row c; four lanes a block, 16 rows' codes of a block are 256 bytes.
+// Tokens to the operand form: a wave takes 16 rows and four steps, 4 rows and a step (256 bytes of each, whole lines) a load.  Four lanes have a block of 32.
 __global__ void __launch_bounds__(256) mx4_tokens_kernel(const uint16_t* __restrict__ X, int T, int K, int steps, char* __restrict__ codes, char* __restrict__ scales) {
   const int quads = (steps + 3) >> 2;
-  const int id = blockIdx.x * 4 + (threadIdx.x >> 6), group = id / quads, S = id - group * quads, lane = threadIdx.x & 63, c = lane >> 2, p = lane & 3;
+  const int id = blockIdx.x * 4 + (threadIdx.x >> 6), group = id / quads, S = id - group * quads, lane = threadIdx.x & 63, c = lane >> 4, q = (lane >> 2) & 3, p = lane & 3;
   if (16 * group >= T) return;
-  const int r = 16 * group + c;
-  const uint16_t* x = X + (size_t)min(r, T - 1) * K;
-  u32x4 w[16];
+  u32x4 w[4][4];                                               // [step][4 rows]
 #pragma unroll
-  for (int i = 0; i < 16; i++) {
-    const int k = 32 * (16 * S + i) + 8 * p;
-    w[i] = k < K ? *reinterpret_cast<const u32x4*>(x + k) : u32x4{0u, 0u, 0u, 0u};
-  }
-  uint32_t mine = 0u;                                          // lane p: the scales of quarter p of the four steps
-  char* out = codes + mx4_code_at(16 * group, 16 * S, steps) + c * 16 + 4 * p;
+  for (int j = 0; j < 4; j++)
 #pragma unroll
-  for (int i = 0; i < 16; i++) {
-    const uint32_t code = mx4_scale_code(quad_max(mx4_top8(w[i])));
-    if ((i & 3) == p) mine |= code << (8 * (i >> 2));
-    if (4 * S + (i >> 2) < steps) *reinterpret_cast<uint32_t*>(out + (size_t)(i >> 2) * MX4_PANEL + (i & 3) * 256) = mx4_codes8(w[i], mx4_scale(code));
+    for (int i = 0; i < 4; i++) {
+      const int k = 128 * (4 * S + j) + 8 * (lane & 15), r = 16 * group + 4 * i + c;
+      w[j][i] = k < K && r < T ? ld_stream(reinterpret_cast<const u32x4*>(X + (size_t)r * K + k)) : u32x4{0u, 0u, 0u, 0u};
+    }
+  char* out = codes + mx4_code_at(16 * group, 16 * S, steps) + q * 256 + 4 * p;
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    const int r = 4 * i + c;
+    uint32_t mine = 0u;                                        // the scales of the quarter's four steps
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+      const uint32_t code = mx4_scale_code(quad_max(mx4_top8(w[j][i])));
+      mine |= code << (8 * j);
+      if (4 * S + j < steps) *reinterpret_cast<uint32_t*>(out + (size_t)j * MX4_PANEL + r * 16) = mx4_codes8(w[j][i], mx4_scale(code));
+    }
+    if (p == 0) *reinterpret_cast<uint32_t*>(scales + mx4_scale_at(16 * group + r, 16 * S + q, steps)) = mine;
   }
-  *reinterpret_cast<uint32_t*>(scales + mx4_scale_at(r, 16 * S + p, steps)) = mine;
 }
 
 // Weights to the operand form, a workgroup 64 rows and a step: lane = channel of the block, wave = quarter of the step.  FORM 0: bf16 W [K][N] to mx4; 1: codes [N][K / 2] and

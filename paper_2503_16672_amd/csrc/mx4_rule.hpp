@@ -37,16 +37,30 @@ inline Mx4Plan mx4_plan(int M, int N, int steps, bool split) {
 
 constexpr long long MX4_SPLIT_MOST = 1LL << 25;   // results of a product that could be split: two rounds of the largest tile
 
-// Few tokens: the kernels of k_experts.hip or the GEMM.  A product's tokens come to mx4 in its own kernel where a workgroup can hold them, or by a launch before it.
-constexpr int FEW_MX4_TOKENS = 32, MX4_FUSED_VALUES = 1 << 16;
-inline bool mx4_few_fused(int T, int K) { return T <= 16 && (long long)T * K <= MX4_FUSED_VALUES; }
-inline bool mx4_few(int T, int, int) { return T <= FEW_MX4_TOKENS; }
-inline bool mx4_few_gated(int T, int, int) { return T <= FEW_MX4_TOKENS; }
+// Few tokens: the kernels of k_experts.hip or the GEMM.  us, few tokens' kernel / GEMM.  Products (T K N): 16 4096 32768 11.2, 12.9; 16 16384 4096 8.7, 12.3; 16 8192 57344 38.3, 35.9; 24 16384 4096 9.6,
+// 12.3; 24 5440 2048 4.2, 7.6; 24 1408 512 3.4, 4.7; the other way round 24 4096 32768 14.3, 13.0; 24 2048 10880 8.6, 5.1; 24 28672 8192 26.9, 23.2: from 17 tokens on where the GEMM would have to
+// split the reduction.  Gate and up (T D F): 16 4096 16384 12.4, 13.2; 16 2048 5440 4.9, 5.4; 16 8192 28672 38.9, 36.0; 24 4096 16384 16.2, 13.4; 24 2048 5440 5.8, 5.5.
+constexpr int FEW_MX4_TOKENS = 16, FEW_MX4_MORE = 32;
+inline bool mx4_few(int T, int K, int N) { return T <= FEW_MX4_TOKENS || (T <= FEW_MX4_MORE && K >= N && N <= 4096); }
+inline bool mx4_few_gated(int T) { return T <= FEW_MX4_TOKENS; }
+// Their tokens come to mx4 in the kernel itself, by every workgroup, or (3.7 us) by a launch before it.  us, both: 8 tokens at 4096 x 16384 gate and up 13.2, 15.8; 16 17.2, 16.3; 4 at 8192 x 28672
+// 38.4, 42.3; 8 42.1, 42.3; 2 of K 16384 to 4096 channels 10.5, 11.9; 4 12.7, 11.8.
+constexpr int MX4_FUSED_VALUES = 1 << 16;
+inline bool mx4_few_fused(int T, int K) { return T <= FEW_MX4_TOKENS && (long long)T * K <= MX4_FUSED_VALUES; }
+// Groups of 16 channels a strip: a wave takes 8 KiB at a time, so that a short reduction needs wide strips for eight waves to have work, a long one many strips.
+inline int mx4_few_groups(int N, int steps) {
+  if (N >= 512 * 64) return 4;
+  if (steps >= 64) return N >= 512 * 32 ? 2 : 1;
+  if (N < 8192) return 1;
+  return steps >= 32 ? 2 : 4;
+}
 
 // Experts: waves a workgroup of the up projection of `strips` strips, half strips, and over how many workgroups a strip's experts of the down projection are dealt out
 // (`units`: of eight steps, at most, that a strip has)
-inline int few_up_waves(int strips) { return strips >= 1024 ? 4 : 8; }
+inline int few_up_waves(int strips) { return strips >= 512 ? 4 : 8; }
 inline bool few_up_halves(int strips) { return strips < 256; }
+// whether experts have so many tokens that 64 of them beside a strip's weights are worth their registers (a workgroup a CU less)
+inline bool moe_crowded(int T, int k, int E) { return T * k > 12 * E; }
 constexpr int MOE_SPLITS = 8;
 inline int moe_down_splits(int strips, int units) {
   const int fill = 256 / strips, most = units / 16;              // (two units a wave at least)
