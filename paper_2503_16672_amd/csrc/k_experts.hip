@@ -6,7 +6,7 @@
 // Mixture of experts, four launches:
 //   router   logits X Wr in 64 bits, a part of D a workgroup (a product of two bf16 is exact in fp32; in 64 bits the choice between near experts is the definition's)
 //   pick     a token's k largest by their rank, ties to the lowest index; shares; and the plan, which expert has which tokens (a single token's: in `up`)
-//   up       a workgroup a strip of 32 features of a chosen expert: h = a(G) U for the tokens that chose it; a row of H for each (token, choice)
+//   up       a workgroup a strip of 32 features of a chosen expert: h = a(G) U for the tokens that chose it; a row of H for each (token, choice), in the experts' order
 //   down     a workgroup a strip of 16 channels and all chosen experts one after the other: the shares' sum stays in LDS, in the order of the experts
 #include "mx4_core.hpp"
 #include "mx4_rule.hpp"
@@ -133,24 +133,36 @@ struct Unit {
       else acc[g][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w[j][g]), __builtin_bit_cast(bf16x8, v), acc[g][i], 0, 0, 0);
     }
   }
-  // the ops of the unit for `groups` groups of tokens; those from NP on are asked for here
+  // the ops of the unit for `groups` groups of tokens; those from NP on are asked for here, a group's steps together
   template <int NT>
   __device__ __forceinline__ void ops(const Tokens& t, const int (&row)[NT], const bool (&on)[NT], int groups, int s0, int steps, int q, f32x4 (&acc)[RG][NT]) const {
 #pragma unroll
-    for (int j = 0; j < U; j++) {
-      if (s0 + j >= steps) break;
-      const int byte = 8 * ((s0 + j) & 3);
+    for (int i = 0; i < NT; i++) {
+      if (i > 0 && i >= groups) break;
+      u32x4 v[U];
+      uint32_t sv[SU];
 #pragma unroll
-      for (int i = 0; i < NT; i++) {
-        if (i > 0 && i >= groups) break;
+      for (int j = 0; j < U; j++) {
+        if constexpr (SRC == LDS_MX4) {
+          v[j] = u32x4{0u, 0u, 0u, 0u};
+        } else {
+          v[j] = i < NP ? x[j][i < NP ? i : 0] : token(t, row[i], on[i], min(s0 + j, steps - 1), q);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < SU; j++) {
+        sv[j] = 0u;
+        if constexpr (SRC == OPERAND_MX4) sv[j] = i < NP ? sx[j][i < NP ? i : 0] : token_scales(t, row[i], on[i], min(s0 + 4 * j, steps - 1), q);
+      }
+#pragma unroll
+      for (int j = 0; j < U; j++) {
+        if (s0 + j >= steps) break;
         if constexpr (SRC == LDS_MX4) {
           const int kb = 4 * (s0 + j) + q, at = kb * t.T + row[i];
           const bool there = on[i] && 32 * kb < t.K;
           op(j, i, s0, there ? *reinterpret_cast<const u32x4*>(t.p + at * 16) : u32x4{0u, 0u, 0u, 0u}, there ? (uint32_t)(uint8_t)t.scales[at] : 0u, acc);
-        } else if (i < NP) {
-          op(j, i, s0, x[j][i < NP ? i : 0], SRC == OPERAND_MX4 ? sx[SRC == OPERAND_MX4 ? j / 4 : 0][i < NP ? i : 0] >> byte : 0u, acc);
         } else {
-          op(j, i, s0, token(t, row[i], on[i], s0 + j, q), SRC == OPERAND_MX4 ? token_scales(t, row[i], on[i], s0 + j, q) >> byte : 0u, acc);
+          op(j, i, s0, v[j], sv[MX4 ? j / 4 : 0] >> (8 * ((s0 + j) & 3)), acc);
         }
       }
     }
@@ -288,8 +300,8 @@ __global__ void __launch_bounds__(64 * W, NT == 1 && WHO != MOE_ONE ? 4 : 2) few
       }
     }
     __syncthreads();
-    first = uniform(mine);                                     // (the pair: the row of H)
-    expert = uniform(one.which[first]);
+    first = (int)slot;
+    expert = uniform(one.which[uniform(mine)]);
   }
   if constexpr (WHO == MOE) {
     if ((int)slot >= e.plan->n_active) return;
@@ -304,8 +316,6 @@ __global__ void __launch_bounds__(64 * W, NT == 1 && WHO != MOE_ONE ? 4 : 2) few
   StagedTokens staged;
   if constexpr (SRC == LDS_MX4) staged.load(e.x, pieces);
 
-  // the pair (row of H) of token `at` of the expert
-  auto pair = [&](int at) { return WHO == MOE ? e.plan->list[first + at] : WHO == MOE_ONE ? first : at; };
   for (int t0 = 0; t0 < (PASSES ? n : 1); t0 += 16 * NT) {
   int row[NT], row_p[NP];
   bool on[NT], on_p[NP];
@@ -313,8 +323,7 @@ __global__ void __launch_bounds__(64 * W, NT == 1 && WHO != MOE_ONE ? 4 : 2) few
   for (int i = 0; i < NT; i++) {
     const int at = t0 + 16 * i + c;
     on[i] = at < n;
-    const int p = on[i] ? pair(at) : 0;
-    row[i] = WHO == ALL_TOKENS ? p : p / e.k;
+    row[i] = !on[i] || WHO == MOE_ONE ? 0 : WHO == MOE ? e.plan->list[first + at] / e.k : at;
   }
   row_p[0] = row[0];
   on_p[0] = on[0];
@@ -363,7 +372,7 @@ __global__ void __launch_bounds__(64 * W, NT == 1 && WHO != MOE_ONE ? 4 : 2) few
         up += red[(k * 16 * RG + 8 * RG + r) * RED + tok];
       }
       const float h = gate_act(e.gate, gate) * up;
-      const int dest = at < n ? pair(at) : 0;
+      const int dest = first + at;                                 // (H's rows are in the plan's order: an expert's one after the other)
       if constexpr (MX4) {
         uint32_t top = magnitude(h);
 #pragma unroll
@@ -451,7 +460,7 @@ __global__ void __launch_bounds__(THREADS, NT == 1 && (RG > 1 || SRC == LDS_MX4)
 struct DownArgs {
   const char* w; size_t w_stride, scales_at;
   int steps, F, D, T, k;
-  const char* h; const char* h_scales; int h_steps;   // rows by pair
+  const char* h; const char* h_scales; int h_steps;   // rows in the order of the plan
   const MoePlan* plan;
   float* parts;                        // [splits][T][D]
   uint16_t* out;
@@ -487,9 +496,8 @@ __global__ void __launch_bounds__(THREADS, 2) moe_down_kernel(DownArgs e) {
     return Strip{codes + (size_t)block * e.steps * MX4_PANEL + g0 * 1024, codes + e.scales_at + (size_t)block * ((e.steps + 3) >> 2) * 1024 + g0 * 256, e.steps};
   };
   auto first_rows = [&](int i, int (&row)[1], bool (&on)[1]) {
-    const int at = start[i / units] + c;
-    on[0] = at < start[i / units + 1];
-    row[0] = on[0] ? list[at] : 0;
+    row[0] = start[i / units] + c;
+    on[0] = row[0] < start[i / units + 1];
   };
   Unit<SRC, 1, U, 1> now, next;
   int i = split * WAVES + wave, row_n[1], row_f[1];
@@ -511,9 +519,8 @@ __global__ void __launch_bounds__(THREADS, 2) moe_down_kernel(DownArgs e) {
     on[0] = on_f[0];
 #pragma unroll
     for (int g = 1; g < NT; g++) {
-      const int at = 16 * g + c;
-      on[g] = at < n;
-      row[g] = on[g] ? list[first + at] : 0;
+      row[g] = first + 16 * g + c;
+      on[g] = 16 * g + c < n;
     }
     f32x4 acc[1][NT];
 #pragma unroll
@@ -523,8 +530,8 @@ __global__ void __launch_bounds__(THREADS, 2) moe_down_kernel(DownArgs e) {
 #pragma unroll
     for (int g = 0; g < NT; g++)
       if (on[g]) {                                         // (a token chooses an expert once: no two lanes of a quarter have the same one)
-        const float p = share[first + 16 * g + c];
-        f32x4* to = reinterpret_cast<f32x4*>(mine + row[g] / e.k * SUM + 4 * q);
+        const float p = share[row[g]];
+        f32x4* to = reinterpret_cast<f32x4*>(mine + list[row[g]] / e.k * SUM + 4 * q);
         f32x4 y = *to;
 #pragma unroll
         for (int v = 0; v < 4; v++) y[v] += p * acc[0][g][v];

@@ -63,10 +63,10 @@ inline bool few_up_halves(int strips) { return strips < 256; }
 inline bool moe_crowded(int T, int k, int E) { return T * k > 12 * E; }
 constexpr int MOE_SPLITS = 8;
 inline int moe_down_splits(int strips, int units) {
-  const int fill = 256 / strips, most = units / 16;              // (two units a wave at least)
+  const int fill = 256 / strips, most = units / 8;               // (a unit a wave at least)
   int s = fill < most ? fill : most;
   s = s < MOE_SPLITS ? s : MOE_SPLITS;
-  return s > 2 ? s : 1;
+  return s > 2 && units >= 24 ? s : 1;
 }
 
 }  // namespace ffn24
