@@ -179,12 +179,12 @@ int launch_mx4_tile(Mx4Gemm g, const typename Epi::Args& ea, int splits, int par
   return (int)hipGetLastError();
 }
 template <class Epi>
-int launch_mx4(const Mx4Gemm& g, const typename Epi::Args& ea, const Mx4Plan& p, hipStream_t s) {
-  switch (p.tile) {
-    case 0: return launch_mx4_tile<Epi, 8, 8>(g, ea, p.splits, p.part, s);
-    case 1: return launch_mx4_tile<Epi, 8, 4>(g, ea, p.splits, p.part, s);
-    case 2: return launch_mx4_tile<Epi, 4, 4>(g, ea, p.splits, p.part, s);
-    default: return launch_mx4_tile<Epi, 4, 2>(g, ea, p.splits, p.part, s);
+int launch_mx4(const Mx4Gemm& g, const typename Epi::Args& ea, int tile, hipStream_t s) {
+  switch (tile) {
+    case 0: return launch_mx4_tile<Epi, 8, 8>(g, ea, 1, 0, s);
+    case 1: return launch_mx4_tile<Epi, 8, 4>(g, ea, 1, 0, s);
+    case 2: return launch_mx4_tile<Epi, 4, 4>(g, ea, 1, 0, s);
+    default: return launch_mx4_tile<Epi, 4, 2>(g, ea, 1, 0, s);
   }
 }
 }  // namespace
@@ -245,20 +245,20 @@ size_t mx4_split_scratch(int M, int N, int K) {
 }
 int launch_mx4_product(const Mx4Operand& w, int M, const Mx4Operand& x, int T, void* Y, const Scratch& scratch, hipStream_t s) {
   const Mx4Gemm g{w, x, M, T, 0, 0};
-  Mx4Plan p = mx4_plan(M, T, w.steps, true);
+  const Mx4Plan p = mx4_plan(M, T, w.steps, true);
   if (p.splits == 1 || mx4_split_scratch(M, T, w.steps * MX4_STEP) > scratch.bytes)
-    return launch_mx4<Mx4Rows>(g, Mx4Rows::Args{static_cast<uint16_t*>(Y), M, T}, p.splits == 1 ? p : mx4_plan(M, T, w.steps, false), s);
+    return launch_mx4<Mx4Rows>(g, Mx4Rows::Args{static_cast<uint16_t*>(Y), M, T}, p.tile, s);
   uint32_t* parts = static_cast<uint32_t*>(scratch.p);
-  if (int rc = launch_mx4<Mx4Part>(g, Mx4Part::Args{parts, M, T}, p, s)) return rc;
+  if (int rc = launch_mx4_tile<Mx4Part, 4, 2>(g, Mx4Part::Args{parts, M, T}, p.splits, p.part, s)) return rc;
   hipLaunchKernelGGL((edge_sum_kernel<false>), dim3((unsigned)(((size_t)M / 4 * T + 255) / 256)), dim3(256), 0, s, parts, p.splits, M, T, I8Scales{}, static_cast<uint16_t*>(Y));
   return (int)hipGetLastError();
 }
 int launch_mx4_gated_up(const Mx4Operand& w, int F, const Mx4Operand& x, int T, float c1, float c3, const Mx4Operand& h, hipStream_t s) {
   const Mx4Gemm g{w, x, 2 * F, T, 0, 0};
-  const Mx4Plan p = mx4_plan(2 * F, T, w.steps, false);
+  const int tile = mx4_plan(2 * F, T, w.steps, false).tile;
   const auto go = [&](auto epi) {
     using Epi = decltype(epi);
-    return launch_mx4<Epi>(g, typename Epi::Args{const_cast<char*>(h.codes), reinterpret_cast<uint8_t*>(const_cast<char*>(h.scales)), F, T, h.steps, Gate{c1, c3}}, p, s);
+    return launch_mx4<Epi>(g, typename Epi::Args{const_cast<char*>(h.codes), reinterpret_cast<uint8_t*>(const_cast<char*>(h.scales)), F, T, h.steps, Gate{c1, c3}}, tile, s);
   };
   return c3 == 0.f && c1 == 1.f ? go(Mx4Gated<false>{}) : go(Mx4Gated<true>{});
 }

@@ -17,7 +17,8 @@ inline long long mx4_time(const Mx4Tile& t, long long tiles, int steps) {
 }
 
 struct Mx4Plan { int tile, splits, part; };
-// M channels, N tokens, `steps` of k; split: whether the reduction may be split (its sums then cost a launch and their way through memory)
+// M channels, N tokens, `steps` of k.  split: whether the reduction may be split over several workgroups a tile, on the smallest tile (its sums then cost a launch and their way
+// through memory; us, 128 x 64 / 128 x 128 tiles at their best split: 4096 64 16384 12.2, 13.4; 4096 128 16384 14.0, 15.4; 1024 64 16384 10.1, 11.3; unsplit 21.5, 21.6, 18.1)
 inline Mx4Plan mx4_plan(int M, int N, int steps, bool split) {
   N = (N + 63) / 64 * 64;      // (the scratch of a context is made for whole 64s)
   Mx4Plan best{0, 1, steps};
@@ -25,7 +26,7 @@ inline Mx4Plan mx4_plan(int M, int N, int steps, bool split) {
   for (int i = 0; i < MX4_NUM_TILES; i++) {
     const Mx4Tile& t = MX4_TILES[i];
     const long long tiles = mx4_tiles(t, M, N);
-    for (int s = 1; s <= (split ? MX4_SPLITS : 1); s++) {
+    for (int s = 1; s <= (split && i == MX4_NUM_TILES - 1 ? MX4_SPLITS : 1); s++) {
       const int part = ((steps + s - 1) / s + 3) / 4 * 4;
       if (s > 1 && (part < 8 || (s - 1) * part >= steps || tiles * s > 2 * MX4_CUS)) continue;
       const long long time = mx4_time(t, tiles * s, s > 1 ? part : steps) + (s > 1 ? 3500 + 8LL * s * M * N / 5000 : 0);
@@ -35,7 +36,7 @@ inline Mx4Plan mx4_plan(int M, int N, int steps, bool split) {
   return best;
 }
 
-constexpr long long MX4_SPLIT_MOST = 1LL << 25;   // results of a product that could be split: two rounds of the largest tile
+constexpr long long MX4_SPLIT_MOST = 1LL << 21;   // results of a product that could be split: 256 tiles of 128 x 64
 
 // Few tokens: the kernels of k_experts.hip or the GEMM.  us, few tokens' kernel / GEMM.  Products (T K N): 16 4096 32768 11.2, 12.9; 16 16384 4096 8.7, 12.3; 16 8192 57344 38.3, 35.9; 24 16384 4096 9.6,
 // 12.3; 24 5440 2048 4.2, 7.6; 24 1408 512 3.4, 4.7; the other way round 24 4096 32768 14.3, 13.0; 24 2048 10880 8.6, 5.1; 24 28672 8192 26.9, 23.2: from 17 tokens on where the GEMM would have to
