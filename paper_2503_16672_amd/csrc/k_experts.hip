@@ -62,12 +62,13 @@ struct StagedTokens {
   // (a row is a whole number of blocks, so the four lanes of a block are all there or none)
   __device__ __forceinline__ void store(char* codes, char* scales, int pieces, int K, int T) const {
     const int per = K / 8, p = threadIdx.x & 3;
+    const uint32_t inverse = 0xFFFFFFFFu / (uint32_t)per + 1u;   // (i / per = the upper half of i * inverse for i, per up to 2^13)
 #pragma unroll
     for (int j = 0; j < LDS_PIECES; j++) {
       const int i = j * THREADS + (int)threadIdx.x;
       if (j * THREADS >= pieces) break;
       const uint32_t code = mx4_scale_code(quad_max(mx4_top8(w[j])));
-      const int t = i / per, at = ((i - t * per) >> 2) * T + t;
+      const int t = (int)__umulhi((uint32_t)i, inverse), at = ((i - t * per) >> 2) * T + t;
       if (i < pieces) {
         *reinterpret_cast<uint32_t*>(codes + at * 16 + 4 * p) = mx4_codes8(w[j], mx4_scale(code));
         if (p == 0) scales[at] = (char)code;
