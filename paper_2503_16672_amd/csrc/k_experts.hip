@@ -166,6 +166,11 @@ struct Unit {
           op(j, i, s0, v[j], sv[MX4 ? j / 4 : 0] >> (8 * ((s0 + j) & 3)), acc);
         }
       }
+      if constexpr (NT > 1 && MX4) {                           // (where the groups' paths part, the compiler may move accumulators)
+        asm volatile("s_nop 15" ::: "memory");
+#pragma unroll
+        for (int g = 0; g < RG; g++) asm volatile("" : "+v"(acc[g][i]));
+      }
     }
   }
 };
