@@ -1,13 +1,20 @@
-// Few tokens: products with weights in the operand form of mx4_core.hpp (mx4, or bf16 in the same order), and the mixture of experts made of them.  Bound by the weights' bytes.
+// Few tokens: products with weights in the operand form of mx4_core.hpp (mx4, or bf16 in the same order), and the mixture of experts made of them.
 //
-// A wave streams weights from memory straight into operands of the 16 x 16 matrix ops (rows: output channels, columns: tokens, 16 at a time); the eight waves of a
-// workgroup share the reduction of a strip of channels and add up through LDS in a fixed order.  A wave has 8 KiB of weights on their way while it works on 8 KiB.
+//   Y[t][n] = sum_k X[t][k] W[k][n];   h = a(X Wg) (X Wu);   y = sum over the chosen experts of p_e (h_e Wd_e)
 //
-// Mixture of experts, four launches:
+// Bound by the weights' bytes: up to 64 tokens a weight meets few products.  A wave streams weights from memory straight into operands of the 16 x 16 matrix ops (rows: output
+// channels, columns: tokens, 16 at a time), for which they lie in the ops' own order: no LDS, no swizzle, whole lines.  The waves of a workgroup share the reduction of a strip of
+// channels and add up through LDS in a fixed order.  A wave has 8 KiB of weights on their way while it works on 8 KiB, a CU 128 KiB.
+//
+// Mixture of experts, four launches and a fifth where strips are shared (a single token: three or four):
 //   router   logits X Wr in 64 bits, a part of D a workgroup (a product of two bf16 is exact in fp32; in 64 bits the choice between near experts is the definition's)
 //   pick     a token's k largest by their rank, ties to the lowest index; shares; and the plan, which expert has which tokens (a single token's: in `up`)
 //   up       a workgroup a strip of 32 features of a chosen expert: h = a(G) U for the tokens that chose it; a row of H for each (token, choice), in the experts' order
 //   down     a workgroup a strip of 16 channels and all chosen experts one after the other: the shares' sum stays in LDS, in the order of the experts
+//   sum      where several workgroups share a strip's experts (moe_down_splits): their sums, in a fixed order
+// us, kernel by kernel (in brackets weights' bytes a second): 64 tokens, 4096 x 2048, all of 64 bf16 experts 4.8, 7.7, up 315 (6.8 TB/s), down 165 (6.5); 8 tokens of 64 mx4 experts
+// 5.0, 6.9, 62 (5.9), 34.6 (5.3); 37 tokens, 1088 x 704, 24 bf16 experts 4.2, 6.2, 15.4 (4.8), 10.7, 3.8; 1 token, 2048 x 1024, 4 of 32 3.8, -, 8.1 (with the choice), 7.1.  The large ones run at the
+// rate of the largest copy (6.4 TB/s); what bounds the small ones is the launches and each one's way through memory and LDS.
 #include "mx4_core.hpp"
 #include "mx4_rule.hpp"
 #include "stream_core.hpp"
@@ -43,6 +50,8 @@ __device__ __forceinline__ void settle(f32x4 (&acc)[RG][NT]) {
 #pragma unroll
     for (int i = 0; i < NT; i++) asm volatile("" : "+v"(acc[g][i]));
 }
+
+// H of the experts is rounded to bf16 (or mx4) once, between its two products: the op that reads it takes no more.  Sums, shares and the gate are fp32.
 
 // Tokens of a product: rows of bf16 [..][K]; the mx4 operand form; or (a small T K) rows of bf16 that the workgroup brings to mx4 in its LDS, codes [K / 32][T][16 bytes] and scales
 // [K / 32][T], while its first weights are on their way
@@ -268,6 +277,7 @@ struct UpArgs {
   MoePlan* plan_out; const double* logits; int n_parts, E, renormalise; int* picks; float* shares;   // MOE_ONE: parts of the logits, where the choice goes
 };
 
+// Gate and up of a feature are rows 16 apart of a strip, so h is made where the waves' sums are added up, and an mx4 block's largest magnitude is over 32 neighbouring lanes.
 // grid (strips, slots).  A slot is a chosen expert; without MOE there is one, and it has all tokens.  A strip is 8 RG features: a block of 64 rows, or (RG 2, bf16, whose result needs no
 // 32 features together) every other group of one.
 // MOE_ONE: a single token of the experts, whose choice every workgroup makes by itself; the first one stores it.  PASSES: over the weights, one for every 16 NT tokens of the expert
@@ -404,6 +414,8 @@ struct RowsArgs {
   const char* x; const char* x_scales; int x_steps;
   uint16_t* out;
 };
+// Few channels and a long reduction want narrow strips, for there to be workgroups, a short one wide strips, for eight waves to have loads (mx4_few_groups).  1 token of 2048 x 8192 3.6 us (8.9 MB: the
+// launch and one way through memory, LDS and back); down of 16 tokens, 16384 x 4096, 8.3 us (4.3 TB/s: two rounds of loads a wave).
 template <int RG, int NT, int SRC>
 __global__ void __launch_bounds__(THREADS, NT == 1 && (RG > 1 || SRC == LDS_MX4) ? 4 : 2) few_rows_kernel(RowsArgs e) {
   constexpr int U = 8 / RG;
@@ -474,7 +486,9 @@ struct DownArgs {
 constexpr int SUM = 20;                                    // pitch of a token's 16 channels
 constexpr int down_lds(int T) { return WAVES * T * SUM * 4; }
 
-// grid (D / 16, splits).  Where the strips are few, several workgroups share one's experts, and a second kernel adds up.
+// A wave takes units of eight steps of any expert; an op's 16 tokens go to their rows of the wave's sums with their shares (a read and a write of LDS, no atomics: the wave has its own), so that neither a
+// row of Y for each expert nor its sum over the experts goes through memory.  The waves' sums are added up in the waves' order.
+// grid (D / 16, splits).  Where the strips are few, several workgroups share one's experts, and a second kernel adds up (tickets instead, with sums past the L2s: 21 -> 24.8 us for 1 token of 2048 x 1024).
 template <bool MX4, int NT>
 __global__ void __launch_bounds__(THREADS, 2) moe_down_kernel(DownArgs e) {
   constexpr int U = 8, SRC = MX4 ? OPERAND_MX4 : ROWS_BF16;
@@ -600,7 +614,7 @@ __global__ void __launch_bounds__(256) moe_router_kernel(const uint16_t* __restr
   }
 }
 
-// A workgroup a token; the one that comes last makes the plan.
+// A workgroup a token; the one that comes last makes the plan (a launch less than a kernel for it; in every workgroup of `up` the lists took longer than this does).
 __global__ void __launch_bounds__(256) moe_pick_kernel(const double* __restrict__ parts, int n_parts, int T, int E, int k, int renormalise, int* __restrict__ picks,
                                                        float* __restrict__ shares, MoePlan* __restrict__ plan) {
   __shared__ Choice c;
@@ -676,8 +690,6 @@ __global__ void __launch_bounds__(256) moe_pick_kernel(const double* __restrict_
 
 int staged_bytes(int T, int K) { return T * K / 2 + T * K / 32; }
 
-// Waves a workgroup and features a strip: eight waves, which ask for more at once, until there are enough workgroups to have four of four waves on a CU; half strips where there
-// are fewer than the CUs.
 template <int SRC, int NT, int WHO, int RG, int W, bool PASSES = false>
 int launch_up_one(const UpArgs& a, int slots, hipStream_t s) {
   auto kern = few_up_kernel<SRC, NT, WHO, RG, W, PASSES>;
@@ -692,8 +704,8 @@ int launch_up_one(const UpArgs& a, int slots, hipStream_t s) {
 }
 template <int SRC, int WHO, bool PASSES = false>
 int launch_up_tokens(const UpArgs& a, int slots, hipStream_t s) {
-  if constexpr (SRC != LDS_MX4 && WHO != MOE_ONE)
-    if (few_up_waves(a.F / 32 * slots) == 4) return launch_up_one<SRC, 1, WHO, 4, 4, PASSES>(a, slots, s);
+  if constexpr (SRC == OPERAND_MX4 && WHO == MOE)
+    if (few_up_waves(a.F / 32 * slots, a.steps) == 4) return launch_up_one<SRC, 1, WHO, 4, 4, PASSES>(a, slots, s);
   if constexpr (SRC == ROWS_BF16 && !PASSES)
     if (few_up_halves(a.F / 32 * slots)) return launch_up_one<SRC, 1, WHO, 2, 8>(a, slots, s);
   return launch_up_one<SRC, 1, WHO, 4, 8, PASSES>(a, slots, s);

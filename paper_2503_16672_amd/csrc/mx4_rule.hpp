@@ -56,18 +56,27 @@ inline int mx4_few_groups(int N, int steps) {
   return steps >= 32 ? 2 : 4;
 }
 
-// Experts: waves a workgroup of the up projection of `strips` strips, half strips, and over how many workgroups a strip's experts of the down projection are dealt out
-// (`units`: of eight steps, at most, that a strip has)
-inline int few_up_waves(int strips) { return strips >= 512 ? 4 : 8; }
+// Experts (T D F E k, us).
+// Waves a workgroup of the up projection: eight, for what they have on their way; four where a reduction has no two loads of four KiB for each of eight (mx4, fewer than 24 steps of 128) and the
+// strips are so many that more workgroups of fewer waves fill the CUs as well.  Mx4, 4 / 8 waves: 16 1024 1024 64 2 26.6, 28.3; 8 1024 512 128 8 31.7, 33.3; 37 2048 1024 64 4 53.8, 55.6; 64 2048 768
+// 128 8 89.5, 92.3; 16 2880 1472 128 4 84.8, 85.2; the other way round 64 3584 1024 64 4 78.4, 76.8; 8 4096 2048 64 4 75.3, 73.2; 4 2048 1024 32 4 (512 strips) 24.8, 24.1.
+inline int few_up_waves(int strips, int steps) { return steps < 24 && strips >= 768 ? 4 : 8; }
+// Strips of half the width where there are fewer whole ones than CUs.  Bf16, whole / half: 1 2048 1024 32 4 (128 strips) 21.2, 19.9; 2 2048 1024 32 2 25.0, 23.2; 2 1024 512 32 4 21.2, 20.2; the
+// other way round 1 2048 1024 32 8 (256) 27.5, 28.4.
 inline bool few_up_halves(int strips) { return strips < 256; }
-// whether experts have so many tokens that 64 of them beside a strip's weights are worth their registers (a workgroup a CU less)
+// From 17 tokens on an expert may have more than 16: one pass over its weights with 64 tokens beside them (half the workgroups a CU, for the registers) where it has many, otherwise a pass for each 16.
+// Bf16, passes / one: 64 2048 1024 16 4 75.7, 65.6; 64 4096 2048 16 4 199, 157; 32 1088 704 8 4 30.1, 27.0; the other way round 37 1088 704 24 4 38.2, 40.5; 64 2048 1024 16 2 53.5, 54.6.  At T k = 10 E
+// (64 1088 704 24 4) 44.8, 43.3; mx4 29.9, 30.4.
 inline bool moe_crowded(int T, int k, int E) { return T * k > 12 * E; }
+// Over how many workgroups the experts of a strip of the down projection are dealt out (`units`: of eight steps, at most, that a strip has): as many as fill the CUs, where the sums' own launch does
+// not cost more.  1 / chosen: bf16 64 2048 768 128 8 235, 202 (2); 16 2048 1024 32 4 75.2, 69.1 (2); 37 1088 704 24 4 47.1, 38.5 (3); 64 1024 2048 32 4 121, 81 (4); mx4 64 2048 768 128 8 89.5, 76.5; 8
+// 1088 704 24 4 (24 units) 24.1, 23.7; with less work than that: 1 2048 1024 32 4 bf16 (16 units) 18.9, 19.8, mx4 15.2, 17.0; and at 180 strips of 2880 channels two lose 2 to 8 %.
 constexpr int MOE_SPLITS = 8;
 inline int moe_down_splits(int strips, int units) {
   const int fill = 256 / strips, most = units / 8;               // (a unit a wave at least)
   int s = fill < most ? fill : most;
   s = s < MOE_SPLITS ? s : MOE_SPLITS;
-  return s > 2 && units >= 24 ? s : 1;
+  return s > 1 && units >= 24 ? s : 1;
 }
 
 }  // namespace ffn24

@@ -23,12 +23,12 @@ int main() {
   while (std::scanf(" %%c %%d %%d %%d %%d %%d", &kind, &T, &K, &N, &E, &k) == 6) {
     if (kind == 'p') product("p", T, K, N, mx4_few_fused(T, K));
     if (kind == 'g') {                                       // T tokens, D = K, F = N
-      if (mx4_few_gated(T)) std::printf("up-few-%%s ", mx4_few_fused(T, K) ? "fused" : few_up_waves(N / 32) == 4 ? "operand4" : "operand8");
+      if (mx4_few_gated(T)) std::printf("up-few-%%s ", mx4_few_fused(T, K) ? "fused" : "operand");
       else std::printf("up-tile%%d ", mx4_plan(2 * N, T, (K + 127) / 128, false).tile);
       product("down", T, N, K, false);
     }
     if (kind == 'm') for (int mx4 = 0; mx4 < 2; mx4++) {
-      const int slots = T * k < E ? T * k : E, strips = N / 32 * slots, waves = few_up_waves(strips);
+      const int slots = T * k < E ? T * k : E, strips = N / 32 * slots, waves = mx4 ? few_up_waves(strips, (K + 127) / 128) : 8;
       const bool halves = !mx4 && few_up_halves(strips);
       std::printf("%%s-", mx4 ? "mx4" : "bf16");
       if (T == 1) std::printf("one-%%s ", halves ? "half" : "whole");
@@ -68,12 +68,12 @@ def test_products_take_every_kernel(paths):
 
 def test_gated_blocks_take_every_kernel(paths):
     got = paths("g", _sizes(test_gpu_mx4.test_gated_block))
-    want = {f"up-tile{i}" for i in range(4)} | {"up-few-fused", "up-few-operand4", "up-few-operand8", "down-few-operand-1-1", "down-few-operand-2-1", "down-tile3split", "down-tile3"}
+    want = {f"up-tile{i}" for i in range(4)} | {"up-few-fused", "up-few-operand", "down-few-operand-1-1", "down-few-operand-2-1", "down-tile3split", "down-tile3"}
     assert not want - got, want - got
 
 
 def test_experts_take_every_kernel(paths):
     got = paths("m", [(T, D, F, E, k) for T, D, F, E, k in test_gpu_moe.CASES])
-    want = {f"{t}-{p}" for t in ("bf16", "mx4") for p in ("one-whole", "few-4", "few-8", "crowded", "passes-4", "passes-8", "down1-alone", "down1-shared", "down4-alone", "down4-shared")}
-    want |= {"bf16-one-half", "bf16-few-half"}
+    want = {f"{t}-{p}" for t in ("bf16", "mx4") for p in ("one-whole", "few-8", "crowded", "passes-8", "down1-alone", "down1-shared", "down4-alone", "down4-shared")}
+    want |= {"bf16-one-half", "bf16-few-half", "mx4-few-4", "mx4-passes-4"}
     assert not want - got, want - got
