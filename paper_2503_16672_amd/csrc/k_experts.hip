@@ -240,7 +240,7 @@ __device__ __forceinline__ void moe_choose(const double* __restrict__ p, size_t 
   if (e < E) {
     const unsigned long long mine = c.order[e];
     rank = 0;
-#pragma unroll 4
+#pragma unroll 16
     for (int i = 0; i < E; i++) rank += c.order[i] > mine || (c.order[i] == mine && i < e);
     if (rank < k) {
       c.logit[rank] = s;

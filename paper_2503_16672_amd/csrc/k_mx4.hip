@@ -91,23 +91,25 @@ __global__ void __launch_bounds__(256) dequantise_mx4_kernel(const uint32_t* __r
   }
 }
 
-// Tokens to the operand form: a wave takes 16 rows and four steps, 4 rows and a step (256 bytes of each, whole lines) a load.  Four lanes have a block of 32.
+// Tokens to the operand form: a wave takes 4 R of 16 rows and four steps, 4 rows and a step (256 bytes of each, whole lines) a load.  Four lanes have a block of 32.
+template <int R>
 __global__ void __launch_bounds__(256) mx4_tokens_kernel(const uint16_t* __restrict__ X, int T, int K, int steps, char* __restrict__ codes, char* __restrict__ scales) {
   const int quads = (steps + 3) >> 2;
-  const int id = blockIdx.x * 4 + (threadIdx.x >> 6), group = id / quads, S = id - group * quads, lane = threadIdx.x & 63, c = lane >> 4, q = (lane >> 2) & 3, p = lane & 3;
+  const int id = blockIdx.x * 4 + (threadIdx.x >> 6), part = id / quads, S = id - part * quads, lane = threadIdx.x & 63, c = lane >> 4, q = (lane >> 2) & 3, p = lane & 3;
+  const int group = part / (4 / R), i0 = part % (4 / R) * R;
   if (16 * group >= T) return;
-  u32x4 w[4][4];                                               // [step][4 rows]
+  u32x4 w[4][R];                                               // [step][4 rows]
 #pragma unroll
   for (int j = 0; j < 4; j++)
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-      const int k = 128 * (4 * S + j) + 8 * (lane & 15), r = 16 * group + 4 * i + c;
+    for (int i = 0; i < R; i++) {
+      const int k = 128 * (4 * S + j) + 8 * (lane & 15), r = 16 * group + 4 * (i0 + i) + c;
       w[j][i] = k < K && r < T ? ld_stream(reinterpret_cast<const u32x4*>(X + (size_t)r * K + k)) : u32x4{0u, 0u, 0u, 0u};
     }
   char* out = codes + mx4_code_at(16 * group, 16 * S, steps) + q * 256 + 4 * p;
 #pragma unroll
-  for (int i = 0; i < 4; i++) {
-    const int r = 4 * i + c;
+  for (int i = 0; i < R; i++) {
+    const int r = 4 * (i0 + i) + c;
     uint32_t mine = 0u;                                        // the scales of the quarter's four steps
 #pragma unroll
     for (int j = 0; j < 4; j++) {
@@ -232,11 +234,15 @@ int launch_bf16_weight(const void* W, int K, int N, bool halves, int count, void
                      halves ? N / 2 : 0, K / 32, static_cast<char*>(out), nullptr, (size_t)K * N, (size_t)bf16_operand_size(N, K), (size_t)0);
   return (int)hipGetLastError();
 }
-int launch_mx4_tokens(const void* X, int T, int K, const Mx4Operand& o, hipStream_t s) {
-  const long long waves = (long long)((T + 15) / 16) * ((o.steps + 3) / 4);
-  hipLaunchKernelGGL(mx4_tokens_kernel, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, static_cast<const uint16_t*>(X), T, K, o.steps, const_cast<char*>(o.codes),
+template <int R>
+int launch_mx4_tokens_rows(const void* X, int T, int K, const Mx4Operand& o, hipStream_t s) {
+  const long long waves = (long long)((T + 15) / 16) * (4 / R) * ((o.steps + 3) / 4);
+  hipLaunchKernelGGL(mx4_tokens_kernel<R>, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, static_cast<const uint16_t*>(X), T, K, o.steps, const_cast<char*>(o.codes),
                      const_cast<char*>(o.scales));
   return (int)hipGetLastError();
+}
+int launch_mx4_tokens(const void* X, int T, int K, const Mx4Operand& o, hipStream_t s) {
+  return mx4_tokens_rows(T, o.steps) == 1 ? launch_mx4_tokens_rows<1>(X, T, K, o, s) : launch_mx4_tokens_rows<4>(X, T, K, o, s);
 }
 
 size_t mx4_split_scratch(int M, int N, int K) {

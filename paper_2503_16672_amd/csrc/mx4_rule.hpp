@@ -44,10 +44,13 @@ constexpr long long MX4_SPLIT_MOST = 1LL << 21;   // results of a product that c
 constexpr int FEW_MX4_TOKENS = 16, FEW_MX4_MORE = 32;
 inline bool mx4_few(int T, int K, int N) { return T <= FEW_MX4_TOKENS || (T <= FEW_MX4_MORE && K >= N && N <= 4096); }
 inline bool mx4_few_gated(int T) { return T <= FEW_MX4_TOKENS; }
-// Their tokens come to mx4 in the kernel itself, by every workgroup, or (3.7 us) by a launch before it.  us, both: 8 tokens at 4096 x 16384 gate and up 13.2, 15.8; 16 17.2, 16.3; 4 at 8192 x 28672
-// 38.4, 42.3; 8 42.1, 42.3; 2 of K 16384 to 4096 channels 10.5, 11.9; 4 12.7, 11.8.
-constexpr int MX4_FUSED_VALUES = 1 << 16;
+// Their tokens come to mx4 in the kernel itself, by every workgroup, or by a launch before it.  us, both: products (T K N) 8 4096 32768 11.8, 12.7; 16 2048 8192 5.0, 5.4; 1 28672 8192 19.7, 24.3; 3 16384
+// 4096 9.3, 9.9; 4 16384 4096 10.2, 9.9; 8 8192 8192 11.4, 9.8; 16 4096 4096 7.0, 5.7; gated (T D F) 1 4096 16384 20.7, 22.4; 12 4096 16384 23.0, 23.6; 16 4096 16384 24.2, 23.7.
+constexpr int MX4_FUSED_VALUES = 3 << 14;
 inline bool mx4_few_fused(int T, int K) { return T <= FEW_MX4_TOKENS && (long long)T * K <= MX4_FUSED_VALUES; }
+// That launch: rows in fours, of 16, that a wave takes of its four steps; one until there are eight waves a CU.  us with one / four (product and launch): 333 1088 4168 7.8, 9.1; 8192 512 1024 13.5,
+// 15.7; 2048 4096 1024 16.4, 17.3; 4096 4096 1024 21.5, 21.6; 8192 4096 1024 35.7, 35.4.
+inline int mx4_tokens_rows(int T, int steps) { return (long long)((T + 15) / 16) * ((steps + 3) / 4) < 2048 ? 1 : 4; }
 // Groups of 16 channels a strip: a wave takes 8 KiB at a time, so that a short reduction needs wide strips for eight waves to have work, a long one many strips.
 inline int mx4_few_groups(int N, int steps) {
   if (N >= 512 * 64) return 4;

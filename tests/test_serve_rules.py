@@ -15,6 +15,7 @@ MAIN = """
 using namespace ffn24;
 void product(const char* name, int T, int K, int N, bool fused) {
   const int steps = (K + 127) / 128;
+  if (!fused) std::printf("%%s-tokens-%%d ", name, mx4_tokens_rows(T, steps));
   if (mx4_few(T, K, N)) std::printf("%%s-few-%%s-%%d-%%d ", name, fused ? "fused" : "operand", T > 16 ? 2 : 1, T > 16 ? 1 : mx4_few_groups(N, steps));
   else { const Mx4Plan p = mx4_plan(N, T, steps, true); std::printf("%%s-tile%%d%%s ", name, p.tile, p.splits > 1 ? "split" : ""); }
 }
@@ -62,7 +63,7 @@ def _sizes(test):
 
 
 def test_products_take_every_kernel(paths):
-    want = {f"p-tile{i}" for i in range(4)} | {"p-tile3split", "p-few-operand-2-1"} | {f"p-few-{s}-1-{g}" for s in ("fused", "operand") for g in (1, 2, 4)}
+    want = {f"p-tile{i}" for i in range(4)} | {"p-tile3split", "p-few-operand-2-1", "p-tokens-1", "p-tokens-4"} | {f"p-few-{s}-1-{g}" for s in ("fused", "operand") for g in (1, 2, 4)}
     assert not want - (paths("p", test_gpu_mx4.PRODUCTS) | {p.replace("down", "p") for p in paths("g", _sizes(test_gpu_mx4.test_gated_block))})
 
 
