@@ -180,7 +180,8 @@ int moe_ctx_create(moe_ctx** out, int64_t T, int64_t D, int64_t F, int64_t E, in
   const bool ok = hipGetDevice(&c->device) == hipSuccess && hipMalloc(&c->Wr, (size_t)bf16_operand_size(E, D)) == hipSuccess && hipMalloc(&c->up, (size_t)(E * up)) == hipSuccess &&
                   hipMalloc(&c->down, (size_t)(E * down)) == hipSuccess && hipMalloc(&c->parts, moe_parts_size((int)T, (int)D, (int)E)) == hipSuccess &&
                   hipMalloc(&c->picks, (size_t)(4 * T * k)) == hipSuccess && hipMalloc(&c->shares, (size_t)(4 * T * k)) == hipSuccess &&
-                  hipMalloc(&c->sums, (size_t)(4 * MOE_SPLITS * T * D)) == hipSuccess && cleared(&c->plan, (int64_t)moe_plan_size()) && (!mx4 || cleared(&c->X, mx4_operand_size(T, D))) && cleared(&c->H, mx4 ? mx4_operand_size(T * k, F) : 2 * T * k * F) && hipDeviceSynchronize() == hipSuccess;
+                  hipMalloc(&c->sums, (size_t)(4 * MOE_SPLITS * T * D)) == hipSuccess && cleared(&c->plan, (int64_t)moe_plan_size()) &&
+                  (!mx4 || cleared(&c->X, mx4_operand_size(T, D))) && cleared(&c->H, mx4 ? mx4_operand_size(T * k, F) : 2 * T * k * F) && hipDeviceSynchronize() == hipSuccess;
   if (!ok) {
     (void)hipGetLastError();
     moe_ctx_destroy(c);

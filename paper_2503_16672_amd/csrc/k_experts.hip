@@ -12,9 +12,9 @@
 //   up       a workgroup a strip of 32 features of a chosen expert: h = a(G) U for the tokens that chose it; a row of H for each (token, choice), in the experts' order
 //   down     a workgroup a strip of 16 channels and all chosen experts one after the other: the shares' sum stays in LDS, in the order of the experts
 //   sum      where several workgroups share a strip's experts (moe_down_splits): their sums, in a fixed order
-// us, kernel by kernel (in brackets weights' bytes a second): 64 tokens, 4096 x 2048, all of 64 bf16 experts 4.8, 7.7, up 315 (6.8 TB/s), down 165 (6.5); 8 tokens of 64 mx4 experts
-// 5.0, 6.9, 62 (5.9), 34.6 (5.3); 37 tokens, 1088 x 704, 24 bf16 experts 4.2, 6.2, 15.4 (4.8), 10.7, 3.8; 1 token, 2048 x 1024, 4 of 32 3.8, -, 8.1 (with the choice), 7.1.  The large ones run at the
-// rate of the largest copy (6.4 TB/s); what bounds the small ones is the launches and each one's way through memory and LDS.
+// us, kernel by kernel (in brackets weights' bytes a second): 64 tokens, 4096 x 2048, all of 64 bf16 experts 4.8, 7.7, up 315 (6.8 TB/s), down 165 (6.5); 8 tokens of 64 mx4
+// experts 5.0, 6.9, 62 (5.9), 34.6 (5.3); 37 tokens, 1088 x 704, 24 bf16 experts 4.2, 6.2, 15.4 (4.8), 10.7, 3.8; 1 token, 2048 x 1024, 4 of 32 3.8, -, 8.1 (with the choice),
+// 7.1.  The large ones run at the rate of the largest copy (6.4 TB/s); what bounds the small ones is the launches and each one's way through memory and LDS.
 #include "mx4_core.hpp"
 #include "mx4_rule.hpp"
 #include "stream_core.hpp"
@@ -35,8 +35,8 @@ __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirs
 // Where a wave's weights are: the strip's codes and scales, bytes from a step (four steps' scales) to the next
 struct Strip { const char* codes; const char* scales; int steps; };
 
-// The scaled op with its accumulator in place, as in mx4_core.hpp (the builtin also keeps 32 bytes of registers for an operand of 16).  The compiler does not see what it needs: two
-// states behind the vector instructions that make its operands, and where the same accumulator comes round at once (RG 1), the op before it; settle() before results are read.
+// The scaled op with its accumulator in place, as in mx4_core.hpp (the builtin also keeps 32 bytes of registers for an operand of 16).  The compiler does not see what it needs:
+// two states behind the vector instructions that make its operands, and where the same accumulator comes round at once (RG 1), the op before it; settle() before results are read.
 template <int RG>
 __device__ __forceinline__ void op16_mx4_few(const u32x4& a, const u32x4& b, uint32_t sa, uint32_t sb, f32x4& c) {
   if constexpr (RG == 1) asm volatile("s_nop 7\n\tv_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[0,0,0] op_sel_hi:[0,0,0] cbsz:4 blgp:4" : "+v"(c) : "v"(a), "v"(b), "v"(sa), "v"(sb));
@@ -53,8 +53,8 @@ __device__ __forceinline__ void settle(f32x4 (&acc)[RG][NT]) {
 
 // H of the experts is rounded to bf16 (or mx4) once, between its two products: the op that reads it takes no more.  Sums, shares and the gate are fp32.
 
-// Tokens of a product: rows of bf16 [..][K]; the mx4 operand form; or (a small T K) rows of bf16 that the workgroup brings to mx4 in its LDS, codes [K / 32][T][16 bytes] and scales
-// [K / 32][T], while its first weights are on their way
+// Tokens of a product: rows of bf16 [..][K]; the mx4 operand form; or (a small T K) rows of bf16 that the workgroup brings to mx4 in its LDS, codes [K / 32][T][16 bytes] and
+// scales [K / 32][T], while its first weights are on their way
 enum { ROWS_BF16 = 0, OPERAND_MX4 = 1, LDS_MX4 = 2 };
 struct Tokens { const char* p; const char* scales; int K, steps, T; };
 constexpr int LDS_PIECES = MX4_FUSED_VALUES / 8 / THREADS;     // of 8 values a work item
@@ -278,10 +278,10 @@ struct UpArgs {
 };
 
 // Gate and up of a feature are rows 16 apart of a strip, so h is made where the waves' sums are added up, and an mx4 block's largest magnitude is over 32 neighbouring lanes.
-// grid (strips, slots).  A slot is a chosen expert; without MOE there is one, and it has all tokens.  A strip is 8 RG features: a block of 64 rows, or (RG 2, bf16, whose result needs no
-// 32 features together) every other group of one.
-// MOE_ONE: a single token of the experts, whose choice every workgroup makes by itself; the first one stores it.  PASSES: over the weights, one for every 16 NT tokens of the expert
-// (otherwise it has no more than those).
+// grid (strips, slots).  A slot is a chosen expert; without MOE there is one, and it has all tokens.  A strip is 8 RG features: a block of 64 rows, or (RG 2, bf16, whose result
+// needs no 32 features together) every other group of one.
+// MOE_ONE: a single token of the experts, whose choice every workgroup makes by itself; the first one stores it.  PASSES: over the weights, one for every 16 NT tokens of the
+// expert (otherwise it has no more than those).
 enum { ALL_TOKENS = 0, MOE = 1, MOE_ONE = 2 };
 template <int SRC, int NT, int WHO, int RG, int W, bool PASSES = false>
 __global__ void __launch_bounds__(64 * W, NT == 1 && WHO != MOE_ONE ? 4 : 2) few_up_kernel(UpArgs e) {
@@ -414,8 +414,8 @@ struct RowsArgs {
   const char* x; const char* x_scales; int x_steps;
   uint16_t* out;
 };
-// Few channels and a long reduction want narrow strips, for there to be workgroups, a short one wide strips, for eight waves to have loads (mx4_few_groups).  1 token of 2048 x 8192 3.6 us (8.9 MB: the
-// launch and one way through memory, LDS and back); down of 16 tokens, 16384 x 4096, 8.3 us (4.3 TB/s: two rounds of loads a wave).
+// Few channels and a long reduction want narrow strips, for there to be workgroups, a short one wide strips, for eight waves to have loads (mx4_few_groups).  1 token of 2048 x
+// 8192 3.6 us (8.9 MB: the launch and one way through memory, LDS and back); down of 16 tokens, 16384 x 4096, 8.3 us (4.3 TB/s: two rounds of loads a wave).
 template <int RG, int NT, int SRC>
 __global__ void __launch_bounds__(THREADS, NT == 1 && (RG > 1 || SRC == LDS_MX4) ? 4 : 2) few_rows_kernel(RowsArgs e) {
   constexpr int U = 8 / RG;
@@ -486,9 +486,10 @@ struct DownArgs {
 constexpr int SUM = 20;                                    // pitch of a token's 16 channels
 constexpr int down_lds(int T) { return WAVES * T * SUM * 4; }
 
-// A wave takes units of eight steps of any expert; an op's 16 tokens go to their rows of the wave's sums with their shares (a read and a write of LDS, no atomics: the wave has its own), so that neither a
-// row of Y for each expert nor its sum over the experts goes through memory.  The waves' sums are added up in the waves' order.
-// grid (D / 16, splits).  Where the strips are few, several workgroups share one's experts, and a second kernel adds up (tickets instead, with sums past the L2s: 21 -> 24.8 us for 1 token of 2048 x 1024).
+// A wave takes units of eight steps of any expert; an op's 16 tokens go to their rows of the wave's sums with their shares (a read and a write of LDS, no atomics: the wave has
+// its own), so that neither a row of Y for each expert nor its sum over the experts goes through memory.  The waves' sums are added up in the waves' order.
+// grid (D / 16, splits).  Where the strips are few, several workgroups share one's experts, and a second kernel adds up (tickets instead, with sums past the L2s: 21 -> 24.8 us
+// for 1 token of 2048 x 1024).
 template <bool MX4, int NT>
 __global__ void __launch_bounds__(THREADS, 2) moe_down_kernel(DownArgs e) {
   constexpr int U = 8, SRC = MX4 ? OPERAND_MX4 : ROWS_BF16;

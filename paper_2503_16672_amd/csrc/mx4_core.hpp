@@ -70,6 +70,10 @@ struct Mx4Gemm {
   int first, steps;         // the part of the reduction
 };
 
+// Bound by the matrix units where there is work for them: the op takes 18 cycles in a loop of nothing else (7.16 PFLOP/s with random bits at the 1.98 GHz that the power leaves;
+// 8.9 with zeros), a step of the 256 x 256 tile 1300-1390 for 64 of them (1152), 5.1-5.25 PFLOP/s at K 16384.  A tile's results cost as much as six steps (bf16, all CUs' stores
+// at once) or ten (the gate), so at K 4096 two 256 x 128 tiles a CU win, whose results and ops overlap: 8192 x 4096 x 16384 253 us (4.35 PFLOP/s, units busy 63 %), gate and up
+// 8192 x 4096 x 32768 487 (4.5, 69 %); down 8192 x 16384 x 4096 on 256 x 256 220 (5.0, 73 %).  Small products are bound by launches and latency: 333 x 1088 x 4168 5.5 us.
 // The block tile: 2 x 2 waves of 16 AM x 16 BN.  The ring holds RING stages of one step; the scales of four steps come beside them.  256 x 128 tiles have a ring of three, so that
 // two share a CU: one's results go out while the other's matrix ops run.
 template <int AM, int BN>
@@ -312,6 +316,7 @@ struct Mx4Part {   // the sums of a part of the reduction, [part][n][m]
   }
 };
 
+// h is rounded once, to mx4, from 32 bits: the down product takes nothing wider.  The gate's arithmetic is what this epilogue costs (12500-15000 cycles of a 256 x 256 tile).
 // The gated block: h = a(G) U of 32 features of a token lies in four lanes, 8 each; their largest magnitude gives the scale, and the codes go out as the down product reads
 // them: 16 tokens' 32 features are 256 bytes in a row.
 template <bool CUBIC>
