@@ -37,7 +37,8 @@ def _check(ctx, X, Wr, Wgu, Wd, act, renormalise, weights):
 
 
 CASES = [(1, 64, 64, 1, 1), (1, 2048, 1024, 32, 4), (2, 128, 192, 5, 2), (7, 320, 704, 24, 3), (8, 1024, 512, 64, 8), (16, 192, 320, 8, 8), (17, 576, 128, 100, 7), (33, 64, 448, 17, 5),
-         (64, 512, 320, 256, 16), (64, 256, 192, 3, 1), (40, 4096, 64, 16, 2), (5, 64, 4160, 7, 3), (48, 128, 128, 128, 16), (1, 128, 8256, 4, 2), (64, 4416, 192, 5, 4)]
+         (64, 512, 320, 256, 16), (64, 256, 192, 3, 1), (40, 4096, 64, 16, 2), (5, 64, 4160, 7, 3), (48, 128, 128, 128, 16), (1, 128, 8256, 4, 2), (64, 4416, 192, 5, 4),
+         (64, 16384, 64, 256, 16), (1, 16384, 128, 256, 16), (50, 64, 65536, 4, 3), (1, 64, 65536, 3, 3), (64, 1536, 512, 16, 16)]
 
 
 @pytest.mark.parametrize("weights", ["bf16", "mx4"])

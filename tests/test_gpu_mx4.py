@@ -68,7 +68,8 @@ def test_values_of_all_codes():
 # few tokens in each kernel and form, the GEMM's tiles (tests/test_serve_rules.py), k and channels that end inside a step, a block of 64 and a tile, reductions that are split
 PRODUCTS = [(1, 32, 8), (1, 2048, 520), (3, 96, 24), (16, 160, 264), (17, 544, 264), (32, 1088, 1000), (33, 1088, 1000), (64, 128, 72), (65, 224, 256), (333, 1088, 4168),
             (1000, 640, 3000), (1500, 512, 2048), (4099, 288, 4104), (2, 16416, 16), (1, 512, 16400), (13, 384, 33000), (29, 8224, 200), (100, 16384, 512), (130, 8992, 136),
-            (48, 131072, 8), (5, 131072, 40), (9, 1024, 9000), (9, 4096, 8200), (16, 4224, 8200), (16, 4224, 33000), (2100, 3008, 5000), (4096, 16384, 4096), (2000, 4096, 8200)]
+            (48, 131072, 8), (5, 131072, 40), (9, 1024, 9000), (9, 4096, 8200), (16, 4224, 8200), (16, 4224, 33000), (2100, 3008, 5000), (4096, 16384, 4096), (2000, 4096, 8200),
+            (3, 32, 1 << 20), (40, 64, 1 << 20), (1 << 20, 32, 8), (1 << 20, 96, 136), (3, 131072, 2048)]
 
 
 @pytest.mark.parametrize("T,K,N", PRODUCTS)
@@ -104,7 +105,7 @@ def _gated(T, D, F, act, seed=1):
 @pytest.mark.parametrize("act", ["silu", "gelu"])
 @pytest.mark.parametrize("T,D,F", [(1, 64, 64), (2, 128, 192), (16, 576, 1344), (17, 64, 448), (33, 192, 448), (64, 512, 2048), (65, 256, 512), (24, 2048, 4160), (4, 3968, 16384),
                                    (700, 320, 704), (1609, 640, 640), (2500, 512, 2816), (40, 1024, 8192), (12, 8192, 512), (16, 4160, 16384), (3000, 1024, 4096), (2000, 4096, 4160),
-                                   (4096, 8192, 2048), (4096, 16384, 2048)])
+                                   (4096, 8192, 2048), (4096, 16384, 2048), (3, 131072, 64), (3, 64, 131072), (70, 64, 131072), (70, 131072, 64), (1 << 18, 64, 128)])
 def test_gated_block(T, D, F, act):
     X, Wgu, Wd, (y, d) = _gated(T, D, F, act)
     ctx = serve.GatedMx4Context(T + 5, Wgu, Wd, act=act)
