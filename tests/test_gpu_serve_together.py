@@ -16,8 +16,7 @@ def _normal(shape, seed):
 
 
 def _norm(s):
-    """The norm of the stored sum in bf16, and of each value the neighbour that its rounding might have given instead: the norm itself is tested against 64 bits elsewhere, so
-    the products behind it are held to what it gives here."""
+    """The norm of the stored sum in bf16: it is tested against 64 bits elsewhere, so the products behind it are held to what it gives here."""
     from paper_2503_16672_amd import block
     return block.layer_norm_fwd(s, torch.ones(s.shape[1], device="cuda"), torch.zeros(s.shape[1], device="cuda"))[0]
 
@@ -41,6 +40,26 @@ def test_a_stack_of_sublayers(T):
     assert ref.holds(c, y, d)
     with pytest.raises(ValueError):
         first.quantised("int4")
+
+
+def test_two_streams_at_once():
+    """Contexts of their own, one set of weights and tokens: calls that run beside each other give what they give alone, with other sizes before and after."""
+    D, F, E, k = 512, 704, 12, 3
+    Wr, Wgu, Wd = _normal((D, E), 1), _normal((E, D, 2 * F), 2) * D ** -0.5, _normal((E, F, D), 3) * F ** -0.5
+    X, W4 = _normal((64, D), 4), serve.Mx4Weight(Wgu[0])
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    sets = [(serve.MoeContext(64, Wr, Wgu, Wd, k, weights=w), serve.GatedMx4Context(64, Wgu[i].contiguous(), Wd[i].contiguous())) for i, w in enumerate(("bf16", "mx4"))]
+    work = lambda c, t: (c[0].fwd(X[:t]), c[1].fwd(X[:t]), serve.linear_mx4(X[:t], W4))
+    sizes = (64, 1, 17, 5, 64, 33)
+    want = [[work(c, t) for t in sizes] for c in sets]
+    torch.cuda.synchronize()
+    got = [[] for _ in sets]
+    for _ in range(20):
+        for c, s, out in zip(sets, streams, got):
+            with torch.cuda.stream(s):
+                out[:] = [work(c, t) for t in sizes]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for one, other in zip(want, got) for x, y in zip(one, other) for a, b in zip(x, y))
 
 
 def _large(shape, seed, scale=1.0):
