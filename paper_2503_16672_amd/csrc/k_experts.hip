@@ -12,9 +12,9 @@
 //   up       a workgroup a strip of 32 features of a chosen expert: h = a(G) U for the tokens that chose it; a row of H for each (token, choice), in the experts' order
 //   down     a workgroup a strip of 16 channels and all chosen experts one after the other: the shares' sum stays in LDS, in the order of the experts
 //   sum      where several workgroups share a strip's experts (moe_down_splits): their sums, in a fixed order
-// us, kernel by kernel (in brackets weights' bytes a second): 64 tokens, 4096 x 2048, all of 64 bf16 experts 4.8, 7.7, up 315 (6.8 TB/s), down 165 (6.5); 8 tokens of 64 mx4
-// experts 5.0, 6.9, 62 (5.9), 34.6 (5.3); 37 tokens, 1088 x 704, 24 bf16 experts 4.2, 6.2, 15.4 (4.8), 10.7, 3.8; 1 token, 2048 x 1024, 4 of 32 3.8, -, 8.1 (with the choice),
-// 7.1.  The large ones run at the rate of the largest copy (6.4 TB/s); what bounds the small ones is the launches and each one's way through memory and LDS.
+// us, kernel by kernel (in brackets weights' bytes a second): 64 tokens, 4096 x 2048, all of 64 bf16 experts 5.0, 5.8, up 312 (6.9 TB/s), down 166 (6.5); 8 tokens of 64 mx4
+// experts 5.0, 5.9, 61.5 (5.9), 35 (5.3); 37 tokens, 1088 x 704, 24 bf16 experts 4.2, 5.8, 15.3 (4.8), 10.8, 3.9; 1 token, 2048 x 1024, 4 of 32 4.0, -, 8.0 (with the choice),
+// 7.0.  The large ones run at the rate of the largest copy (6.4 TB/s); what bounds the small ones is the launches and each one's way through memory and LDS.
 #include "mx4_core.hpp"
 #include "mx4_rule.hpp"
 #include "stream_core.hpp"
@@ -204,44 +204,48 @@ template <class T> __device__ __forceinline__ T get(const T* p) { return __hip_a
 // A value as an integer of the same order; NaN below all
 __device__ __forceinline__ unsigned long long order_of(double x) {
   const unsigned long long b = __builtin_bit_cast(unsigned long long, x + 0.0);   // (-0 is 0)
-  return x != x ? 0ull : b >> 63 ? ~b : b | 1ull << 63;
+  return x != x ? 1ull : b >> 63 ? ~b : b | 1ull << 63;
 }
 
-// The choice of one token by the first 256 work items of a workgroup (all of them come here): its k experts by falling logit, and their shares.  p: the token's parts of the
-// logits, `stride` values from a part to the next.
+// The choice of one token by a workgroup of THREADS: its k experts by falling logit, and their shares.  Several work items have an expert, each a part of its logit's sum and of
+// the comparisons that give its rank.  p: the token's parts of the logits, `stride` values from a part to the next.
 struct Choice {
-  double sums[256], logit[MOE_MAX_K];
+  double sums[THREADS], logit[MOE_MAX_K];
   unsigned long long order[MOE_E];
-  int which[MOE_MAX_K];
+  int rank[MOE_E], which[MOE_MAX_K];
   float share[MOE_MAX_K], part[4];
 };
 __device__ __forceinline__ void moe_choose(const double* __restrict__ p, size_t stride, int n_parts, int E, int k, bool renormalise, Choice& c) {
-  const int e = threadIdx.x, ways = 256 / E, way = e / E, ex = e - way * E;
-  if (e < 256) {
-    double s = 0.0;
-    if (way < ways)
-      for (int i = way; i < n_parts; i += 8 * ways) {          // eight on their way at once
-        double v[8];
-#pragma unroll
-        for (int j = 0; j < 8; j++) v[j] = i + j * ways < n_parts ? p[(size_t)(i + j * ways) * stride + ex] : 0.0;
-#pragma unroll
-        for (int j = 0; j < 8; j++) s += v[j];
-      }
-    c.sums[e] = s;
-  }
-  __syncthreads();
+  const int e = threadIdx.x, ways = THREADS / E, way = e / E, ex = e - way * E;
   double s = 0.0;
+  if (way < ways)
+    for (int i = way; i < n_parts; i += 8 * ways) {            // eight on their way at once
+      double v[8];
+#pragma unroll
+      for (int j = 0; j < 8; j++) v[j] = i + j * ways < n_parts ? p[(size_t)(i + j * ways) * stride + ex] : 0.0;
+#pragma unroll
+      for (int j = 0; j < 8; j++) s += v[j];
+    }
+  c.sums[e] = s;
+  __syncthreads();
+  s = 0.0;
   if (e < E) {
     for (int i = 0; i < ways; i++) s += c.sums[i * E + e];
     c.order[e] = order_of(s);
+    c.rank[e] = 0;
+  }
+  __syncthreads();
+  if (way < ways) {
+    const unsigned long long mine = c.order[ex];
+    int before = 0;
+#pragma unroll 4
+    for (int i = way; i < E; i += ways) before += c.order[i] > (i < ex ? mine - 1 : mine);   // (an equal one of a lower index is before it; no order is 0)
+    atomicAdd(&c.rank[ex], before);
   }
   __syncthreads();
   int rank = MOE_E;
   if (e < E) {
-    const unsigned long long mine = c.order[e];
-    rank = 0;
-#pragma unroll 16
-    for (int i = 0; i < E; i++) rank += c.order[i] > mine || (c.order[i] == mine && i < e);
+    rank = c.rank[e];
     if (rank < k) {
       c.logit[rank] = s;
       c.which[rank] = e;
@@ -253,7 +257,7 @@ __device__ __forceinline__ void moe_choose(const double* __restrict__ p, size_t 
   float sum = x;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d, 64);
-  if (e < 256 && (e & 63) == 0) c.part[e >> 6] = sum;
+  if (e < MOE_E && (e & 63) == 0) c.part[e >> 6] = sum;
   __syncthreads();
   if (rank < k) c.share[rank] = x / (c.part[0] + c.part[1] + c.part[2] + c.part[3]);
   __syncthreads();
@@ -288,6 +292,7 @@ __global__ void __launch_bounds__(64 * W, NT == 1 && WHO != MOE_ONE ? 4 : 2) few
   constexpr bool MX4 = SRC != ROWS_BF16;
   constexpr int U = PASSES && MX4 ? 1 : 8 / RG, NP = 1, FEATS = 8 * RG;   // (more would not fit the registers)
   static_assert(RG == 4 || (RG == 2 && !MX4), "whole blocks of 32 features");
+  static_assert(WHO != MOE_ONE || W == WAVES, "chosen by all work items");
   __shared__ __attribute__((aligned(16))) float red[W * 16 * RG * RED];
   extern __shared__ __attribute__((aligned(16))) char staged_lds[];   // LDS_MX4: T K 17 / 32 bytes
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, q = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -616,7 +621,7 @@ __global__ void __launch_bounds__(256) moe_router_kernel(const uint16_t* __restr
 }
 
 // A workgroup a token; the one that comes last makes the plan (a launch less than a kernel for it; in every workgroup of `up` the lists took longer than this does).
-__global__ void __launch_bounds__(256) moe_pick_kernel(const double* __restrict__ parts, int n_parts, int T, int E, int k, int renormalise, int* __restrict__ picks,
+__global__ void __launch_bounds__(THREADS) moe_pick_kernel(const double* __restrict__ parts, int n_parts, int T, int E, int k, int renormalise, int* __restrict__ picks,
                                                        float* __restrict__ shares, MoePlan* __restrict__ plan) {
   __shared__ Choice c;
   __shared__ int count[MOE_E], cursor[MOE_E], come;
@@ -631,24 +636,24 @@ __global__ void __launch_bounds__(256) moe_pick_kernel(const double* __restrict_
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
   if (tid == 0) come = __hip_atomic_fetch_add(&plan->ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  count[tid] = 0;
+  if (tid < MOE_E) count[tid] = 0;
   __syncthreads();
   if (come != T - 1) return;
 
   const int pairs = T * k;
-  int mine[MOE_PAIRS / 256];
-  float p[MOE_PAIRS / 256];
+  int mine[MOE_PAIRS / THREADS];
+  float p[MOE_PAIRS / THREADS];
 #pragma unroll
-  for (int j = 0; j < MOE_PAIRS / 256; j++) {
-    const int i = 256 * j + tid;
+  for (int j = 0; j < MOE_PAIRS / THREADS; j++) {
+    const int i = THREADS * j + tid;
     if (i < pairs) {
       mine[j] = get(&plan->picks[i]);
       p[j] = get(&plan->shares[i]);
     }
   }
 #pragma unroll
-  for (int j = 0; j < MOE_PAIRS / 256; j++)
-    if (256 * j + tid < pairs) atomicAdd(&count[mine[j]], 1);
+  for (int j = 0; j < MOE_PAIRS / THREADS; j++)
+    if (THREADS * j + tid < pairs) atomicAdd(&count[mine[j]], 1);
   __syncthreads();
   if (tid < 64) {                                              // four experts a lane: pairs before them below, chosen ones above
     int n[4], all = 0;
@@ -681,10 +686,10 @@ __global__ void __launch_bounds__(256) moe_pick_kernel(const double* __restrict_
   }
   __syncthreads();
 #pragma unroll
-  for (int j = 0; j < MOE_PAIRS / 256; j++)
-    if (256 * j + tid < pairs) {
+  for (int j = 0; j < MOE_PAIRS / THREADS; j++)
+    if (THREADS * j + tid < pairs) {
       const int at = atomicAdd(&cursor[mine[j]], 1);
-      plan->list[at] = 256 * j + tid;
+      plan->list[at] = THREADS * j + tid;
       plan->share[at] = p[j];
     }
 }
@@ -755,7 +760,7 @@ int launch_moe_route(const MoeCall& m, const Mx4Operand* x, hipStream_t s) {
   hipLaunchKernelGGL(moe_router_kernel, dim3((unsigned)n, (unsigned)((m.T + 15) / 16)), dim3(256), 0, s, static_cast<const uint16_t*>(m.X), static_cast<const char*>(m.Wr), m.T, m.D,
                      m.E, static_cast<double*>(m.logits), x ? x->steps : 0, x ? const_cast<char*>(x->codes) : nullptr, x ? const_cast<char*>(x->scales) : nullptr);
   if (m.T > 1)
-    hipLaunchKernelGGL(moe_pick_kernel, dim3((unsigned)m.T), dim3(256), 0, s, static_cast<const double*>(m.logits), n, m.T, m.E, m.k, (int)m.renormalise, m.picks, m.shares,
+    hipLaunchKernelGGL(moe_pick_kernel, dim3((unsigned)m.T), dim3(THREADS), 0, s, static_cast<const double*>(m.logits), n, m.T, m.E, m.k, (int)m.renormalise, m.picks, m.shares,
                        static_cast<MoePlan*>(m.plan));
   return (int)hipGetLastError();
 }
