@@ -48,10 +48,10 @@ FFN24_API int gated_mx4_fwd(gated_mx4_ctx* ctx, const void* X, int64_t T, void* 
  *   l = x Wr  (Wr bf16 [D][E]; in 64 bits);  its k experts: the largest l, among equals the lowest index (a NaN counts as the lowest);
  *   shares p = exp(l) over the sum of exp(l), of the chosen ones (renormalise != 0) or of all E;
  *   y = bf16(sum over the chosen of p_e (h_e Wd_e)),  h_e = a(x Wg_e) (x Wu_e), sums in fp32;
- * FFN24_EXPERTS_BF16: h_e is rounded to bf16;  FFN24_EXPERTS_MX4: x, h_e and the weights are mx4 (the router is not).
+ * FFN24_EXPERTS_BF16: h_e is held to 2^-16 of it, as two bf16;  FFN24_EXPERTS_MX4: x, h_e and the weights are mx4 (the router is not).
  * 1 <= T <= 64 (every call says how many it has), D and F multiples of 64, D at most 2^14, F at most 2^16, 1 <= E <= 256, 1 <= k <= min(E, 16).  moe_set_weights lays out Wr,
  * Wgu [E][D][2 F] and Wd [E][F][D] in the context (their size, in mx4 17/64 of it), which does not need them afterwards.  Workspace besides:
- * at most 49 MiB + 2 KiB F.  moe_fwd stores the choice too where experts (int32 [T][k], by falling l) and shares (fp32 [T][k]) are given: both or
+ * at most 49 MiB + 4 KiB F.  moe_fwd stores the choice too where experts (int32 [T][k], by falling l) and shares (fp32 [T][k]) are given: both or
  * neither.  No other token's values enter a token's result, and results repeat bit for bit; the order of its sums may depend on how many tokens
  * there are and which experts they chose.  The contexts' other rules are those of gated_ctx. */
 typedef enum { FFN24_EXPERTS_BF16 = 0, FFN24_EXPERTS_MX4 = 1 } ffn24_experts;

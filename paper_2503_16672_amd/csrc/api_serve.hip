@@ -44,7 +44,7 @@ struct moe_ctx {
   GateCoefficients gate;
   int renormalise, device, have_weights;
   MoeWeights w;
-  void *Wr, *up, *down, *X, *parts, *plan, *sums, *H, *picks, *shares;   // X, H: tokens and activations as mx4 (H: or bf16)
+  void *Wr, *up, *down, *X, *parts, *plan, *sums, *H, *picks, *shares;   // X, H: tokens and activations as mx4 (H: or two bf16 a value)
 };
 
 extern "C" {
@@ -181,7 +181,7 @@ int moe_ctx_create(moe_ctx** out, int64_t T, int64_t D, int64_t F, int64_t E, in
                   hipMalloc(&c->down, (size_t)(E * down)) == hipSuccess && hipMalloc(&c->parts, moe_parts_size((int)T, (int)D, (int)E)) == hipSuccess &&
                   hipMalloc(&c->picks, (size_t)(4 * T * k)) == hipSuccess && hipMalloc(&c->shares, (size_t)(4 * T * k)) == hipSuccess &&
                   hipMalloc(&c->sums, (size_t)(4 * MOE_SPLITS * T * D)) == hipSuccess && cleared(&c->plan, (int64_t)moe_plan_size()) &&
-                  (!mx4 || cleared(&c->X, mx4_operand_size(T, D))) && cleared(&c->H, mx4 ? mx4_operand_size(T * k, F) : 2 * T * k * F) && hipDeviceSynchronize() == hipSuccess;
+                  (!mx4 || cleared(&c->X, mx4_operand_size(T, D))) && cleared(&c->H, mx4 ? mx4_operand_size(T * k, F) : 4 * ((T * k + 15) / 16 * 16) * F) && hipDeviceSynchronize() == hipSuccess;
   if (!ok) {
     (void)hipGetLastError();
     moe_ctx_destroy(c);

@@ -10,7 +10,7 @@
 //   router   logits X Wr in 64 bits, a part of D a workgroup (a product of two bf16 is exact in fp32; in 64 bits the choice between near experts is the definition's)
 //   pick     a token's k largest by their rank, ties to the lowest index; shares; and the plan, which expert has which tokens (a single token's: in `up`)
 //   up       a workgroup a strip of 32 features of a chosen expert: h = a(G) U for the tokens that chose it; a row of H for each (token, choice), in the experts' order
-//   down     a workgroup a strip of 16 channels and all chosen experts one after the other: the shares' sum stays in LDS, in the order of the experts
+//   down     a workgroup a strip of 16 to 64 channels and all chosen experts one after the other: the shares' sum stays in LDS, in the order of the experts
 //   sum      where several workgroups share a strip's experts (moe_down_splits): their sums, in a fixed order
 // us, kernel by kernel (in brackets weights' bytes a second): 64 tokens, 4096 x 2048, all of 64 bf16 experts 5.0, 5.8, up 312 (6.9 TB/s), down 166 (6.5); 8 tokens of 64 mx4
 // experts 5.0, 5.9, 61.5 (5.9), 35 (5.3); 37 tokens, 1088 x 704, 24 bf16 experts 4.2, 5.8, 15.3 (4.8), 10.8, 3.9; 1 token, 2048 x 1024, 4 of 32 4.0, -, 8.0 (with the choice),
@@ -51,11 +51,18 @@ __device__ __forceinline__ void settle(f32x4 (&acc)[RG][NT]) {
     for (int i = 0; i < NT; i++) asm volatile("" : "+v"(acc[g][i]));
 }
 
-// H of the experts is rounded to bf16 (or mx4) once, between its two products: the op that reads it takes no more.  Sums, shares and the gate are fp32.
+// Sums, shares and the gate are fp32.  Between the products h of mx4 experts is rounded to mx4, which their definition says; of bf16 experts it is the sum of two bf16, its upper
+// 16 bits and the rest rounded, which leaves 2^-16 of it: the op takes no fp32, and rounded to one bf16 h would cost as much accuracy as Y's own rounding.
+__device__ __forceinline__ uint32_t two_parts(float h) {          // the first in the low half; an infinity or a NaN has no rest
+  const float first = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, h) & 0xFFFF0000u);
+  const float rest = magnitude(h) < 0x7F800000u ? h - first : 0.f;
+  return __builtin_bit_cast(uint32_t, first) >> 16 | pack_bf16x2(0.f, rest);
+}
 
-// Tokens of a product: rows of bf16 [..][K]; the mx4 operand form; or (a small T K) rows of bf16 that the workgroup brings to mx4 in its LDS, codes [K / 32][T][16 bytes] and
-// scales [K / 32][T], while its first weights are on their way
-enum { ROWS_BF16 = 0, OPERAND_MX4 = 1, LDS_MX4 = 2 };
+// Tokens of a product: rows of bf16 [..][K]; the mx4 operand form; (a small T K) rows of bf16 that the workgroup brings to mx4 in its LDS, codes [K / 32][T][16 bytes] and
+// scales [K / 32][T], while its first weights are on their way; or values in two parts as the bf16 op reads them, [16 rows][step of 32 k][part][lane][16 bytes]
+enum { ROWS_BF16 = 0, OPERAND_MX4 = 1, LDS_MX4 = 2, OPERAND_PARTS = 3 };
+__device__ __forceinline__ size_t parts_at(int r, int s, int q, int K) { return ((size_t)(r >> 4) * (K >> 5) + s) * 2048 + q * 256 + (r & 15) * 16; }   // row r, k 32 s + 8 q
 struct Tokens { const char* p; const char* scales; int K, steps, T; };
 constexpr int LDS_PIECES = MX4_FUSED_VALUES / 8 / THREADS;     // of 8 values a work item
 
@@ -90,13 +97,15 @@ struct StagedTokens {
 // for behind the weights would wait for them.
 template <int SRC, int RG, int U, int NP, int GS = 1>   // GS: from a group to the next of the strip's
 struct Unit {
-  static constexpr bool MX4 = SRC != ROWS_BF16;
+  static constexpr bool MX4 = SRC == OPERAND_MX4 || SRC == LDS_MX4;
   static constexpr int SU = MX4 ? (U + 3) / 4 : 1, XU = SRC == LDS_MX4 ? 1 : U;
-  u32x4 w[U][RG], x[XU][NP];
+  static constexpr int P = SRC == OPERAND_PARTS ? 2 : 1, C = P == 2 && RG == 1 ? U / 2 : U;   // parts of a value; steps of a later group at once (eight in parts would not fit the registers)
+  u32x4 w[U][RG], x[XU][NP][P];
   uint32_t sw[SU][RG], sx[SRC == OPERAND_MX4 ? SU : 1][NP];
 
-  // the lane's 16 bytes of token row `row` in step s, and its scales of the four steps of s
-  static __device__ __forceinline__ u32x4 token(const Tokens& t, int row, bool on, int s, int q) {
+  // the lane's 16 bytes of token row `row` in step s (part p of its values), and its scales of the four steps of s
+  static __device__ __forceinline__ u32x4 token(const Tokens& t, int row, bool on, int s, int q, int p) {
+    if constexpr (SRC == OPERAND_PARTS) return *reinterpret_cast<const u32x4*>(t.p + parts_at(row, s, q, t.K) + 1024 * p);   // (`row` is one that is there)
     if (!on) return u32x4{0u, 0u, 0u, 0u};
     if constexpr (SRC == OPERAND_MX4) return *reinterpret_cast<const u32x4*>(t.p + mx4_code_at(row, 4 * s + q, t.steps));
     return *reinterpret_cast<const u32x4*>(t.p + ((size_t)row * t.K + 32 * s + 8 * q) * 2);
@@ -111,7 +120,9 @@ struct Unit {
 #pragma unroll
       for (int j = 0; j < U; j++)
 #pragma unroll
-        for (int i = 0; i < NP; i++) x[j][i] = token(t, row[i], on[i], min(s0 + j, p.steps - 1), q);
+        for (int i = 0; i < NP; i++)
+#pragma unroll
+          for (int a = 0; a < P; a++) x[j][i][a] = token(t, row[i], on[i], min(s0 + j, p.steps - 1), q, a);
     }
     if constexpr (SRC == OPERAND_MX4) {
 #pragma unroll
@@ -143,36 +154,41 @@ struct Unit {
       else acc[g][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w[j][g]), __builtin_bit_cast(bf16x8, v), acc[g][i], 0, 0, 0);
     }
   }
-  // the ops of the unit for `groups` groups of tokens; those from NP on are asked for here, a group's steps together
+  // the ops of the unit for `groups` groups of tokens; those from NP on are asked for here, C steps of a group (and part) together
   template <int NT>
   __device__ __forceinline__ void ops(const Tokens& t, const int (&row)[NT], const bool (&on)[NT], int groups, int s0, int steps, int q, f32x4 (&acc)[RG][NT]) const {
 #pragma unroll
     for (int i = 0; i < NT; i++) {
       if (i > 0 && i >= groups) break;
-      u32x4 v[U];
       uint32_t sv[SU];
-#pragma unroll
-      for (int j = 0; j < U; j++) {
-        if constexpr (SRC == LDS_MX4) {
-          v[j] = u32x4{0u, 0u, 0u, 0u};
-        } else {
-          v[j] = i < NP ? x[j][i < NP ? i : 0] : token(t, row[i], on[i], min(s0 + j, steps - 1), q);
-        }
-      }
 #pragma unroll
       for (int j = 0; j < SU; j++) {
         sv[j] = 0u;
         if constexpr (SRC == OPERAND_MX4) sv[j] = i < NP ? sx[j][i < NP ? i : 0] : token_scales(t, row[i], on[i], min(s0 + 4 * j, steps - 1), q);
       }
 #pragma unroll
-      for (int j = 0; j < U; j++) {
-        if (s0 + j >= steps) break;
-        if constexpr (SRC == LDS_MX4) {
-          const int kb = 4 * (s0 + j) + q, at = kb * t.T + row[i];
-          const bool there = on[i] && 32 * kb < t.K;
-          op(j, i, s0, there ? *reinterpret_cast<const u32x4*>(t.p + at * 16) : u32x4{0u, 0u, 0u, 0u}, there ? (uint32_t)(uint8_t)t.scales[at] : 0u, acc);
-        } else {
-          op(j, i, s0, v[j], sv[MX4 ? j / 4 : 0] >> (8 * ((s0 + j) & 3)), acc);
+      for (int a = 0; a < U / C * P; a++) {
+        const int j0 = a / P * C;
+        u32x4 v[C];
+#pragma unroll
+        for (int j = 0; j < C; j++) {
+          if constexpr (SRC == LDS_MX4) {
+            v[j] = u32x4{0u, 0u, 0u, 0u};
+          } else {
+            v[j] = i < NP ? x[j0 + j][i < NP ? i : 0][a % P] : token(t, row[i], on[i], min(s0 + j0 + j, steps - 1), q, a % P);
+          }
+        }
+#pragma unroll
+        for (int c = 0; c < C; c++) {
+          const int j = j0 + c;
+          if (s0 + j >= steps) break;
+          if constexpr (SRC == LDS_MX4) {
+            const int kb = 4 * (s0 + j) + q, at = kb * t.T + row[i];
+            const bool there = on[i] && 32 * kb < t.K;
+            op(j, i, s0, there ? *reinterpret_cast<const u32x4*>(t.p + at * 16) : u32x4{0u, 0u, 0u, 0u}, there ? (uint32_t)(uint8_t)t.scales[at] : 0u, acc);
+          } else {
+            op(j, i, s0, v[c], sv[MX4 ? j / 4 : 0] >> (8 * ((s0 + j) & 3)), acc);
+          }
         }
       }
       if constexpr (NT > 1 && MX4) {                           // (where the groups' paths part, the compiler may move accumulators)
@@ -276,7 +292,7 @@ struct UpArgs {
   int steps, K, F, T;                  // steps of K; features
   Gate gate;
   const char* x; const char* x_scales; // bf16 [T][K], or the operand form
-  char* h; char* h_scales; int h_steps;   // bf16 rows [..][F], or the mx4 operand form
+  char* h; char* h_scales; int h_steps;   // the operand form, of values in two parts or of mx4
   const MoePlan* plan; int k;          // MOE
   MoePlan* plan_out; const double* logits; int n_parts, E, renormalise; int* picks; float* shares;   // MOE_ONE: parts of the logits, where the choice goes
 };
@@ -406,7 +422,12 @@ __global__ void __launch_bounds__(64 * W, NT == 1 && WHO != MOE_ONE ? 4 : 2) few
         if (at < n && f == 0) e.h_scales[mx4_scale_at(dest, block, e.h_steps)] = (char)code;
       } else {
         const int feat = 32 * block + (RG == 4 ? f : 8 * (f >> 2) + 4 * half + (f & 3));
-        if (at < n) reinterpret_cast<uint16_t*>(e.h)[(size_t)dest * e.F + feat] = (uint16_t)pack_bf16x2(h, 0.f);
+        const uint32_t parts = two_parts(h);
+        uint16_t* to = reinterpret_cast<uint16_t*>(e.h + parts_at(dest, block, (feat >> 3) & 3, e.F)) + (feat & 7);
+        if (at < n) {
+          to[0] = (uint16_t)parts;
+          to[512] = (uint16_t)(parts >> 16);
+        }
       }
     }
   }
@@ -488,22 +509,24 @@ struct DownArgs {
   float* parts;                        // [splits][T][D]
   uint16_t* out;
 };
-constexpr int SUM = 20;                                    // pitch of a token's 16 channels
-constexpr int down_lds(int T) { return WAVES * T * SUM * 4; }
+constexpr int down_pitch(int groups) { return 16 * groups + 4; }   // of a token's channels of a strip
+constexpr int down_lds(int T, int groups) { return WAVES * T * down_pitch(groups) * 4; }
 
-// A wave takes units of eight steps of any expert; an op's 16 tokens go to their rows of the wave's sums with their shares (a read and a write of LDS, no atomics: the wave has
+// A wave takes units of 8 KiB of any expert's weights; an op's 16 tokens go to their rows of the wave's sums with their shares (a read and a write of LDS, no atomics: the wave has
 // its own), so that neither a row of Y for each expert nor its sum over the experts goes through memory.  The waves' sums are added up in the waves' order.
-// grid (D / 16, splits).  Where the strips are few, several workgroups share one's experts, and a second kernel adds up (tickets instead, with sums past the L2s: 21 -> 24.8 us
+// A strip reads the activations of all its experts' tokens, 4 bytes a value in parts, from L2, and a CU takes in weights and activations at 39 KB a us together: with 16 channels a
+// strip, 64 tokens of 64 experts of 4096 x 2048, each meant as many bytes, 215 us; 32 channels (RG 2) 182, 64 (RG 4) 165 (moe_down_groups).
+// grid (D / (16 RG), splits).  Where the strips are few, several workgroups share one's experts, and a second kernel adds up (tickets instead, with sums past the L2s: 21 -> 24.8 us
 // for 1 token of 2048 x 1024).
-template <bool MX4, int NT>
+template <bool MX4, int NT, int RG>
 __global__ void __launch_bounds__(THREADS, 2) moe_down_kernel(DownArgs e) {
-  constexpr int U = 8, SRC = MX4 ? OPERAND_MX4 : ROWS_BF16;
+  constexpr int U = 8 / RG, SUM = down_pitch(RG), SRC = MX4 ? OPERAND_MX4 : OPERAND_PARTS;
   extern __shared__ __attribute__((aligned(16))) float sums[];   // [wave][token][SUM]
   __shared__ int active[MOE_E], start[MOE_E + 1], list[MOE_PAIRS];
   __shared__ float share[MOE_PAIRS];
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, q = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const unsigned id = run_of(blockIdx.y * gridDim.x + blockIdx.x, gridDim.x * gridDim.y), splits = gridDim.y;
-  const int strip = (int)(id / splits), split = (int)(id - strip * splits), block = strip >> 2, g0 = strip & 3, stride = WAVES * (int)splits;
+  const int strip = (int)(id / splits), split = (int)(id - strip * splits), block = strip / (4 / RG), g0 = strip % (4 / RG) * RG, stride = WAVES * (int)splits;
   for (int i = tid; i < WAVES * e.T * SUM; i += THREADS) sums[i] = 0.f;
   const int n_active = e.plan->n_active;
   for (int i = tid; i < e.T * e.k; i += THREADS) {
@@ -516,64 +539,81 @@ __global__ void __launch_bounds__(THREADS, 2) moe_down_kernel(DownArgs e) {
   float* mine = sums + wave * e.T * SUM;
   const Tokens x{e.h, e.h_scales, e.F, e.h_steps, 0};
   const int units = (e.steps + U - 1) / U, total = n_active * units;   // units of U steps, the experts' one after the other, dealt out to the waves
-  // of unit i: the strip, and the lane's row of the first 16 of the expert's tokens
   auto strip_of = [&](int i) {
     const char* codes = e.w + (size_t)uniform(active[i / units]) * e.w_stride;
     return Strip{codes + (size_t)block * e.steps * MX4_PANEL + g0 * 1024, codes + e.scales_at + (size_t)block * ((e.steps + 3) >> 2) * 1024 + g0 * 256, e.steps};
   };
-  auto first_rows = [&](int i, int (&row)[1], bool (&on)[1]) {
-    row[0] = start[i / units] + c;
-    on[0] = row[0] < start[i / units + 1];
+  using Piece = Unit<SRC, RG, U, 1>;
+  struct Rows { int row[1]; bool on[1]; };
+  // (lanes without a token read the expert's first: a column of an op is a token's alone, and theirs are not used)
+  auto load = [&](Piece& u, Rows& rows, int i) {
+    const int first = start[i / units];
+    rows.on[0] = first + c < start[i / units + 1];
+    rows.row[0] = first + (rows.on[0] ? c : 0);
+    u.load(strip_of(i), x, rows.row, rows.on, i % units * U, lane);
   };
-  Unit<SRC, 1, U, 1> now, next;
-  int i = split * WAVES + wave, row_n[1], row_f[1];
-  bool on_n[1], on_f[1];
-  if (i < total) {
-    first_rows(i, row_f, on_f);
-    now.load(strip_of(i), x, row_f, on_f, i % units * U, lane);
-  }
-  for (; i < total; i += stride) {
-    const bool more = i + stride < total;
-    if (more) {
-      first_rows(i + stride, row_n, on_n);
-      next.load(strip_of(i + stride), x, row_n, on_n, (i + stride) % units * U, lane);
-    }
+  auto work = [&](const Piece& u, const Rows& rows, int i) {
     const int first = uniform(start[i / units]), n = uniform(start[i / units + 1]) - first, groups = (n + 15) >> 4;
     int row[NT];
     bool on[NT];
-    row[0] = row_f[0];
-    on[0] = on_f[0];
+    row[0] = rows.row[0];
+    on[0] = rows.on[0];
 #pragma unroll
     for (int g = 1; g < NT; g++) {
-      row[g] = first + 16 * g + c;
       on[g] = 16 * g + c < n;
+      row[g] = first + (on[g] ? 16 * g + c : 0);
     }
-    f32x4 acc[1][NT];
+    f32x4 acc[RG][NT];
 #pragma unroll
-    for (int g = 0; g < NT; g++) acc[0][g] = f32x4{0.f, 0.f, 0.f, 0.f};
-    now.ops(x, row, on, groups, i % units * U, e.steps, q, acc);
+    for (int r = 0; r < RG; r++)
+#pragma unroll
+      for (int g = 0; g < NT; g++) acc[r][g] = f32x4{0.f, 0.f, 0.f, 0.f};
+    u.ops(x, row, on, groups, i % units * U, e.steps, q, acc);
     settle(acc);
 #pragma unroll
     for (int g = 0; g < NT; g++)
       if (on[g]) {                                         // (a token chooses an expert once: no two lanes of a quarter have the same one)
         const float p = share[row[g]];
         f32x4* to = reinterpret_cast<f32x4*>(mine + list[row[g]] / e.k * SUM + 4 * q);
-        f32x4 y = *to;
 #pragma unroll
-        for (int v = 0; v < 4; v++) y[v] += p * acc[0][g][v];
-        *to = y;
+        for (int r = 0; r < RG; r++) {
+          f32x4 y = to[4 * r];
+#pragma unroll
+          for (int v = 0; v < 4; v++) y[v] += p * acc[r][g][v];
+          to[4 * r] = y;
+        }
       }
-    if (more) now = next;
-    row_f[0] = row_n[0];
-    on_f[0] = on_n[0];
+  };
+  // (two units in turn, and the last apart: where paths with and without loads under way meet, the compiler waits for all of them)
+  int i = split * WAVES + wave;
+  if (i < total) {
+    Piece one, two;
+    Rows rows1, rows2;
+    load(one, rows1, i);
+    for (;;) {
+      if (i + stride >= total) {
+        work(one, rows1, i);
+        break;
+      }
+      load(two, rows2, i + stride);
+      work(one, rows1, i);
+      i += stride;
+      if (i + stride >= total) {
+        work(two, rows2, i);
+        break;
+      }
+      load(one, rows1, i + stride);
+      work(two, rows2, i);
+      i += stride;
+    }
   }
   __syncthreads();
-  for (int o = tid; o < 16 * e.T; o += THREADS) {
-    const int r = o & 15, t = o >> 4;
+  for (int o = tid; o < 16 * RG * e.T; o += THREADS) {
+    const int r = o % (16 * RG), t = o / (16 * RG);
     float y = 0.f;
 #pragma unroll
     for (int k = 0; k < WAVES; k++) y += sums[(k * e.T + t) * SUM + r];
-    const size_t at = (size_t)t * e.D + 64 * block + channel_of(g0, r);
+    const size_t at = (size_t)t * e.D + 64 * block + channel_of(g0 + r / 16, r % 16);
     if (splits == 1) e.out[at] = (uint16_t)pack_bf16x2(y, 0.f);
     else e.parts[(size_t)split * e.T * e.D + at] = y;
   }
@@ -722,13 +762,21 @@ int launch_moe_up(const UpArgs& a, int slots, hipStream_t s) {
   if (a.T <= 16) return launch_up_tokens<SRC, MOE>(a, slots, s);
   return moe_crowded(a.T, a.k, a.E) ? launch_up_one<SRC, 4, MOE, 4, 8>(a, slots, s) : launch_up_tokens<SRC, MOE, true>(a, slots, s);
 }
-template <bool MX4, int NT>
+template <bool MX4, int NT, int RG>
 int launch_down(const DownArgs& a, int splits, hipStream_t s) {
-  auto kern = moe_down_kernel<MX4, NT>;
+  auto kern = moe_down_kernel<MX4, NT, RG>;
   static std::atomic<bool> configured[MAX_DEVICES] = {};
-  if (int rc = ensure_dynamic_lds(reinterpret_cast<const void*>(kern), down_lds(MOE_TOKENS), configured)) return rc;
-  hipLaunchKernelGGL(kern, dim3((unsigned)(a.D / 16), (unsigned)splits), dim3(THREADS), down_lds(a.T), s, a);
+  if (int rc = ensure_dynamic_lds(reinterpret_cast<const void*>(kern), down_lds(MOE_TOKENS, RG), configured)) return rc;
+  hipLaunchKernelGGL(kern, dim3((unsigned)(a.D / (16 * RG)), (unsigned)splits), dim3(THREADS), down_lds(a.T, RG), s, a);
   return (int)hipGetLastError();
+}
+template <int NT>
+int launch_down_groups(const DownArgs& a, int groups, int splits, hipStream_t s) {
+  switch (groups) {
+    case 4: return launch_down<false, NT, 4>(a, splits, s);
+    case 2: return launch_down<false, NT, 2>(a, splits, s);
+    default: return launch_down<false, NT, 1>(a, splits, s);
+  }
 }
 template <int RG, int SRC, int NT>
 int launch_rows_tokens(const RowsArgs& a, hipStream_t s) {
@@ -786,9 +834,9 @@ int launch_moe_experts(const MoeCall& m, const MoeWeights& w, const Mx4Operand* 
   d.h = up.h; d.h_scales = h.scales; d.h_steps = h.steps;
   d.plan = up.plan; d.out = static_cast<uint16_t*>(m.Y);
   d.parts = static_cast<float*>(m.parts);
-  const int splits = moe_down_splits(D / 16, slots * ((d.steps + 7) / 8));
-  const int rc = T <= 16 ? (w.mx4 ? launch_down<true, 1>(d, splits, s) : launch_down<false, 1>(d, splits, s))
-                         : (w.mx4 ? launch_down<true, 4>(d, splits, s) : launch_down<false, 4>(d, splits, s));
+  const int groups = w.mx4 ? 1 : moe_down_groups(T, D, F), splits = moe_down_splits(D / (16 * groups), slots * ((d.steps * groups + 7) / 8));
+  const int rc = T <= 16 ? (w.mx4 ? launch_down<true, 1, 1>(d, splits, s) : launch_down_groups<1>(d, groups, splits, s))
+                         : (w.mx4 ? launch_down<true, 4, 1>(d, splits, s) : launch_down_groups<4>(d, groups, splits, s));
   if (rc || splits == 1) return rc;
   hipLaunchKernelGGL((edge_sum_kernel<false>), dim3((unsigned)((D / 4 * T + 255) / 256)), dim3(256), 0, s, static_cast<const uint32_t*>(m.parts), splits, D, T, I8Scales{},
                      static_cast<uint16_t*>(m.Y));

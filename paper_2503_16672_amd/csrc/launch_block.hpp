@@ -78,7 +78,7 @@ constexpr int MOE_TOKENS = 64, MOE_MAX_E = 256, MOE_MAX_K = 16;
 struct MoeWeights { bool mx4; const void *up, *down; size_t up_stride, down_stride, up_scales, down_scales; };
 size_t moe_parts_size(int T, int D, int E);
 size_t moe_plan_size();                          // zero before its first use
-// of a call: logits: moe_parts_size bytes; plan: moe_plan_size; parts: MOE_SPLITS T D floats; H: rows of bf16, or the operand form of h_rows rows
+// of a call: logits: moe_parts_size bytes; plan: moe_plan_size; parts: MOE_SPLITS T D floats; H: 4 F bytes for each of its rows (in 16s), or the mx4 operand form of h_rows rows
 struct MoeCall { const void *X, *Wr; int T, D, F, E, k; bool renormalise; void *logits, *plan; int* picks; float* shares; void* H; int h_rows; void *parts, *Y; };
 int launch_moe_route(const MoeCall& m, const Mx4Operand* x, hipStream_t s);   // x: the tokens as mx4 go there
 int launch_moe_experts(const MoeCall& m, const MoeWeights& w, const Mx4Operand* x, float c1, float c3, hipStream_t s);
