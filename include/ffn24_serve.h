@@ -24,11 +24,11 @@ FFN24_API int quantise_mx4(const void* X, int64_t T, int64_t K, ffn24_norm_dtype
 FFN24_API int dequantise_mx4(const void* codes, const void* scales, int64_t T, int64_t K, ffn24_norm_dtype dtype, void* Y, void* stream);
 
 /* Weights W [K][N] for the products, blocks along K, laid out once: mx4_weight_bytes(K, N) bytes at `out`, to be used with the same K and N.  mx4_weight quantises bf16;
- * mx4_weight_codes takes codes [N][K / 2] and scales [N][K / 32] that are mx4 already.  halves != 0: W is [Wg | Wu] of a gated block, for gated_mx4 (N a multiple of 64).
- * K a multiple of 32, at most 2^17; N a multiple of 8, at most 2^20. */
+ * mx4_weight_codes takes codes [N][K / 2] and scales [N][K / 32] that are mx4 already.  reserved: 0, anything else is FFN24_ERR_SHAPE (the contexts below lay out their own
+ * weights).  K a multiple of 32, at most 2^17; N a multiple of 8, at most 2^20. */
 FFN24_API int64_t mx4_weight_bytes(int64_t K, int64_t N);   /* or -1 for sizes out of range */
-FFN24_API int mx4_weight(const void* W, int64_t K, int64_t N, int halves, void* out, void* stream);
-FFN24_API int mx4_weight_codes(const void* codes, const void* scales, int64_t K, int64_t N, int halves, void* out, void* stream);
+FFN24_API int mx4_weight(const void* W, int64_t K, int64_t N, int reserved, void* out, void* stream);
+FFN24_API int mx4_weight_codes(const void* codes, const void* scales, int64_t K, int64_t N, int reserved, void* out, void* stream);
 /* Y [T][N] = bf16(X4 W4): bf16 X [T][K] to mx4 on the way, sums in fp32.  T at most 2^20.  scratch: linear_mx4_scratch(T, K, N) bytes, used until the call's last
  * kernel has run. */
 FFN24_API int64_t linear_mx4_scratch(int64_t T, int64_t K, int64_t N);   /* or -1 */

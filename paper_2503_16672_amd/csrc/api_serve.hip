@@ -69,18 +69,18 @@ int dequantise_mx4(const void* codes, const void* scales, int64_t T, int64_t K, 
 
 int64_t mx4_weight_bytes(int64_t K, int64_t N) { return sizes(K, N) ? mx4_operand_size(N, K) : -1; }
 
-int mx4_weight(const void* W, int64_t K, int64_t N, int halves, void* out, void* stream) {
-  if (!sizes(K, N) || (halves && N % 64)) return FFN24_ERR_SHAPE;
+int mx4_weight(const void* W, int64_t K, int64_t N, int reserved, void* out, void* stream) {
+  if (!sizes(K, N) || reserved) return FFN24_ERR_SHAPE;
   if (!W || !out) return FFN24_ERR_NULL;
   if (misaligned(W, out)) return FFN24_ERR_ALIGN;
-  return done(launch_mx4_weight(W, (int)K, (int)N, halves != 0, 1, out, static_cast<hipStream_t>(stream)));
+  return done(launch_mx4_weight(W, (int)K, (int)N, false, 1, out, static_cast<hipStream_t>(stream)));
 }
 
-int mx4_weight_codes(const void* codes, const void* scales, int64_t K, int64_t N, int halves, void* out, void* stream) {
-  if (!sizes(K, N) || (halves && N % 64)) return FFN24_ERR_SHAPE;
+int mx4_weight_codes(const void* codes, const void* scales, int64_t K, int64_t N, int reserved, void* out, void* stream) {
+  if (!sizes(K, N) || reserved) return FFN24_ERR_SHAPE;
   if (!codes || !scales || !out) return FFN24_ERR_NULL;
   if (misaligned(codes, scales, out)) return FFN24_ERR_ALIGN;
-  return done(launch_mx4_weight_codes(codes, scales, (int)K, (int)N, halves != 0, out, static_cast<hipStream_t>(stream)));
+  return done(launch_mx4_weight_codes(codes, scales, (int)K, (int)N, out, static_cast<hipStream_t>(stream)));
 }
 
 int64_t linear_mx4_scratch(int64_t T, int64_t K, int64_t N) {

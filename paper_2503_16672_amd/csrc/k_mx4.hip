@@ -125,13 +125,14 @@ __global__ void __launch_bounds__(256) mx4_tokens_kernel(const uint16_t* __restr
 }
 
 // Weights to the operand form, a workgroup 64 rows and a step: lane = channel of the block, wave = quarter of the step.  FORM 0: bf16 W [K][N] to mx4; 1: codes [N][K / 2] and
-// scales [N][K / 32]; 2: bf16 W as bf16, 32 k a step.  F > 0: W is [gate | up] of F channels each.  grid (blocks, steps, matrices)
+// scales [N][K / 32]; 2: bf16 W as bf16, 32 k a step.  F > 0: bf16 W is [gate | up] of F channels each.  grid (blocks, steps, matrices)
 enum { FROM_BF16 = 0, FROM_CODES = 1, KEEP_BF16 = 2 };
 template <int FORM>
 __global__ void __launch_bounds__(256) operand_weight_kernel(const void* __restrict__ W, const uint8_t* __restrict__ Ws, int K, int N, int F, int steps, char* __restrict__ codes,
                                                              char* __restrict__ scales, size_t w_stride, size_t code_stride, size_t scale_stride) {
   constexpr int KS = FORM == KEEP_BF16 ? 32 : MX4_STEP, KQ = KS / 4;
   const int block = blockIdx.x, step = blockIdx.y, lane = threadIdx.x & 63, q = threadIdx.x >> 6, k0 = KS * step + KQ * q;
+  if constexpr (FORM == FROM_CODES) F = 0;
   const int n = F > 0 ? 32 * block + (lane & 31) + (lane >> 5) * F : 64 * block + lane;
   const int row = (2 * (lane >> 5) + ((lane >> 2) & 1)) * 16 + 4 * ((lane >> 3) & 3) + (lane & 3);
   const bool in = k0 < K && (F > 0 ? 32 * block + (lane & 31) < F : n < N);
@@ -226,10 +227,10 @@ int launch_mx4_weight(const void* W, int K, int N, bool halves, int count, void*
                      halves ? N / 2 : 0, o.steps, const_cast<char*>(o.codes), const_cast<char*>(o.scales), (size_t)K * N, size, size);
   return (int)hipGetLastError();
 }
-int launch_mx4_weight_codes(const void* codes, const void* scales, int K, int N, bool halves, void* out, hipStream_t s) {
+int launch_mx4_weight_codes(const void* codes, const void* scales, int K, int N, void* out, hipStream_t s) {
   const Mx4Operand o = mx4_operand(out, N, K);
   hipLaunchKernelGGL((operand_weight_kernel<FROM_CODES>), dim3((unsigned)((N + 63) / 64), (unsigned)o.steps), dim3(256), 0, s, codes, static_cast<const uint8_t*>(scales), K, N,
-                     halves ? N / 2 : 0, o.steps, const_cast<char*>(o.codes), const_cast<char*>(o.scales), (size_t)0, (size_t)0, (size_t)0);
+                     0, o.steps, const_cast<char*>(o.codes), const_cast<char*>(o.scales), (size_t)0, (size_t)0, (size_t)0);
   return (int)hipGetLastError();
 }
 int launch_bf16_weight(const void* W, int K, int N, bool halves, int count, void* out, hipStream_t s) {

@@ -64,7 +64,7 @@ Mx4Operand mx4_operand(const void* p, int rows, int K);
 // `count` matrices W [K][N] one after the other
 int launch_mx4_weight(const void* W, int K, int N, bool halves, int count, void* out, hipStream_t s);
 int launch_bf16_weight(const void* W, int K, int N, bool halves, int count, void* out, hipStream_t s);
-int launch_mx4_weight_codes(const void* codes, const void* scales, int K, int N, bool halves, void* out, hipStream_t s);
+int launch_mx4_weight_codes(const void* codes, const void* scales, int K, int N, void* out, hipStream_t s);
 int launch_mx4_tokens(const void* X, int T, int K, const Mx4Operand& out, hipStream_t s);
 size_t mx4_split_scratch(int M, int N, int K);
 int launch_mx4_product(const Mx4Operand& w, int M, const Mx4Operand& x, int T, void* Y, const Scratch& scratch, hipStream_t s);
