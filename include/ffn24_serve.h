@@ -26,7 +26,9 @@ FFN24_API int dequantise_mx4(const void* codes, const void* scales, int64_t T, i
 /* Weights W [K][N] for the products, blocks along K, laid out once: mx4_weight_bytes(K, N) bytes at `out`, to be used with the same K and N.  mx4_weight quantises bf16;
  * mx4_weight_codes takes codes [N][K / 2] and scales [N][K / 32] that are mx4 already.  reserved: 0, anything else is FFN24_ERR_SHAPE (the contexts below lay out their own
  * weights).  K a multiple of 32, at most 2^17; N a multiple of 8, at most 2^20. */
-FFN24_API int64_t mx4_weight_bytes(int64_t K, int64_t N);   /* or -1 for sizes out of range */
+/* ceil(N / 64) (4096 s + 1024 ceil(s / 4)) with s = ceil(K / 128): 17/32 of a byte a value where N is a multiple of 64 and K of 512, more where blocks are filled up;
+ * -1 for sizes out of range */
+FFN24_API int64_t mx4_weight_bytes(int64_t K, int64_t N);
 FFN24_API int mx4_weight(const void* W, int64_t K, int64_t N, int reserved, void* out, void* stream);
 FFN24_API int mx4_weight_codes(const void* codes, const void* scales, int64_t K, int64_t N, int reserved, void* out, void* stream);
 /* Y [T][N] = bf16(X4 W4): bf16 X [T][K] to mx4 on the way, sums in fp32.  T at most 2^20.  scratch: linear_mx4_scratch(T, K, N) bytes, used until the call's last
@@ -35,8 +37,8 @@ FFN24_API int64_t linear_mx4_scratch(int64_t T, int64_t K, int64_t N);   /* or -
 FFN24_API int linear_mx4(const void* X, int64_t T, const void* weight, int64_t K, int64_t N, void* Y, void* scratch, void* stream);
 
 /* The gated block on mx4 weights: G, U from such products of X and [Wg | Wu], in fp32;  h = a(G) U;  H4 = mx4(h), blocks along F;  Y = bf16(H4 Wd4).  T, D, F, gate as
- * for gated_ctx_create, D and F at most 2^17.  Workspace: 17/32 bytes for each value of X, H and the weights, and what a split reduction takes (some tens of MiB at
- * most).  gated_mx4_set_weights quantises Wgu [D][2 F] and Wd [F][D] (bf16) into the context, which does not need them afterwards;
+ * for gated_ctx_create, D and F at most 2^17.  Workspace: mx4_weight_bytes(D, 2 F) + (F, D) for the weights, mx4_weight_bytes(D, T) for X, (F, T) for H (T filled up to 8s), and what a
+ * split reduction takes (some tens of MiB at most).  gated_mx4_set_weights quantises Wgu [D][2 F] and Wd [F][D] (bf16) into the context, which does not need them afterwards;
  * gated_mx4_fwd before it returns FFN24_ERR_STATE. */
 typedef struct gated_mx4_ctx gated_mx4_ctx;
 FFN24_API int gated_mx4_ctx_create(gated_mx4_ctx** out, int64_t T, int64_t D, int64_t F, ffn24_gate gate);
@@ -50,8 +52,8 @@ FFN24_API int gated_mx4_fwd(gated_mx4_ctx* ctx, const void* X, int64_t T, void* 
  *   y = bf16(sum over the chosen of p_e (h_e Wd_e)),  h_e = a(x Wg_e) (x Wu_e), sums in fp32;
  * FFN24_EXPERTS_BF16: h_e is held to 2^-16 of it, as two bf16;  FFN24_EXPERTS_MX4: x, h_e and the weights are mx4 (the router is not).
  * 1 <= T <= 64 (every call says how many it has), D and F multiples of 64, D at most 2^14, F at most 2^16, 1 <= E <= 256, 1 <= k <= min(E, 16).  moe_set_weights lays out Wr,
- * Wgu [E][D][2 F] and Wd [E][F][D] in the context (their size, in mx4 17/64 of it), which does not need them afterwards.  Workspace besides:
- * at most 49 MiB + 4 KiB F.  moe_fwd stores the choice too where experts (int32 [T][k], by falling l) and shares (fp32 [T][k]) are given: both or
+ * Wgu [E][D][2 F] and Wd [E][F][D] in the context (their size, Wr's with E filled up to 64s; in mx4 E (mx4_weight_bytes(D, 2 F) + mx4_weight_bytes(F, D))), which does not need
+ * them afterwards.  Workspace besides: at most 49 MiB + 4 KiB F.  moe_fwd stores the choice too where experts (int32 [T][k], by falling l) and shares (fp32 [T][k]) are given: both or
  * neither.  No other token's values enter a token's result, and results repeat bit for bit; the order of its sums may depend on how many tokens
  * there are and which experts they chose.  The contexts' other rules are those of gated_ctx. */
 typedef enum { FFN24_EXPERTS_BF16 = 0, FFN24_EXPERTS_MX4 = 1 } ffn24_experts;
