@@ -422,12 +422,10 @@ __global__ void __launch_bounds__(64 * W, NT == 1 && WHO != MOE_ONE ? 4 : 2) few
         if (at < n && f == 0) e.h_scales[mx4_scale_at(dest, block, e.h_steps)] = (char)code;
       } else {
         const int feat = 32 * block + (RG == 4 ? f : 8 * (f >> 2) + 4 * half + (f & 3));
-        const uint32_t parts = two_parts(h);
-        uint16_t* to = reinterpret_cast<uint16_t*>(e.h + parts_at(dest, block, (feat >> 3) & 3, e.F)) + (feat & 7);
-        if (at < n) {
-          to[0] = (uint16_t)parts;
-          to[512] = (uint16_t)(parts >> 16);
-        }
+        // two neighbours' first parts go out from the even lane, their rests from the odd one
+        const uint32_t mine = two_parts(h), other = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)mine, quad_perm(1, 0, 3, 2), 0xF, 0xF, true);
+        const uint32_t two = f & 1 ? other >> 16 | (mine & 0xFFFF0000u) : (mine & 0xFFFFu) | other << 16;
+        if (at < n) *reinterpret_cast<uint32_t*>(e.h + parts_at(dest, block, (feat >> 3) & 3, e.F) + 1024 * (f & 1) + 2 * (feat & 6)) = two;
       }
     }
   }
