@@ -12,9 +12,9 @@
 //   up       a workgroup a strip of 32 features of a chosen expert: h = a(G) U for the tokens that chose it; a row of H for each (token, choice), in the experts' order
 //   down     a workgroup a strip of 16 to 64 channels and all chosen experts one after the other: the shares' sum stays in LDS, in the order of the experts
 //   sum      where several workgroups share a strip's experts (moe_down_splits): their sums, in a fixed order
-// us, kernel by kernel (in brackets weights' bytes a second): 64 tokens, 4096 x 2048, all of 64 bf16 experts 5.0, 5.8, up 312 (6.9 TB/s), down 166 (6.5); 8 tokens of 64 mx4
-// experts 5.0, 5.9, 61.5 (5.9), 35 (5.3); 37 tokens, 1088 x 704, 24 bf16 experts 4.2, 5.8, 15.3 (4.8), 10.8, 3.9; 1 token, 2048 x 1024, 4 of 32 4.0, -, 8.0 (with the choice),
-// 7.0.  The large ones run at the rate of the largest copy (6.4 TB/s); what bounds the small ones is the launches and each one's way through memory and LDS.
+// us, kernel by kernel (in brackets weights' bytes a second): 64 tokens, 4096 x 2048, all of 64 bf16 experts 4.8, 5.6, up 319 (6.7 TB/s), down 160 (6.7), 4.8; 8 tokens of 64 mx4
+// experts 5.0, 6.0, 62.4 (5.8), 34.6 (5.2); 37 tokens, 1088 x 704, 24 bf16 experts 4.3, 5.8, 16.4 (4.5), 11.7, 3.9; 1 token, 2048 x 1024, 4 of 32 3.8, -, 7.9 (with the choice),
+// 7.8.  The large ones run at 0.95 of the rate of reads alone (7.1 TB/s of 4 GiB); what bounds the small ones is the launches and each one's way through memory and LDS.
 #include "mx4_core.hpp"
 #include "mx4_rule.hpp"
 #include "stream_core.hpp"
@@ -513,7 +513,7 @@ constexpr int down_lds(int T, int groups) { return WAVES * T * down_pitch(groups
 // A wave takes units of 8 KiB of any expert's weights; an op's 16 tokens go to their rows of the wave's sums with their shares (a read and a write of LDS, no atomics: the wave has
 // its own), so that neither a row of Y for each expert nor its sum over the experts goes through memory.  The waves' sums are added up in the waves' order.
 // A strip reads the activations of all its experts' tokens, 4 bytes a value in parts, from L2, and a CU takes in weights and activations at 39 KB a us together: with 16 channels a
-// strip, 64 tokens of 64 experts of 4096 x 2048, each meant as many bytes, 215 us; 32 channels (RG 2) 182, 64 (RG 4) 165 (moe_down_groups).
+// strip, 64 tokens of 64 experts of 4096 x 2048, each meant as many bytes, 215 us; 32 channels (RG 2) 175, 64 (RG 4) 160 (moe_down_groups).
 // grid (D / (16 RG), splits).  Where the strips are few, several workgroups share one's experts, and a second kernel adds up (tickets instead, with sums past the L2s: 21 -> 24.8 us
 // for 1 token of 2048 x 1024).
 template <bool MX4, int NT, int RG>

@@ -1,8 +1,8 @@
 // mx4 numbers (mx4_core.hpp): quantisation and back, the weights' layout, the products of many tokens.
 //
 //   scale = 2^(floor(log2 max |block|) - 2) over 32 neighbours of a row (no less than 2^-127);  code = x / scale to the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (ties to the even
-// code) Both rounding kernels and the tokens' are bound by memory and move every byte once, 16 bytes a lane, non-temporal: 16384 x 4096 bf16 26 us to codes and scales and 28 back
-// (170 MB, 6.4 and 6.0 TB/s: the largest copy here reaches 6.4), 1031 x 1056 fp32 2.9 and 3.5 us (a launch); 8192 x 4096 tokens to the operand form 17 us (5.0 TB/s).  The
+// code).  Both rounding kernels and the tokens' are bound by memory and move every byte once, 16 bytes a lane, non-temporal: 16384 x 4096 bf16 26 us to codes and scales and 28 back
+// (170 MB, 6.4 and 6.0 TB/s: the largest copy here reaches 6.4, reads alone 7.1), 1031 x 1056 fp32 2.9 and 3.5 us (a launch); 8192 x 4096 tokens to the operand form 17 us (5.0 TB/s).  The
 // weights' layout, once: 4096 x 16384 42 us.
 #include "mx4_core.hpp"
 #include "launch_edge.hpp"

@@ -86,7 +86,7 @@ struct Mx4Geo {
   static constexpr int UNROLL = RING == 4 ? 4 : 12;                                 // steps until ring and scales' bytes come round together
 };
 
-// The accumulator tied in place: through the builtin the compiler moves accumulators round the scaled op and runs at half its rate (4.9 against 7.1 PFLOP/s in a loop of nothing
+// The accumulator tied in place: through the builtin the compiler moves accumulators round the scaled op and runs at half its rate (5.2 against 7.16 PFLOP/s in a loop of nothing
 // else).  J: the byte of the scales' registers, the step's number of four.
 template <int J>
 __device__ __forceinline__ void op16_mx4(const u32x4& a, const u32x4& b, uint32_t sa, uint32_t sb, f32x4& c) {

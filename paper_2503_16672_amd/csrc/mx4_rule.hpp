@@ -1,4 +1,6 @@
 // Which tile, split and kernel an mx4 product takes: rules on its sizes alone.
+// Figures here are of passes over the same weights one after the other, unless "cold" is said: up to 256 MB of them are then in the last-level cache.  Cold, from HBM (copies in turn), few
+// tokens take 1 to 2 us more: 1 2048 8192 3.0, 4.3; 16 4096 4096 6.4, 7.1; 16 8192 8192 9.3, 11.4; gated 16 4096 16384 25.2, 26.6; experts 1 2048 1024 32 4 20.1, 21.5.
 #pragma once
 
 namespace ffn24 {
@@ -38,10 +40,12 @@ inline Mx4Plan mx4_plan(int M, int N, int steps, bool split) {
 
 constexpr long long MX4_SPLIT_MOST = 1LL << 21;   // results of a product that could be split: 256 tiles of 128 x 64
 
-// Few tokens: the kernels of k_experts.hip or the GEMM.  us, few tokens' kernel / GEMM.  Products (T K N): 16 4096 32768 11.2, 12.9; 16 16384 4096 8.7, 12.3; 16 8192 57344 38.3,
-// 35.9; 24 16384 4096 9.6, 12.3; 24 5440 2048 4.2, 7.6; 24 1408 512 3.4, 4.7; the other way round 24 4096 32768 14.3, 13.0; 24 2048 10880 8.6, 5.1; 24 28672 8192 26.9, 23.2: from
-// 17 tokens on where the GEMM would have to split the reduction.  Gate and up (T D F): 16 4096 16384 12.4, 13.2; 16 2048 5440 4.9, 5.4; 16 8192 28672 38.9, 36.0; 24 4096 16384
-// 16.2, 13.4; 24 2048 5440 5.8, 5.5.
+// Few tokens: the kernels of k_experts.hip or the GEMM.  us, few tokens' kernel / GEMM.  Products (T K N): 16 4096 32768 11.2, 12.9; 16 16384 4096 8.7, 12.3; 24 16384 4096 9.6, 12.3;
+// 24 5440 2048 4.2, 7.6; 24 1408 512 3.4, 4.7; the other way round 24 4096 32768 14.3, 13.0; 24 2048 10880 8.6, 5.1; 24 28672 8192 26.9, 23.2: from 17 tokens on where the GEMM would
+// have to split the reduction.  Gate and up (T D F): 16 4096 16384 12.4, 13.2; 16 2048 5440 4.9, 5.4; 24 4096 16384 16.2, 13.4; 24 2048 5440 5.8, 5.5.  Up to 16 tokens of wide layers the
+// GEMM is ahead on weights in the last-level cache and behind on cold ones, which a model's are.  Whole calls, cold: 16 8192 57344 45.0, 51.0 (warm 43.4, 39.5); 16 16384 32768 51.9, 55.1
+// (51.3, 46.9); 16 8192 28672 25.3, 29.0 (23.5, 23.4); 16 4096 65536 27.8, 31.5 (25.9, 25.4); 16 16384 16384 27.5, 33.4; 16 8192 131072 91, 112; gated 16 8192 28672 67, 75 (68, 81); 16 4096
+// 16384 26.0, 31.8; 16 8192 65536 132, 164.
 constexpr int FEW_MX4_TOKENS = 16, FEW_MX4_MORE = 32;
 inline bool mx4_few(int T, int K, int N) { return T <= FEW_MX4_TOKENS || (T <= FEW_MX4_MORE && K >= N && N <= 4096); }
 inline bool mx4_few_gated(int T) { return T <= FEW_MX4_TOKENS; }
@@ -73,7 +77,8 @@ inline int few_up_waves(int strips, int steps) { return steps < 24 && strips >= 
 inline bool few_up_halves(int strips) { return strips < 256; }
 // From 17 tokens on an expert may have more than 16: one pass over its weights with 64 tokens beside them (half the workgroups a CU, for the registers) where it has many,
 // otherwise a pass for each 16. Bf16, passes / one: 64 2048 1024 16 4 75.7, 65.6; 64 4096 2048 16 4 199, 157; 32 1088 704 8 4 30.1, 27.0; the other way round 37 1088 704 24 4
-// 38.2, 40.5; 64 2048 1024 16 2 53.5, 54.6.  At T k = 10 E (64 1088 704 24 4) 44.8, 43.3; mx4 29.9, 30.4.
+// 38.2, 40.5; 64 2048 1024 16 2 53.5, 54.6.  At T k = 10 E (64 1088 704 24 4) 44.8, 43.3; mx4 29.9, 30.4.  The choices here are spread evenly and only their mean is known to the host: where
+// all 64 tokens choose the same eight experts, passes read their gate and up weights four times (bf16 4096 2048 64 8: 241 us, where one pass over those weights is 40; spread 490).
 inline bool moe_crowded(int T, int k, int E) { return T * k > 12 * E; }
 // Groups of 16 channels a strip of the down projection has, of bf16 experts: every strip reads the tokens' activations (4 bytes a value), so wide ones read fewer bytes and narrow ones
 // are more workgroups, without or with fewer sums of a launch of their own.  1, 2, 4 groups, each with its splits: 64 4096 2048 64 8 541, 504, 491; 64 4096 2048 16 4 169, 158, 153;

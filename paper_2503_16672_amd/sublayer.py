@@ -45,7 +45,7 @@ class GatedSublayer:
             p.sub_((rate * p.float().norm().clamp(min=1.0) / g.float().norm().clamp(min=1e-20) * g).to(p.dtype))
 
     def serve(self, x, stream, int8=None):
-        """forward without a backward; int8: a context that `quantised` made, of either type."""
+        """forward without a backward; int8: a context that `quantised` made, of either type (int8 or mx4)."""
         y, stream, _, _ = block.layer_norm_fwd(x, self.norm_weight, self.norm_bias, self.eps, residual=stream)
         return (self.serving.fwd(y, self.Wgu, self.Wd) if int8 is None else int8.fwd(y)), stream
 
@@ -58,7 +58,9 @@ class GatedSublayer:
 
 
 class ExpertSublayer:
-    """The sublayer with a mixture of E gated blocks, k of them a token, for up to T <= 64 tokens a call (serving only); weights: "bf16" or "mx4"."""
+    """The sublayer with a mixture of E gated blocks, k of them a token, for up to T <= 64 tokens a call (serving only); weights: "bf16" or "mx4".
+
+    The bf16 weights it was made from stay beside the experts' own copy as Wr, Wgu and Wd; a server that has no other use for them deletes those."""
 
     def __init__(self, T: int, D: int, F: int, E: int, k: int, act: str = "silu", eps: float = 1e-5, seed: int = 0, weights: str = "bf16"):
         g = torch.Generator(device="cuda").manual_seed(seed)
