@@ -154,7 +154,7 @@ struct Unit {
       else acc[g][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w[j][g]), __builtin_bit_cast(bf16x8, v), acc[g][i], 0, 0, 0);
     }
   }
-  // the ops of the unit for `groups` groups of tokens; those from NP on are asked for here, C steps of a group (and part) together
+  // the ops of the unit for `groups` groups of tokens; those from NP on are asked for here, C steps of a group together
   template <int NT>
   __device__ __forceinline__ void ops(const Tokens& t, const int (&row)[NT], const bool (&on)[NT], int groups, int s0, int steps, int q, f32x4 (&acc)[RG][NT]) const {
 #pragma unroll
@@ -167,17 +167,18 @@ struct Unit {
         if constexpr (SRC == OPERAND_MX4) sv[j] = i < NP ? sx[j][i < NP ? i : 0] : token_scales(t, row[i], on[i], min(s0 + 4 * j, steps - 1), q);
       }
 #pragma unroll
-      for (int a = 0; a < U / C * P; a++) {
-        const int j0 = a / P * C;
-        u32x4 v[C];
+      for (int j0 = 0; j0 < U; j0 += C) {
+        u32x4 v[C][P];
 #pragma unroll
-        for (int j = 0; j < C; j++) {
-          if constexpr (SRC == LDS_MX4) {
-            v[j] = u32x4{0u, 0u, 0u, 0u};
-          } else {
-            v[j] = i < NP ? x[j0 + j][i < NP ? i : 0][a % P] : token(t, row[i], on[i], min(s0 + j0 + j, steps - 1), q, a % P);
+        for (int j = 0; j < C; j++)
+#pragma unroll
+          for (int a = 0; a < P; a++) {
+            if constexpr (SRC == LDS_MX4) {
+              v[j][a] = u32x4{0u, 0u, 0u, 0u};
+            } else {
+              v[j][a] = i < NP ? x[j0 + j][i < NP ? i : 0][a] : token(t, row[i], on[i], min(s0 + j0 + j, steps - 1), q, a);
+            }
           }
-        }
 #pragma unroll
         for (int c = 0; c < C; c++) {
           const int j = j0 + c;
@@ -187,7 +188,8 @@ struct Unit {
             const bool there = on[i] && 32 * kb < t.K;
             op(j, i, s0, there ? *reinterpret_cast<const u32x4*>(t.p + at * 16) : u32x4{0u, 0u, 0u, 0u}, there ? (uint32_t)(uint8_t)t.scales[at] : 0u, acc);
           } else {
-            op(j, i, s0, v[c], sv[MX4 ? j / 4 : 0] >> (8 * ((s0 + j) & 3)), acc);
+#pragma unroll
+            for (int a = 0; a < P; a++) op(j, i, s0, v[c][a], sv[MX4 ? j / 4 : 0] >> (8 * ((s0 + j) & 3)), acc);
           }
         }
       }
@@ -832,7 +834,7 @@ int launch_moe_experts(const MoeCall& m, const MoeWeights& w, const Mx4Operand* 
   d.h = up.h; d.h_scales = h.scales; d.h_steps = h.steps;
   d.plan = up.plan; d.out = static_cast<uint16_t*>(m.Y);
   d.parts = static_cast<float*>(m.parts);
-  const int groups = w.mx4 ? 1 : moe_down_groups(T, D, F), splits = moe_down_splits(D / (16 * groups), slots * ((d.steps * groups + 7) / 8));
+  const int groups = w.mx4 ? 1 : moe_down_groups(T * k, D, F), splits = moe_down_splits(D / (16 * groups), slots * ((d.steps * groups + 7) / 8));
   const int rc = T <= 16 ? (w.mx4 ? launch_down<true, 1, 1>(d, splits, s) : launch_down_groups<1>(d, groups, splits, s))
                          : (w.mx4 ? launch_down<true, 4, 1>(d, splits, s) : launch_down_groups<4>(d, groups, splits, s));
   if (rc || splits == 1) return rc;

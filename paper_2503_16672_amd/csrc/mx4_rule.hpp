@@ -80,13 +80,14 @@ inline bool few_up_halves(int strips) { return strips < 256; }
 // 38.2, 40.5; 64 2048 1024 16 2 53.5, 54.6.  At T k = 10 E (64 1088 704 24 4) 44.8, 43.3; mx4 29.9, 30.4.  The choices here are spread evenly and only their mean is known to the host: where
 // all 64 tokens choose the same eight experts, passes read their gate and up weights four times (bf16 4096 2048 64 8: 241 us, where one pass over those weights is 40; spread 490).
 inline bool moe_crowded(int T, int k, int E) { return T * k > 12 * E; }
-// Groups of 16 channels a strip of the down projection has, of bf16 experts: every strip reads the tokens' activations (4 bytes a value), so wide ones read fewer bytes and narrow ones
-// are more workgroups, without or with fewer sums of a launch of their own.  1, 2, 4 groups, each with its splits: 64 4096 2048 64 8 541, 504, 491; 64 4096 2048 16 4 169, 158, 153;
-// 48 3584 1024 64 4 239, 227, 224; 12 2880 1472 16 2 81.5, 78.6, 70; 64 2560 1024 16 2 65.6, 60.0, 61.0; 64 2048 768 128 8 205, 195, 197; 64 2048 1024 16 4 61.9, 59.4, 60.8; 64 1536
-// 512 16 16 66.7, 58.1, 55.0; 20 1536 1024 32 4 64.6, 60.0, 62.2; short reductions 64 8192 512 8 2 76.2, 66.5, 68.3; 64 4096 512 16 2 50.9, 51.4, 53.0; few channels 37 1088 704 24 3
-// 36.6, 37.3, 38.5; 64 512 1024 64 8 58.0, 63.5, 72.9; 37 768 1536 16 4 40.7, 41.4, 45.2 (64 1024 2048 32 4 87.8, 85.9, 94.8); few tokens 1 2048 1024 32 4 19.5, 20.0, 20.2; 2 1024 512
-// 32 4 20.7, 21.2, 22.0; 2 4096 2048 16 2 37.9, 38.3, 38.1 (1 4096 2048 64 8 72.2, 71.1, 70.9).
-inline int moe_down_groups(int T, int D, int F) { return T < 4 || D < 1280 ? 1 : D < 2560 || F < 1024 ? 2 : 4; }
+// Groups of 16 channels a strip of the down projection has, of bf16 experts (pairs: T k): every strip reads the tokens' activations (4 bytes a value), so wide ones read fewer bytes and
+// narrow ones are more workgroups, without or with fewer sums of a launch of their own.  1, 2, 4 groups, each with its splits: 64 4096 2048 64 8 541, 504, 488; 64 4096 2048 16 4 169,
+// 158, 153; 48 3584 1024 64 4 239, 227, 224; 12 2880 1472 16 2 81.5, 78.6, 70; 64 2304 1024 16 4 79, 67.5, 66.6; 64 2560 1024 16 2 66, 61.3, 62.5; 64 2048 768 128 8 205, 195, 197; 64 2048
+// 1024 16 4 61.6, 59.9, 61.1; 20 1536 1024 32 4 66.5, 60.9, 62.8; 64 1536 512 16 16 56.6, 51.7, 51.8; short reductions 64 8192 512 8 2 73, 66.0, 67.7; 64 4096 768 32 4 116, 112, 111; 64 4096
+// 512 16 2 50.3, 51.2, 53.1; few channels 64 1024 2048 32 4 89.0, 86.1, 95; 64 1024 4096 16 4 110, 105, 117; 64 1024 1024 32 4 53.8, 54.1, 60; 64 1088 704 24 4 43.4, 43.7, 46.9; 64 512 1024
+// 64 8 58.7, 64.1, 73.6; few pairs 1 2048 1024 32 4 19.5, 20.0, 20.2; 2 1024 512 32 4 20.7, 21.2, 22.0; 2 4096 2048 16 2 37.9, 38.3, 38.1; 1 4096 2048 64 8 76.8, 75.7, 75.3; 3 2048 1024 32 4
+// 42.3, 41.8, 41.6; 2 4096 2048 64 8 138, 133, 131.
+inline int moe_down_groups(int pairs, int D, int F) { return pairs < 12 || D < 1024 || (D < 1280 && F < 2048) ? 1 : D < 2560 || F < 1024 ? 2 : 4; }
 // Over how many workgroups the experts of a strip of the down projection are dealt out (`units`: of eight steps, at most, that a strip has): as many as fill the CUs, where the
 // sums' own launch does not cost more.  1 / chosen: bf16 64 2048 768 128 8 235, 202 (2); 16 2048 1024 32 4 75.2, 69.1 (2); 37 1088 704 24 4 47.1, 38.5 (3); 64 1024 2048 32 4 121,
 // 81 (4); mx4 64 2048 768 128 8 89.5, 76.5; 8 1088 704 24 4 (24 units) 24.1, 23.7; with less work than that: 1 2048 1024 32 4 bf16 (16 units) 18.9, 19.8, mx4 15.2, 17.0; and at

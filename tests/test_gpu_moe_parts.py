@@ -21,7 +21,8 @@ HELD = 2.0 ** -16
 # every kernel of bf16 experts (below): one token, whole and half strips; up to 16; more, one pass and several; down with strips of 16, 32 and 64 channels, alone and shared
 CASES = [(1, 64, 64, 1, 1), (1, 2048, 1024, 32, 4), (1, 256, 4160, 8, 4), (1, 192, 8256, 4, 2), (2, 128, 192, 5, 2), (8, 1024, 512, 64, 8), (16, 192, 320, 8, 8), (17, 576, 128, 100, 7),
          (33, 64, 448, 17, 5), (64, 512, 320, 256, 16), (64, 256, 192, 3, 1), (37, 1088, 704, 24, 3), (64, 4416, 192, 5, 4), (64, 1536, 512, 16, 16), (3, 4096, 64, 8, 2),
-         (16, 1344, 64, 4, 2), (8, 1344, 512, 16, 4), (37, 1536, 512, 16, 4), (4, 2624, 1024, 1, 1), (20, 2624, 1024, 1, 1), (9, 2880, 1472, 16, 2), (64, 2624, 1024, 12, 3), (5, 8320, 1024, 3, 2), (64, 2624, 1024, 6, 6)]
+         (16, 1344, 64, 4, 2), (8, 1344, 512, 16, 4), (37, 1536, 512, 16, 4), (4, 2624, 1024, 1, 1), (20, 2624, 1024, 1, 1), (9, 2880, 1472, 16, 2), (64, 2624, 1024, 12, 3), (5, 8320, 1024, 3, 2), (64, 2624, 1024, 6, 6),
+         (16, 2624, 1024, 1, 1), (2, 2624, 1024, 9, 8), (12, 1024, 2048, 7, 2), (50, 1152, 2112, 9, 3)]
 
 
 def _expected(X, Wr, Wgu, Wd, k, act, renormalise, kept=lambda h: h):
@@ -103,7 +104,7 @@ MAIN = """
 int main() {
   int T, D, F, E, k;
   while (std::scanf(" %%d %%d %%d %%d %%d", &T, &D, &F, &E, &k) == 5) {
-    const int groups = ffn24::moe_down_groups(T, D, F), slots = T * k < E ? T * k : E;
+    const int groups = ffn24::moe_down_groups(T * k, D, F), slots = T * k < E ? T * k : E;
     std::printf("%%d-%%d-%%s ", T <= 16 ? 1 : 4, groups, ffn24::moe_down_splits(D / (16 * groups), slots * ((F / 32 * groups + 7) / 8)) > 1 ? "shared" : "alone");
   }
 }
